@@ -376,6 +376,105 @@ orbit_status adaln_int4_quantize_weights(const uint16_t* W, int64_t N, int64_t K
 orbit_status adaln_int4_linear(const uint16_t* X, int64_t M, int64_t ldx, const uint8_t* q, const uint16_t* scales,
                                int64_t N, int64_t K, const uint16_t* bias, float* Y, int64_t ldy, void* stream);
 
+/* ------------------------------------------- between the QKV projection and attention */
+
+typedef struct orbit_rope_s* orbit_rope;
+
+/*
+ * Rows of heads, [batch][token][head][D] on the device with the D values of a head contiguous:
+ * strides in elements, ORBIT_OUT_F32 or ORBIT_OUT_BF16 values.  A view of a fused projection's
+ * output (queries, keys and values side by side) or of an attention layout ([batch][head][token])
+ * is such rows.  The data and the strides (of dimensions with more than one entry) are multiples of
+ * 16 bytes.  Strides of inputs may be 0 (broadcast); rows of an output must not overlap.
+ */
+typedef struct {
+    void* data;
+    int64_t batch, token, head;
+    int32_t heads, dtype;
+} orbit_heads;
+
+/*
+ * rope_plan -- angles of rotary positions with one to eight axes (time, height and width of a
+ * video's tokens, for example).  Axis a turns dims[a] / 2 pairs of each head; its pair j at position
+ * i by i * theta^(-2 j / dims[a]).  The axes' pairs follow each other: with D_r the sum of dims,
+ * pair p of a head is values (2p, 2p + 1), or (p, p + D_r / 2) where `halves` is 1.  Cosines and
+ * sines are computed in fp64, stored as fp32 and kept as a table per axis, on the device as for
+ * rpbh_plan (8 bytes per position and pair).
+ *   axes      1..8
+ *   dims      host, [axes]: even, their sum D_r a multiple of 8 up to 512
+ *   lengths   host, [axes]: positions 0 .. lengths[a] - 1 have angles
+ *   theta     finite, above 0
+ * Errors: ORBIT_EINVAL; ORBIT_EUNSUPPORTED (D_r, or more than 2^27 angles); ORBIT_ENOMEM; ORBIT_EHIP.
+ */
+orbit_status rope_plan(int32_t axes, const int32_t* dims, const int32_t* lengths, double theta, int32_t halves,
+                       orbit_rope* out);
+
+/*
+ * rope_plan_from_angles -- the same handle from the caller's angles (scaled, interpolated or learned
+ * positions): host fp64, axis by axis, [lengths[a]][dims[a] / 2], all finite.
+ */
+orbit_status rope_plan_from_angles(int32_t axes, const int32_t* dims, const int32_t* lengths, const double* angles,
+                                   int32_t halves, orbit_rope* out);
+
+/* Copy the plan's tables to the current device, as rpbh_plan_upload. */
+orbit_status rope_plan_upload(orbit_rope p);
+
+/* Free a plan.  NULL is ignored. */
+void rope_plan_destroy(orbit_rope p);
+
+/*
+ * axial_rope -- y = x with each head's pairs turned by the angles of the token's position: (u, v)
+ * becomes (u cos - v sin, u sin + v cos), or the opposite turn where `inverse` is 1, which is the
+ * gradient's.  Values beyond D_r are copied.  Computed in fp32.
+ *   x, y       the same heads and type; y may be x (same data and strides), else they do not overlap
+ *   B, L, D    batches, tokens, head size: a multiple of 8, D_r <= D <= 512
+ *   positions  device, int32 [B or 1][L][axes]; pos_batch elements from one batch's to the next's (0:
+ *              all share one).  They are not checked before the launch: a position outside its axis's
+ *              lengths gives NaN in the values of that axis
+ * Errors: ORBIT_EINVAL (null pointers, types, strides, alignment, a plan without tables on the device);
+ * ORBIT_EUNSUPPORTED (D, more than 2^31 - 1 head rows); ORBIT_EHIP.  B = 0 or L = 0 returns at once.
+ */
+orbit_status axial_rope(orbit_rope plan, const orbit_heads* x, const orbit_heads* y, int64_t B, int64_t L, int64_t D,
+                        const int32_t* positions, int64_t pos_batch, int32_t inverse, void* stream);
+
+/*
+ * qk_norm_rope -- the RMS norm of each query and key head and the rotation in one pass:
+ *     y = turn(x / sqrt(mean(x^2) + eps) * weight).
+ * Sums and products in fp32 (a row whose mean square passes fp32's range gives zeros), rounded
+ * once at the end.
+ *   plan, positions   as for axial_rope; plan = NULL: the norms alone, positions are not read
+ *   q, k              one type; as many heads as each has (grouped queries); k, k_out may both be NULL
+ *   q_out, k_out      one type, the heads of q and k; may be q and k themselves
+ *   q_weight, k_weight  device, [D] of w_dtype, or NULL (1)
+ *   eps               finite, >= 0
+ * Errors as for axial_rope.
+ */
+orbit_status qk_norm_rope(orbit_rope plan, const orbit_heads* q, const orbit_heads* k, const orbit_heads* q_out,
+                          const orbit_heads* k_out, int64_t B, int64_t L, int64_t D, const int32_t* positions,
+                          int64_t pos_batch, const void* q_weight, const void* k_weight, int32_t w_dtype, float eps,
+                          void* stream);
+
+/* Bytes of device workspace that weight gradients take for heads of D on the current device. */
+orbit_status qk_norm_rope_backward_workspace_size(int64_t D, size_t* bytes);
+
+/*
+ * qk_norm_rope_backward -- gradients of qk_norm_rope's inputs from those of its outputs, dq and dk
+ * (one type): q_grad and k_grad have the types of q and k, which are the forward call's inputs (not
+ * its outputs, if those replaced them).  A weight's gradient, fp32 [D], is the sum over all of its
+ * rows in a fixed order (the same bits on the same device); NULL where it is not needed.
+ *   q_grad, k_grad    may be dq and dk themselves where the types are equal, or q and k
+ *   workspace         device, aligned to 16 bytes, where a weight's gradient is asked for; its
+ *                     contents on entry do not matter, ownership as for orbit_qlinear_ws
+ * Errors as for axial_rope; ORBIT_EINVAL also for a weight's gradient without the weight and for a
+ * workspace that is too small.  Without rows (B = 0 or L = 0) the weights' gradients are zeros.
+ */
+orbit_status qk_norm_rope_backward(orbit_rope plan, const orbit_heads* dq, const orbit_heads* dk, const orbit_heads* q,
+                                   const orbit_heads* k, const orbit_heads* q_grad, const orbit_heads* k_grad, int64_t B,
+                                   int64_t L, int64_t D, const int32_t* positions, int64_t pos_batch,
+                                   const void* q_weight, const void* k_weight, int32_t w_dtype, float eps,
+                                   float* q_weight_grad, float* k_weight_grad, void* workspace, size_t workspace_bytes,
+                                   void* stream);
+
 #ifdef __cplusplus
 }
 #endif

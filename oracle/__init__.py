@@ -11,6 +11,10 @@ OrbitQuant (arXiv 2607.02461), written from the paper's definitions:
   qlinear.py   contraction of the two code sets           Sec. 4.3 (rotation cancellation)
   adaln_rtn.py INT4 RTN g64 weight-only AdaLN projection  Sec. 5 setup; Suppl. layer list; Sec. 6.2
 
+and, beside the paper's layer, of what a transformer has next to it:
+
+  attention_input.py  rotary positions with several axes, norms of queries and keys, gradients
+
 Only the tests, the package's smoke check and the benchmark's CPU-baseline leg
 may import this package.  The product path (the HIP library and its binding)
 never imports, links or executes anything here, and this package imports
@@ -31,6 +35,7 @@ from .quantize import (normalize_rows, encode, decode_levels, pack_codes, unpack
                        fp16_round, to_labels, from_labels)
 from .qlinear import layer_epilogue, qlinear, qlinear_dense_reference
 from .adaln_rtn import rtn_int4_quantize, rtn_int4_dequantize, pack_rtn_int4, unpack_rtn_int4, rtn_int4_linear
+from .attention_input import rope_angles, rope_turn, qk_norm_rope, qk_norm_rope_backward
 
 EPS_DEFAULT = 1e-10  # Sec. 4.3: the clamp guarding zero-norm (padding) tokens
 
@@ -42,4 +47,5 @@ __all__ = [
     "quantize_act", "quantize_weights", "near_tie_mask", "nearest_threshold", "bf16_round", "bf16_bits", "fp16_round", "to_labels", "from_labels",
     "qlinear", "qlinear_dense_reference", "EPS_DEFAULT",
     "rtn_int4_quantize", "rtn_int4_dequantize", "pack_rtn_int4", "unpack_rtn_int4", "rtn_int4_linear",
+    "rope_angles", "rope_turn", "qk_norm_rope", "qk_norm_rope_backward",
 ]

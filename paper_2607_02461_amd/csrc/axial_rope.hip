@@ -1,0 +1,356 @@
+// Rotary positions with several axes, alone and behind the RMS norms of queries and keys, for gfx950.
+//
+// A head of D values holds P = D_r / 2 pairs that are rotated and D - D_r values that are not.  Pair p belongs to
+// one axis of the token's position (time, height, width) and turns by angle(p, position on that axis); cosines and
+// sines come from a table per axis, made in 64 bits when the plan was.  With n = x / sqrt(mean(x^2) + eps) * w
+// for the norm of one head (n = x without it), a pair (u, v) of n becomes (u cos - v sin, u sin + v cos).
+//
+// Backward: g = dy turned by the negative angles is the gradient of n, and with r = 1 / sqrt(mean(x^2) + eps)
+//     dw = sum over rows of g x r,     dx = r (g w - x r^2 mean(g w x)).
+// r comes from x again, which has to be read anyhow; both means come out of one pass over the row.
+//
+// All of it is bound by HBM: a value is read and written once and takes 3 to 16 operations.  So a head's row stays
+// in registers, eight values (16 bytes of bf16) to a lane and D / 8 lanes to a head, a wave holds the same token's
+// heads side by side and has the loads of up to kRows rows in flight before the first is used, and the cosines and
+// sines of a lane's four pairs are fetched once per token for all of its heads.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "device.h"
+#include "vec.h"
+
+namespace orbit {
+
+namespace {
+
+constexpr int kRows = 6;       // head rows that a wave's lanes have in flight
+constexpr int kBackRows = 3;   // the same for the backward pass, which reads two tensors
+constexpr int kWaves = 4;      // waves to a workgroup
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+    return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), CTRL, 0xF, 0xF, true));
+}
+
+// The sum over aligned groups of `lanes` lanes (a power of two), in each of them.  Every lane is active.
+__device__ __forceinline__ float group_sum(float v, int lanes) {
+    if (lanes > 1) v = dpp_add<0xB1>(v);   // quad_perm [1,0,3,2]
+    if (lanes > 2) v = dpp_add<0x4E>(v);   // quad_perm [2,3,0,1]
+    if (lanes > 4) v = dpp_add<0x141>(v);  // row_half_mirror
+    if (lanes > 8) v = dpp_add<0x140>(v);  // row_mirror
+    if (lanes > 16) v += __shfl_xor(v, 16);
+    if (lanes > 32) v += __shfl_xor(v, 32);
+    return v;
+}
+
+// A lane's eight values: two fours in a row, or pairs' first halves and their second halves.
+template <typename T, bool HALVES>
+struct Row8 {
+    Vec8<T> v;
+    __device__ __forceinline__ void load(const T* p, int, int) { v.load(p); }
+    __device__ __forceinline__ void get(float* f) const { v.get(f); }
+    static __device__ __forceinline__ void store(T* p, int, int, const float* f) { Vec8<T>::store(p, f); }
+};
+
+template <typename T>
+struct Row8<T, true> {
+    Vec4<T> a, b;
+    __device__ __forceinline__ void load(const T* p, int lo, int hi) { a.load(p + lo), b.load(p + hi); }
+    __device__ __forceinline__ void get(float* f) const { a.get(f), b.get(f + 4); }
+    static __device__ __forceinline__ void store(T* p, int lo, int hi, const float* f) {
+        Vec4<T>::store(p + lo, f);
+        Vec4<T>::store(p + hi, f + 4);
+    }
+};
+
+// What a lane does in every row: chunk c of a head, and where its eight values lie in the row.
+template <bool HALVES>
+struct Lane {
+    int c, lo, hi;
+    bool live, turned;
+    __device__ __forceinline__ Lane(const RopeParams& p, int lane) {
+        c = lane & (p.lanes - 1);
+        live = c * 8 < p.D;
+        if (!live) c = 0;  // loads what lane 0 of the group does, adds nothing to a sum and stores nothing
+        turned = c * 4 < p.pairs;
+        const bool apart = HALVES && turned;
+        lo = apart ? 4 * c : 8 * c;
+        hi = apart ? p.pairs + 4 * c : 8 * c + 4;
+    }
+};
+
+__device__ __forceinline__ void load_weights(const RopeTensor& t, int lo, int hi, float* w) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int at = i < 4 ? lo + i : hi + i - 4;
+        w[i] = !t.w ? 1.f : t.w_f32 ? ((const float*)t.w)[at] : bf16_low(((const uint16_t*)t.w)[at]);
+    }
+}
+
+// Cosines and sines of the lane's four pairs for one token; NaN where a position lies outside its axis's table.
+__device__ __forceinline__ void load_angles(const RopeParams& p, int c, int64_t b, int64_t l, float* cs, float* sn) {
+    const int32_t* pos = p.pos + b * p.pos_batch + l * p.axes;
+    int at[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int pair = 4 * c + i;
+        int axis = 0, length = p.length[0], base = p.base[0], width = p.width[0];
+        for (int a = 1; a < p.axes; ++a) {
+            const bool mine = pair >= p.first[a];
+            axis = mine ? a : axis;
+            length = mine ? p.length[a] : length;
+            base = mine ? p.base[a] : base;
+            width = mine ? p.width[a] : width;
+        }
+        const int where = pos[axis];
+        at[i] = (uint32_t)where < (uint32_t)length ? base + where * width + pair : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x2 v = ((const f32x2*)p.table)[at[i] < 0 ? 0 : at[i]];
+        cs[i] = at[i] < 0 ? __builtin_nanf("") : v.x;
+        sn[i] = at[i] < 0 ? __builtin_nanf("") : v.y;
+    }
+}
+
+template <bool HALVES>
+__device__ __forceinline__ void turn(float* v, const float* cs, const float* sn, float sign, bool turned) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int j = HALVES ? i : 2 * i, k = HALVES ? i + 4 : 2 * i + 1;
+        const float s = sign * sn[i];
+        const float a = v[j] * cs[i] - v[k] * s, b = v[j] * s + v[k] * cs[i];
+        v[j] = turned ? a : v[j];
+        v[k] = turned ? b : v[k];
+    }
+}
+
+// One wave's work: tokens t.wave_tokens * group .. and of each the heads of one chunk.  Lane group j of the wave has
+// token j / t.wave_heads of them and head j % t.wave_heads, then every t.wave_heads-th head after it.
+struct Item {
+    int64_t b, l;
+    int head;
+    bool live;
+    __device__ __forceinline__ Item(const RopeParams& p, const RopeTensor& t, uint32_t item, int lane) {
+        const uint32_t group = item / (uint32_t)t.chunks, chunk = item - group * (uint32_t)t.chunks;
+        const int j = lane / p.lanes, k = j / t.wave_heads;
+        uint32_t token = group * (uint32_t)t.wave_tokens + (uint32_t)k;
+        live = token < p.tokens;
+        token = live ? token : p.tokens - 1;
+        b = token / p.L;
+        l = token - (uint32_t)b * p.L;
+        head = (int)chunk * t.rows * t.wave_heads + j - k * t.wave_heads;
+    }
+};
+
+template <typename T>
+__device__ __forceinline__ T* row_of(const HeadRows& r, const Item& it, int head) {
+    return (T*)r.p + it.b * r.b + it.l * r.l + head * r.h;
+}
+
+template <typename TI, typename TO, bool NORM, bool HALVES>
+__global__ __launch_bounds__(64 * kWaves) void axial_rope_kernel(RopeParams p) {
+    const RopeTensor& t = p.t[blockIdx.y];
+    const int lane = threadIdx.x & 63;
+    const uint32_t item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (item >= t.items) return;
+    const Lane<HALVES> me(p, lane);
+    const Item it(p, t, item, lane);
+    Row8<TI, HALVES> x[kRows];
+#pragma unroll
+    for (int u = 0; u < kRows; ++u)
+        if (u < t.rows)
+            x[u].load(row_of<const TI>(t.x, it, min(it.head + u * t.wave_heads, t.heads - 1)) + (HALVES ? 0 : me.lo), me.lo, me.hi);
+    float w[8], cs[4], sn[4];
+    if (NORM) load_weights(t, me.lo, me.hi, w);
+    if (p.pairs) load_angles(p, me.turned ? me.c : 0, it.b, it.l, cs, sn);
+#pragma unroll
+    for (int u = 0; u < kRows; ++u) {
+        if (u >= t.rows) break;
+        const int head = it.head + u * t.wave_heads;
+        float v[8];
+        x[u].get(v);
+        if (NORM) {
+            float sum = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += v[i] * v[i];
+            sum = group_sum(me.live ? sum : 0.f, p.lanes);
+            const float r = rsqrtf(sum * p.inv_d + p.eps);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= r * w[i];
+        }
+        if (p.pairs) turn<HALVES>(v, cs, sn, p.sign, me.turned);
+        if (me.live && it.live && head < t.heads)
+            Row8<TO, HALVES>::store(row_of<TO>(t.y, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi, v);
+    }
+}
+
+// Persistent: the workgroup's sums of the weight's gradient stay in its lanes' registers, eight columns each, until
+// its last row, and leave as one row of partial sums.  They are added in a fixed order, so the result does not
+// depend on which workgroup ends first.
+template <typename TX, typename TG, bool HALVES>
+__global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_backward_kernel(RopeParams p) {
+    __shared__ float part[kWaves][512];
+    const RopeTensor& t = p.t[blockIdx.y];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Lane<HALVES> me(p, lane);
+    float w[8], dw[8];
+    load_weights(t, me.lo, me.hi, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dw[i] = 0.f;
+    for (uint32_t item = blockIdx.x * kWaves + wave; item < t.items; item += gridDim.x * kWaves) {
+        const Item it(p, t, item, lane);
+        Row8<TX, HALVES> x[kBackRows];
+        Row8<TG, HALVES> g[kBackRows];
+#pragma unroll
+        for (int u = 0; u < kBackRows; ++u) {
+            if (u < t.rows) {
+                const int head = min(it.head + u * t.wave_heads, t.heads - 1);
+                x[u].load(row_of<const TX>(t.x, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi);
+                g[u].load(row_of<const TG>(t.g, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi);
+            }
+        }
+        float cs[4], sn[4];
+        if (p.pairs) load_angles(p, me.turned ? me.c : 0, it.b, it.l, cs, sn);
+#pragma unroll
+        for (int u = 0; u < kBackRows; ++u) {
+            if (u >= t.rows) break;
+            const int head = it.head + u * t.wave_heads;
+            const bool live = me.live && it.live && head < t.heads;
+            float xv[8], gv[8];
+            x[u].get(xv);
+            g[u].get(gv);
+            if (p.pairs) turn<HALVES>(gv, cs, sn, -1.f, me.turned);
+            float sum = 0.f, dot = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                sum += xv[i] * xv[i];
+                dot += gv[i] * w[i] * xv[i];
+            }
+            sum = group_sum(me.live ? sum : 0.f, p.lanes);
+            dot = group_sum(me.live ? dot : 0.f, p.lanes);
+            const float r = rsqrtf(sum * p.inv_d + p.eps);
+            const float m = r * r * (dot * p.inv_d);
+            float dx[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                dx[i] = r * (gv[i] * w[i] - xv[i] * m);
+                if (live) dw[i] += gv[i] * (xv[i] * r);
+            }
+            if (live) Row8<TX, HALVES>::store(row_of<TX>(t.y, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi, dx);
+        }
+    }
+    if (!t.dw) return;
+    // lane groups, then waves
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        for (int apart = p.lanes; apart < 64; apart *= 2) dw[i] += __shfl_xor(dw[i], apart);
+    if (lane < p.lanes && me.live) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part[wave][i < 4 ? me.lo + i : me.hi + i - 4] = dw[i];
+    }
+    __syncthreads();
+    for (int d = threadIdx.x; d < p.D; d += 64 * kWaves)
+        t.dw_part[(int64_t)blockIdx.x * p.D + d] = (part[0][d] + part[1][d]) + (part[2][d] + part[3][d]);
+}
+
+// Sums of the workgroups' rows: 16 columns to a workgroup of 1024, 64 of its threads to a column.
+__global__ __launch_bounds__(1024) void norm_weight_grad_kernel(RopeParams p) {
+    __shared__ float part[64][17];
+    const RopeTensor& t = p.t[blockIdx.y];
+    if (!t.dw) return;
+    const int col = threadIdx.x & 15, row = threadIdx.x >> 4, d = blockIdx.x * 16 + col;
+    float sum = 0.f;
+    if (d < p.D) {
+#pragma unroll 8
+        for (int i = row; i < t.parts; i += 64) sum += t.dw_part[(int64_t)i * p.D + d];
+    }
+    part[row][col] = sum;
+    __syncthreads();
+    for (int half = 32; half; half /= 2) {
+        if (row < half) part[row][col] += part[row + half][col];
+        __syncthreads();
+    }
+    if (row == 0 && d < p.D) t.dw[d] = part[0][col];
+}
+
+// How a tensor's head rows go over the waves: as many of a token's heads side by side as fit, several tokens where
+// it has fewer heads than that, and up to `most` rows a lane group after each other.
+void divide(const RopeParams& p, RopeTensor& t, int most, int cus) {
+    const int groups = 64 / p.lanes;
+    int side = 1;
+    while (side < groups && side < t.heads) side *= 2;
+    t.wave_heads = side;
+    t.wave_tokens = groups / side;
+    const int steps = (t.heads + side - 1) / side;
+    const int64_t token_groups = ((int64_t)p.tokens + t.wave_tokens - 1) / t.wave_tokens;
+    t.chunks = (steps + most - 1) / most;
+    // few tokens: fewer rows to a wave, until every SIMD has a wave
+    while (t.chunks < steps && token_groups * t.chunks < 4 * (int64_t)cus) t.chunks = std::min(steps, 2 * t.chunks);
+    t.rows = (steps + t.chunks - 1) / t.chunks;
+    t.chunks = (steps + t.rows - 1) / t.rows;
+    t.items = (uint32_t)(token_groups * t.chunks);
+}
+
+template <typename TI, typename TO, bool NORM>
+void launch(const RopeParams& p, dim3 grid, hipStream_t stream) {
+    if (p.halves)
+        axial_rope_kernel<TI, TO, NORM, true><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else
+        axial_rope_kernel<TI, TO, NORM, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+}
+
+template <typename TX, typename TG>
+void launch_backward(const RopeParams& p, dim3 grid, hipStream_t stream) {
+    if (p.halves)
+        qk_norm_rope_backward_kernel<TX, TG, true><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else
+        qk_norm_rope_backward_kernel<TX, TG, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+}
+
+}  // namespace
+
+hipError_t launch_axial_rope(RopeParams p, bool norm, bool in_f32, bool out_f32, int cus, hipStream_t stream) {
+    uint32_t items = 0;
+    for (int i = 0; i < p.tensors; ++i) {
+        divide(p, p.t[i], kRows, cus);
+        items = std::max(items, p.t[i].items);
+    }
+    const dim3 grid((items + kWaves - 1) / kWaves, p.tensors);
+    if (!norm)
+        in_f32 ? launch<float, float, false>(p, grid, stream) : launch<bf16_t, bf16_t, false>(p, grid, stream);
+    else if (in_f32)
+        out_f32 ? launch<float, float, true>(p, grid, stream) : launch<float, bf16_t, true>(p, grid, stream);
+    else
+        out_f32 ? launch<bf16_t, float, true>(p, grid, stream) : launch<bf16_t, bf16_t, true>(p, grid, stream);
+    return hipGetLastError();
+}
+
+int norm_rope_backward_groups(int cus) { return 4 * cus; }
+
+hipError_t launch_qk_norm_rope_backward(RopeParams p, bool x_f32, bool g_f32, int cus, hipStream_t stream) {
+    uint32_t items = 0;
+    bool dw = false;
+    for (int i = 0; i < p.tensors; ++i) {
+        divide(p, p.t[i], kBackRows, cus);  // no tokens: no items, and the weights' gradients are sums of nothing
+        items = std::max(items, p.t[i].items);
+        dw = dw || p.t[i].dw;
+    }
+    const int groups = (int)std::min<int64_t>((items + kWaves - 1) / kWaves, norm_rope_backward_groups(cus));
+    for (int i = 0; i < p.tensors; ++i) p.t[i].parts = groups;
+    const dim3 grid(groups, p.tensors);
+    if (!groups)
+        ;
+    else if (x_f32)
+        g_f32 ? launch_backward<float, float>(p, grid, stream) : launch_backward<float, bf16_t>(p, grid, stream);
+    else
+        g_f32 ? launch_backward<bf16_t, float>(p, grid, stream) : launch_backward<bf16_t, bf16_t>(p, grid, stream);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || !dw) return e;
+    norm_weight_grad_kernel<<<dim3((p.D + 15) / 16, p.tensors), 1024, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
+}  // namespace orbit

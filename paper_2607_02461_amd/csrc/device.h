@@ -149,4 +149,48 @@ hipError_t launch_adaln_int4_quantize(const uint16_t* W, int64_t N, int K, int64
                                       hipStream_t stream);
 hipError_t launch_adaln_int4_linear(const RtnLinearParams& p, int cus, hipStream_t stream);
 
+// Rotary positions over several axes, alone and behind the norms of queries and keys.
+constexpr int kMaxAxes = 8;
+constexpr int kMaxHeadDim = 512;
+
+struct HeadRows {     // [B][L][heads][D] values, the last dimension contiguous; strides in elements
+    void* p;
+    int64_t b, l, h;
+};
+
+struct RopeTensor {
+    HeadRows x, y, g;  // input, output and, backward, the output's gradient (y is then that of x)
+    const void* w;     // the norm's weight [D], bf16 or fp32, or null (1)
+    int w_f32;
+    int heads;
+    float* dw;         // fp32 [D], the weight's gradient, or null
+    float* dw_part;    // partial sums of dw, [parts][D]
+    int parts;
+    // set by the launcher: heads side by side in a wave, tokens of a wave, rows after each other in a wave, waves
+    // that share a token's heads, and waves of work in all
+    int wave_heads, wave_tokens, rows, chunks;
+    uint32_t items;
+};
+
+struct RopeParams {
+    RopeTensor t[2];
+    int tensors;
+    uint32_t tokens, L;     // B * L, L
+    const int32_t* pos;     // [B or 1][L][axes]
+    int64_t pos_batch;      // elements from one batch's positions to the next's (0: shared)
+    const float* table;     // (cos, sin) pairs
+    int axes, pairs;        // pairs = 0: no rotation
+    int first[kMaxAxes];    // an axis's first pair, its pairs, its positions, and where its table begins less `first`
+    int width[kMaxAxes], length[kMaxAxes], base[kMaxAxes];
+    int D, lanes;           // head size, and the lanes that share a head: a power of two, at least D / 8
+    int halves;             // a pair is (p, p + pairs) and not (2p, 2p + 1)
+    float sign, eps, inv_d;
+};
+
+// Grids hold one wave per item, items at most tokens * heads < 2^31.
+hipError_t launch_axial_rope(RopeParams p, bool norm, bool in_f32, bool out_f32, int cus, hipStream_t stream);
+// Rows of partial sums that the backward pass may write for each tensor.
+int norm_rope_backward_groups(int cus);
+hipError_t launch_qk_norm_rope_backward(RopeParams p, bool x_f32, bool g_f32, int cus, hipStream_t stream);
+
 }  // namespace orbit

@@ -6,6 +6,7 @@
 #include <cstring>
 #include <vector>
 
+#include "abi.h"
 #include "device.h"
 #include "internal.h"
 
@@ -18,19 +19,16 @@ constexpr int64_t kQuantMaxK = 16384;
 constexpr int kQuantMaxH = 4096;  // block sizes 128 .. 4096 (the FWHT's stages across blocks)
 constexpr int kQuantMaxCells = 8192;  // encoder table cells (LDS budget; 6-bit tables reach ~4300 at K = 16384)
 
-bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-
-orbit_status hip_fail(hipError_t e, const char* what) {
-    return fail(ORBIT_EHIP, "%s: %s (%s)", what, hipGetErrorString(e), hipGetErrorName(e));
-}
-
-struct DeviceInfo {
-    int cus = 0;
-};
 DeviceInfo g_dev[kMaxDevices];
 std::mutex g_dev_mu;
 
-orbit_status current_device(int* dev, DeviceInfo* info) {
+}  // namespace
+
+orbit_status orbit::hip_fail(hipError_t e, const char* what) {
+    return fail(ORBIT_EHIP, "%s: %s (%s)", what, hipGetErrorString(e), hipGetErrorName(e));
+}
+
+orbit_status orbit::current_device(int* dev, DeviceInfo* info) {
     hipError_t e = hipGetDevice(dev);
     if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
     if (*dev < 0 || *dev >= kMaxDevices) return fail(ORBIT_EUNSUPPORTED, "device ordinal %d out of range", *dev);
@@ -44,6 +42,35 @@ orbit_status current_device(int* dev, DeviceInfo* info) {
     *info = g_dev[*dev];
     return ORBIT_OK;
 }
+
+orbit_status orbit::device_for_upload(int* dev) {
+    int n = 0;
+    if (hipGetDeviceCount(&n) != hipSuccess || n <= 0) {
+        (void)hipGetLastError();  // leave no sticky error behind on a machine without a GPU
+        *dev = -1;
+        return ORBIT_OK;
+    }
+    hipError_t e = hipGetDevice(dev);
+    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
+    if (*dev < 0 || *dev >= kMaxDevices) return fail(ORBIT_EUNSUPPORTED, "device ordinal %d out of range", *dev);
+    return ORBIT_OK;
+}
+
+orbit_status orbit::upload_copy(const char* who, const void* data, size_t bytes, void** out) {
+    void* d = nullptr;
+    hipError_t e = hipMalloc(&d, bytes);
+    if (e != hipSuccess)
+        return e == hipErrorOutOfMemory ? fail(ORBIT_ENOMEM, "%s: hipMalloc failed", who) : hip_fail(e, "hipMalloc");
+    e = hipMemcpy(d, data, bytes, hipMemcpyHostToDevice);
+    if (e != hipSuccess) {
+        (void)hipFree(d);
+        return hip_fail(e, who);
+    }
+    *out = d;
+    return ORBIT_OK;
+}
+
+namespace {
 
 // The plan's tables on device `dev`: K gather offsets (2*perm[j], the byte offset of the element
 // that moves to position j, with bit 31 set where sign[j] = -1) followed by K/2 sign masks over
@@ -65,34 +92,19 @@ orbit_status plan_upload_dev(orbit_plan p, int dev) {
         if (p->sign[j] < 0) meta[d + j / 2] |= (j & 1) ? 0x80000000u : 0x8000u;
     }
     void* dp = nullptr;
-    hipError_t e = hipMalloc(&dp, meta.size() * sizeof(uint32_t));
-    if (e != hipSuccess)
-        return e == hipErrorOutOfMemory ? fail(ORBIT_ENOMEM, "plan upload: hipMalloc failed") : hip_fail(e, "hipMalloc");
-    e = hipMemcpy(dp, meta.data(), meta.size() * sizeof(uint32_t), hipMemcpyHostToDevice);
-    if (e != hipSuccess) {
-        (void)hipFree(dp);
-        return hip_fail(e, "plan upload: hipMemcpy");
-    }
+    const orbit_status st = upload_copy("plan upload", meta.data(), meta.size() * sizeof(uint32_t), &dp);
     p->dev_meta[dev] = (uint32_t*)dp;
-    return ORBIT_OK;
+    return st;
 }
 
 // The codebook's encoder table on device `dev`, copied once per device at set-up.
 orbit_status codebook_upload_dev(orbit_codebook c, int dev) {
     std::lock_guard<std::mutex> lk(c->mu);
     if (c->dev_enc[dev]) return ORBIT_OK;
-    const size_t bytes = c->enc.bias.size() * sizeof(float);
     void* d = nullptr;
-    hipError_t e = hipMalloc(&d, bytes);
-    if (e != hipSuccess)
-        return e == hipErrorOutOfMemory ? fail(ORBIT_ENOMEM, "codebook upload: hipMalloc failed") : hip_fail(e, "hipMalloc");
-    e = hipMemcpy(d, c->enc.bias.data(), bytes, hipMemcpyHostToDevice);
-    if (e != hipSuccess) {
-        (void)hipFree(d);
-        return hip_fail(e, "codebook upload: hipMemcpy");
-    }
+    const orbit_status st = upload_copy("codebook upload", c->enc.bias.data(), c->enc.bias.size() * sizeof(float), &d);
     c->dev_enc[dev] = (float*)d;
-    return ORBIT_OK;
+    return st;
 }
 
 // Scratch of the allocation-free layer (orbit_qlinear_noalloc): the K-split's fp32 partial sums
@@ -115,20 +127,6 @@ orbit_status scratch_on(int dev, void** out) {
         g_scratch[dev] = ptr;
     }
     *out = g_scratch[dev];
-    return ORBIT_OK;
-}
-
-// The current device, or -1 when no HIP device is visible (handles then stay host-only).
-orbit_status device_for_upload(int* dev) {
-    int n = 0;
-    if (hipGetDeviceCount(&n) != hipSuccess || n <= 0) {
-        (void)hipGetLastError();  // leave no sticky error behind on a machine without a GPU
-        *dev = -1;
-        return ORBIT_OK;
-    }
-    hipError_t e = hipGetDevice(dev);
-    if (e != hipSuccess) return hip_fail(e, "hipGetDevice");
-    if (*dev < 0 || *dev >= kMaxDevices) return fail(ORBIT_EUNSUPPORTED, "device ordinal %d out of range", *dev);
     return ORBIT_OK;
 }
 
@@ -229,21 +227,6 @@ orbit_status quantize_rows(const char* who, orbit_plan p, orbit_codebook cb, con
                        : launch_rpbh_quantize(q, cb->bits, norm_bf16, !p->identity, info.cus, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, who);
     return ORBIT_OK;
-}
-
-// Frees a handle's per-device tables (each on its own device).
-template <typename T>
-void free_per_device(T* (&ptrs)[kMaxDevices]) {
-    for (int dev = 0; dev < kMaxDevices; ++dev) {
-        if (ptrs[dev]) {
-            int cur = 0;
-            (void)hipGetDevice(&cur);
-            (void)hipSetDevice(dev);
-            (void)hipFree(ptrs[dev]);
-            (void)hipSetDevice(cur);
-            ptrs[dev] = nullptr;
-        }
-    }
 }
 
 }  // namespace

@@ -59,6 +59,16 @@ struct orbit_codebook_s {
     float* dev_enc[orbit::kMaxDevices] = {};
 };
 
+// Angles of rotary positions: per axis a table of (cos, sin) over its positions and its pairs.
+struct orbit_rope_s {
+    int32_t axes = 0, pairs = 0;
+    bool halves = false;
+    std::vector<int32_t> width, length;  // pairs and positions of each axis
+    std::vector<float> table;            // axis by axis, [position][pair][cos, sin]
+    std::mutex mu;
+    float* dev_table[orbit::kMaxDevices] = {};
+};
+
 namespace orbit {
 void build_enc_table(orbit_codebook_s* c);
 // Set-up of a new handle (exactly one of p, c non-null): copies its device tables to the current
