@@ -475,6 +475,80 @@ orbit_status qk_norm_rope_backward(orbit_rope plan, const orbit_heads* dq, const
                                    float* q_weight_grad, float* k_weight_grad, void* workspace, size_t workspace_bytes,
                                    void* stream);
 
+/* ------------------------------------------- low-rank adapters beside a shared projection */
+
+typedef struct orbit_lora_s* orbit_lora;
+
+/*
+ * lora_plan -- which rows of a batch use which low-rank adapter: segments (requests) of consecutive
+ * rows, each with one of n_adapters adapters or with none.  One plan serves every projection that the
+ * batch passes (their widths and weights are given with each call).  Its lists are kept on the device
+ * as for rpbh_plan.
+ *   M          rows of the batch
+ *   segments   segment s is rows starts[s] .. starts[s + 1] - 1, the last one ends at M; rows before
+ *              starts[0] have no adapter
+ *   starts     host, [segments]: not falling, 0 .. M (a segment may be empty)
+ *   adapters   host, [segments]: 0 .. n_adapters - 1, or -1 for none; segments may share an adapter
+ *   ranks      host, [n_adapters]: 0 .. 128 (0: as none)
+ *   scales     host, [n_adapters]: finite
+ * Errors: ORBIT_EINVAL; ORBIT_EUNSUPPORTED (rank, M above 2^31 - 1, more than 65535 adapters or 2^22
+ * tiles of 64 rows); ORBIT_ENOMEM; ORBIT_EHIP.
+ */
+orbit_status lora_plan(int64_t M, int64_t segments, const int64_t* starts, const int32_t* adapters, int32_t n_adapters,
+                       const int32_t* ranks, const float* scales, orbit_lora* out);
+
+/* Copy the plan's lists to the current device, as rpbh_plan_upload. */
+orbit_status lora_plan_upload(orbit_lora p);
+
+/* Free a plan.  NULL is ignored. */
+void lora_plan_destroy(orbit_lora p);
+
+/* Bytes of device workspace that lora_add (or, where `backward` is not 0, lora_add_backward) takes on
+ * the current device. */
+orbit_status lora_add_workspace_size(orbit_lora p, int64_t K, int64_t N, int32_t R, int32_t backward, size_t* bytes);
+
+/*
+ * lora_add -- a shared projection's output with each row's adapter added:
+ *     Y[m] = base[m] + scale_a * (X[m] A_a^T) B_a^T,     a the adapter of row m's segment,
+ * and Y[m] = base[m] for rows without one.  X A^T is a sum in fp32 of exact products; it enters the
+ * second product as the sum of two bf16 values (relative error below 2^-16), which again accumulates in
+ * fp32, and Y is rounded once.
+ *   X      device, bf16 [M][ldx]: the projection's input
+ *   A, B   device, bf16 [n_adapters][R][K] and [n_adapters][N][R]; R a multiple of 8 up to 128 and at
+ *          least every rank.  What lies beyond an adapter's rank does not matter
+ *   base   device, [M][ldb] of `dtype` (orbit_qlinear's output, bias included), or NULL (zeros)
+ *   Y      device, [M][ldy] of `dtype` (ORBIT_OUT_F32 or ORBIT_OUT_BF16); may be base with the same row
+ *          stride, else they do not overlap
+ *   h      device, fp32 [M][R], or NULL: receives X A^T (zeros beyond the rank and in rows without an
+ *          adapter), which the backward call takes
+ *   workspace   lora_add_workspace_size bytes, aligned to 16; contents and ownership as for orbit_qlinear_ws
+ * K a positive multiple of 8, N positive, both up to 2^21; any row strides.  Pointers: A, B and h 16-byte aligned,
+ * the others to their element.  Errors: ORBIT_EINVAL; ORBIT_EUNSUPPORTED (R, K or N); ORBIT_EHIP.
+ * M = 0 returns at once.
+ */
+orbit_status lora_add(orbit_lora p, const uint16_t* X, int64_t ldx, const uint16_t* A, const uint16_t* B, int64_t K,
+                      int64_t N, int32_t R, const void* base, int64_t ldb, int32_t dtype, void* Y, int64_t ldy, float* h,
+                      void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * lora_add_backward -- gradients of lora_add from dY, the gradient of Y in bf16 (base's gradient is dY
+ * itself):
+ *     dX[m] = base[m] + scale_a * (dY[m] B_a) A_a
+ *     dA_a  = scale_a * sum over a's rows of (dY[m] B_a)^T X[m],    dB_a = scale_a * sum of dY[m]^T h[m]
+ * Sums are in fp32 and in a fixed order (the same bits on the same device).
+ *   dY     device, bf16 [M][ldd]
+ *   X, A, B, h   lora_add's inputs and its h
+ *   base   device, bf16 [M][ldb], the gradient that X has from elsewhere (the projection), or NULL
+ *   dX     device, bf16 [M][lddx]; may be base with the same row stride
+ *   dA, dB device, fp32 [n_adapters][R][K] and [n_adapters][N][R]: every element is written, zeros beyond
+ *          the ranks and for adapters without rows
+ * Other arguments, limits and errors as for lora_add.  M = 0 gives zeros in dA and dB.
+ */
+orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, const uint16_t* X, int64_t ldx,
+                               const uint16_t* A, const uint16_t* B, const float* h, int64_t K, int64_t N, int32_t R,
+                               const uint16_t* base, int64_t ldb, uint16_t* dX, int64_t lddx, float* dA, float* dB,
+                               void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

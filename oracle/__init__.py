@@ -14,6 +14,7 @@ OrbitQuant (arXiv 2607.02461), written from the paper's definitions:
 and, beside the paper's layer, of what a transformer has next to it:
 
   attention_input.py  rotary positions with several axes, norms of queries and keys, gradients
+  lora.py             low-rank adapters of many requests beside a shared projection, gradients
 
 Only the tests, the package's smoke check and the benchmark's CPU-baseline leg
 may import this package.  The product path (the HIP library and its binding)
@@ -36,6 +37,7 @@ from .quantize import (normalize_rows, encode, decode_levels, pack_codes, unpack
 from .qlinear import layer_epilogue, qlinear, qlinear_dense_reference
 from .adaln_rtn import rtn_int4_quantize, rtn_int4_dequantize, pack_rtn_int4, unpack_rtn_int4, rtn_int4_linear
 from .attention_input import rope_angles, rope_turn, qk_norm_rope, qk_norm_rope_backward
+from .lora import lora_add, lora_add_backward
 
 EPS_DEFAULT = 1e-10  # Sec. 4.3: the clamp guarding zero-norm (padding) tokens
 
@@ -48,4 +50,5 @@ __all__ = [
     "qlinear", "qlinear_dense_reference", "EPS_DEFAULT",
     "rtn_int4_quantize", "rtn_int4_dequantize", "pack_rtn_int4", "unpack_rtn_int4", "rtn_int4_linear",
     "rope_angles", "rope_turn", "qk_norm_rope", "qk_norm_rope_backward",
+    "lora_add", "lora_add_backward",
 ]

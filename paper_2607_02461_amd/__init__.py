@@ -70,6 +70,15 @@ SIGNATURES = {
     "qk_norm_rope_backward": (ctypes.c_int, [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64,
                                              _i64, _i64, _c_void_p, _i64, _c_void_p, _c_void_p, _i32, ctypes.c_float, _c_void_p,
                                              _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+    "lora_plan": (ctypes.c_int, [_i64, _i64, _c_void_p, _c_void_p, _i32, _c_void_p, _c_void_p, ctypes.POINTER(_c_void_p)]),
+    "lora_plan_upload": (ctypes.c_int, [_c_void_p]),
+    "lora_plan_destroy": (None, [_c_void_p]),
+    "lora_add_workspace_size": (ctypes.c_int, [_c_void_p, _i64, _i64, _i32, _i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "lora_add": (ctypes.c_int, [_c_void_p, _c_void_p, _i64, _c_void_p, _c_void_p, _i64, _i64, _i32, _c_void_p, _i64, _i32,
+                                _c_void_p, _i64, _c_void_p, _c_void_p, ctypes.c_size_t, _c_void_p]),
+    "lora_add_backward": (ctypes.c_int, [_c_void_p, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _c_void_p, _c_void_p, _i64,
+                                         _i64, _i32, _c_void_p, _i64, _c_void_p, _i64, _c_void_p, _c_void_p, _c_void_p,
+                                         ctypes.c_size_t, _c_void_p]),
 }
 
 ORBIT_ACT_NONE, ORBIT_ACT_GELU = 0, 1
@@ -433,10 +442,11 @@ def adaln_int4_linear(X: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, bi
     return out
 
 
+from .adapters import LoraPlan, lora_add, lora_add_backward, lora_plan  # noqa: E402
 from .attention_input import (RopePlan, axial_rope, qk_norm_rope, qk_norm_rope_backward, rope_plan,  # noqa: E402
                               rope_plan_from_angles)
 
-__all__ = ["RopePlan", "rope_plan", "rope_plan_from_angles", "axial_rope", "qk_norm_rope", "qk_norm_rope_backward", "adaln_int4_quantize_weights", "adaln_int4_linear", "rpbh_plan", "rpbh_plan_from_arrays", "lloydmax_codebook", "quantize_weights_offline",
+__all__ = ["LoraPlan", "lora_plan", "lora_add", "lora_add_backward", "RopePlan", "rope_plan", "rope_plan_from_angles", "axial_rope", "qk_norm_rope", "qk_norm_rope_backward", "adaln_int4_quantize_weights", "adaln_int4_linear", "rpbh_plan", "rpbh_plan_from_arrays", "lloydmax_codebook", "quantize_weights_offline",
            "rpbh_quantize_act", "orbit_qlinear", "orbit_qlinear_ex",
            "orbit_qlinear_workspace_size", "orbit_qlinear_ws", "Plan", "Codebook", "OrbitError", "lib", "LIB_PATH",
            "SIGNATURES", "code_bytes"]

@@ -193,4 +193,76 @@ hipError_t launch_axial_rope(RopeParams p, bool norm, bool in_f32, bool out_f32,
 int norm_rope_backward_groups(int cus);
 hipError_t launch_qk_norm_rope_backward(RopeParams p, bool x_f32, bool g_f32, int cus, hipStream_t stream);
 
+// Low-rank adapters of many requests.
+constexpr int kLoraMaxSplits = 16;  // of the contraction of a few rows
+constexpr int kLoraTileRows = 64;
+constexpr int kLoraMaxRank = 128;
+
+struct LoraTile {   // up to kLoraTileRows rows of one adapter (adapter -1, rank 0: of none)
+    int32_t row, rows, adapter, rank;
+    float scale;
+    int32_t pad[3];
+};
+
+struct LoraSplit {  // tiles [begin, end) of one adapter
+    int32_t begin, end;
+};
+
+struct LoraShrink {
+    const LoraTile* tiles;
+    const uint16_t* x;     // bf16 [M][ldx]
+    int64_t ldx, M, K;
+    const uint16_t* pool;  // bf16 [adapter][R][ldp], 16-byte aligned, ldp a multiple of 8 and at least K
+    int64_t ldp;
+    int R;
+    int steps;             // of 32 to a wave (set by the launcher)
+    float* h;              // fp32 [split][M][R], every element written
+};
+
+struct LoraExpand {
+    const LoraTile* tiles;
+    const float* h;        // fp32 [splits][M][R]
+    float* sum;            // fp32 [M][R], the splits' sum, or null
+    int splits, R;
+    int64_t M, N;
+    const uint16_t* pool;  // bf16 [adapter][N][R], 16-byte aligned
+    const void* base;      // [M][ldb] of y's type, or null (zeros); may be y
+    int64_t ldb;
+    void* y;               // [M][ldy] fp32 or bf16
+    int64_t ldy;
+    int strips;            // of 64 columns to a wave (set by the launcher)
+};
+
+struct LoraTranspose {
+    const uint16_t *a, *b;  // bf16 [adapter][R][K] and [adapter][N][R]
+    uint16_t *at, *bt;      // [adapter][K][R] and [adapter][R][ldt]
+    int64_t K, N, ldt;
+    int R;
+};
+
+struct LoraGradSide {
+    const uint16_t* wide;  // bf16 [M][ld]
+    int64_t ld, width;
+    const float* narrow;   // fp32 [M][R]
+    float* part;           // fp32 [split][R][width]
+    float* out;            // fp32 [adapter][R][width], the second side's [adapter][width][R]
+};
+
+struct LoraGrad {
+    const LoraTile* tiles;
+    const LoraSplit* list;
+    const int32_t* first;  // [adapters + 1]: splits of each adapter
+    LoraGradSide side[2];
+    int R;
+    int chunks, chunks_x, sum_blocks_x;  // workgroups of a split and of its first side, and of the first side's sums (set by
+                                         // the launcher)
+};
+
+// Splits of a contraction over K for this many tiles: at most kLoraMaxSplits.
+int lora_splits(int tiles, int64_t K, int cus);
+hipError_t launch_lora_shrink(LoraShrink p, int tiles, int splits, hipStream_t stream);
+hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream);
+hipError_t launch_lora_transpose(const LoraTranspose& p, int adapters, hipStream_t stream);
+hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, hipStream_t stream);
+
 }  // namespace orbit

@@ -69,6 +69,20 @@ struct orbit_rope_s {
     float* dev_table[orbit::kMaxDevices] = {};
 };
 
+// Requests' rows and adapters, as the kernels' lists (device.h): tiles, adapter by adapter and those of none last; the
+// tiles of one adapter in splits of 4 << level tiles, each level with its splits' first index per adapter.
+constexpr int kLoraLevels = 5;
+struct orbit_lora_s {
+    int64_t rows = 0;
+    int32_t adapters = 0, max_rank = 0;
+    int64_t tiles = 0;
+    std::vector<unsigned char> lists;
+    size_t at_splits[kLoraLevels] = {}, at_first[kLoraLevels] = {};  // byte offsets; the tiles are at 0
+    int64_t splits[kLoraLevels] = {};
+    std::mutex mu;
+    unsigned char* dev_lists[orbit::kMaxDevices] = {};
+};
+
 namespace orbit {
 void build_enc_table(orbit_codebook_s* c);
 // Set-up of a new handle (exactly one of p, c non-null): copies its device tables to the current
