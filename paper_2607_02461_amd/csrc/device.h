@@ -215,7 +215,7 @@ struct LoraShrink {
     const uint16_t* pool;  // bf16 [adapter][R][ldp], 16-byte aligned, ldp a multiple of 8 and at least K
     int64_t ldp;
     int R;
-    int steps;             // of 32 to a wave (set by the launcher)
+    int steps;             // chunks of 128 to a split (set by the launcher)
     float* h;              // fp32 [split][M][R], every element written
 };
 
@@ -230,20 +230,25 @@ struct LoraExpand {
     int64_t ldb;
     void* y;               // [M][ldy] fp32 or bf16
     int64_t ldy;
-    int strips;            // of 64 columns to a wave (set by the launcher)
+    uint16_t* turned;      // s h as three bf16 parts for the gradients (lora_operand_bytes), or null
+    int columns;           // to a workgroup, a multiple of 512 (set by the launcher)
 };
 
-struct LoraTranspose {
+struct LoraTurn {
     const uint16_t *a, *b;  // bf16 [adapter][R][K] and [adapter][N][R]
-    uint16_t *at, *bt;      // [adapter][K][R] and [adapter][R][ldt]
-    int64_t K, N, ldt;
-    int R;
+    uint16_t *at, *bt;      // [adapter][K][R] and [adapter][R][ldn]
+    int64_t K, N, ldn;
+    int R, adapters;
+    const LoraTile* tiles;
+    int64_t count;          // of tiles
+    const float* h;         // fp32 [M][R]
+    uint16_t* turned;       // s h as three bf16 parts for the gradients (lora_operand_bytes)
 };
 
 struct LoraGradSide {
     const uint16_t* wide;  // bf16 [M][ld]
     int64_t ld, width;
-    const float* narrow;   // fp32 [M][R]
+    const uint16_t* narrow;  // s h or s g as three bf16 parts
     float* part;           // fp32 [split][R][width]
     float* out;            // fp32 [adapter][R][width], the second side's [adapter][width][R]
 };
@@ -261,8 +266,10 @@ struct LoraGrad {
 // Splits of a contraction over K for this many tiles: at most kLoraMaxSplits.
 int lora_splits(int tiles, int64_t K, int cus);
 hipError_t launch_lora_shrink(LoraShrink p, int tiles, int splits, hipStream_t stream);
+// Bytes of one narrow matrix in three bf16 parts, in the order of the gradients' operands: tiles of 64 rows.
+inline int64_t lora_operand_bytes(int64_t tiles, int R) { return tiles * kLoraTileRows * ((R + 15) / 16 * 16) * 3 * 2; }
 hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream);
-hipError_t launch_lora_transpose(const LoraTranspose& p, int adapters, hipStream_t stream);
+hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream);
 hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, hipStream_t stream);
 
 }  // namespace orbit

@@ -9,11 +9,13 @@
 //   expand  y (or dx): a narrow matrix times a narrow one, added to the wide base on its way through the registers
 //   grad    dA, dB: contraction over rows, of a wide matrix and a narrow one
 // The matrix cores multiply bf16.  x, dy, A and B are bf16 and their products exact; h and g are fp32 sums and go into
-// the next product as the sum of two bf16 values (16 bits of their fraction: 2^-17 of them is lost, where one bf16 would
-// lose 2^-9), which costs a second MFMA and no memory traffic.
+// the next product as a sum of bf16 values: three where the result is fp32 (all 24 bits of their fraction), two where it
+// is rounded to bf16 (2^-17 of them is lost, below the rounding's 2^-9).  That costs MFMAs and no memory traffic.
 //
-// A tile is up to 64 rows of one adapter; the plan lists them.  MFMA operands come straight from memory: a lane holds 8
-// values in a row of the contraction for row (or column) lane % 16, so a wave's load covers 16 rows of 64 bytes.
+// A tile is up to 64 rows of one adapter; the plan lists them.  An MFMA operand is 8 values in a row of the contraction for
+// row (or column) lane % 16; loaded as such from rows 128 bytes or more apart, each lane's 16 bytes are a request of their
+// own, 65 cycles to a wave's load against 18 for 1 KB in a row (measured in L2).  So wide rows, and narrow ones that
+// several waves read, go through LDS, or lie in memory in the operands' order.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -55,13 +57,18 @@ __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x
 // v - hi, and 0 where hi holds v already: of an infinity too
 __device__ __forceinline__ float rest(float v, float hi) { return v == hi ? 0.f : v - hi; }
 
-// v as hi + lo, both bf16
-__device__ __forceinline__ void split8(const float* v, u32x4& hi, u32x4& lo) {
+// v as the sum of PARTS bf16 values, the largest first; v becomes what is left
+template <int PARTS>
+__device__ __forceinline__ void split8(float* v, u32x4* part) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        hi[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-        lo[i] = pack_bf16(rest(v[2 * i], bf16_low(hi[i])), rest(v[2 * i + 1], bf16_high(hi[i])));
-    }
+    for (int k = 0; k < PARTS; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = pack_bf16(v[2 * i], v[2 * i + 1]);
+            part[k][i] = w;
+            v[2 * i] = rest(v[2 * i], bf16_low(w));
+            v[2 * i + 1] = rest(v[2 * i + 1], bf16_high(w));
+        }
 }
 
 // 8 rows of 8 values become 8 columns
@@ -78,259 +85,454 @@ __device__ __forceinline__ void transpose8(u32x4 (&v)[8]) {
 
 constexpr int kWaves = 4;
 
-// h partial sums [split][M][R] of rows x [M][K] and pool [adapter][R][K]: a workgroup takes 16 MT rows of a tile and a
-// split of K, its waves a quarter of that each.
-template <int MT, int RF>
+// Where value (row of a tile, r) of part k lies in what the gradients' kernel reads, in the order of its operands: per 32
+// rows, part and 16 r's, 64 lanes of 8 rows.
+__device__ __forceinline__ int64_t lora_operand(int64_t tile, int row, int k, int r, int R) {
+    const int64_t block = ((tile * 2 + row / 32) * 3 + k) * ((R + 15) / 16) + r / 16;
+    return (block * 64 + row % 32 / 8 * 16 + r % 16) * 8 + row % 8;
+}
+
+// h partial sums [split][M][R] of rows x [M][K] and pool [adapter][R][K]: a workgroup takes a tile and a split of K, in
+// chunks of 128 that all its waves bring to LDS, the next one's loads on their way while this one is multiplied.  A wave
+// has 16 rows; in a tile with fewer rows, several have the same and every second or fourth step of 32.
+template <int RF>
 __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) {
-    constexpr int kSub = 4 / MT;
-    __shared__ float part[kWaves][MT * 16][RF * 16 + (RF < 8 ? 1 : 0)];  // at most 64 KB
-    const LoraTile t = p.tiles[blockIdx.x / kSub];
-    const int first = (int)(blockIdx.x % kSub) * MT * 16;
-    if (first >= t.rows) return;
-    const int rows = min(t.rows - first, MT * 16);
-    const int64_t row0 = t.row + first;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, kg = lane >> 4;
+    constexpr int kX = 64 * 16, kA = RF * 16 * 16;                    // pieces of 16 bytes: 16 to a row
+    constexpr int kSums = kWaves * 16 * (RF * 16 + 4) / 4;            // the same space holds the waves' sums at the end
+    __shared__ u32x4 lds[kX + kA > kSums ? kX + kA : kSums];
+    const LoraTile t = p.tiles[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+    const int shift = t.rows > 32 ? 2 : t.rows > 16 ? 1 : 0;          // log2 of the row groups
+    const int first = (wave & ((1 << shift) - 1)) * 16, turn = wave >> shift;
 
-    f32x4 acc[MT][RF];
+    f32x4 acc[RF];
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int r = 0; r < RF; ++r) acc[m][r] = (f32x4){0, 0, 0, 0};
+    for (int r = 0; r < RF; ++r) acc[r] = (f32x4){0, 0, 0, 0};
     if (t.rank > 0) {
-        const uint16_t* x[MT];
+        // this thread's piece of a row, and its rows tid / 16 + 16 j
+        const int piece = tid & 15, line = tid >> 4;
+        const uint16_t* x[4];
         const uint16_t* a[RF];
-        bool live[RF];
 #pragma unroll
-        for (int m = 0; m < MT; ++m) x[m] = p.x + (row0 + min(m * 16 + i, rows - 1)) * p.ldx + kg * 8;
+        for (int j = 0; j < 4; ++j) x[j] = p.x + ((int64_t)t.row + min(line + 16 * j, t.rows - 1)) * p.ldx + piece * 8;
 #pragma unroll
-        for (int r = 0; r < RF; ++r) {
-            live[r] = r * 16 + i < t.rank;
-            a[r] = p.pool + ((int64_t)t.adapter * p.R + (live[r] ? r * 16 + i : 0)) * p.ldp + kg * 8;
-        }
-        const int64_t begin = ((int64_t)blockIdx.y * kWaves + wave) * p.steps * 32;
-        const int64_t end = min(begin + (int64_t)p.steps * 32, p.K);
-        const int whole = (int)(max(end - begin, (int64_t)0) / 32);
-        int64_t k = begin;
-#pragma unroll 4
-        for (int step = 0; step < whole; ++step, k += 32) {
-            u32x4 xv[MT], av[RF];
+        for (int j = 0; j < RF; ++j) a[j] = p.pool + ((int64_t)t.adapter * p.R + min(line + 16 * j, t.rank - 1)) * p.ldp + piece * 8;
+        int64_t k = (int64_t)blockIdx.y * p.steps * 128;
+        const int64_t end = min(k + (int64_t)p.steps * 128, p.K);
+        u32x4 xv[4], av[RF];
+        auto load = [&]() __attribute__((always_inline)) {
+            if (k + 128 <= end) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) xv[m] = load8(x[m] + k);
+                for (int j = 0; j < 4; ++j)
+                    if (16 * j < t.rows) xv[j] = load8(x[j] + k);
 #pragma unroll
-            for (int r = 0; r < RF; ++r) {
-                av[r] = *(const u32x4*)(a[r] + k);
-                if (!live[r]) av[r] = (u32x4){0, 0, 0, 0};
+                for (int j = 0; j < RF; ++j) av[j] = *(const u32x4*)(a[j] + k);
+            } else {
+                // the pool's rows are padded to 8 values
+                const int64_t left = end - k - piece * 8;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (16 * j < t.rows) xv[j] = load8_part(x[j] + k, left);
+#pragma unroll
+                for (int j = 0; j < RF; ++j) {
+                    av[j] = (u32x4){0, 0, 0, 0};
+                    if (left > 0) av[j] = *(const u32x4*)(a[j] + k);
+                }
             }
+        };
+        if (k < end) load();
+        while (k < end) {
+            // piece c of row r lies at c ^ r % 16: rows read at one piece fall on different banks
 #pragma unroll
-            for (int m = 0; m < MT; ++m)
+            for (int j = 0; j < 4; ++j)
+                if (16 * j < t.rows) lds[(line + 16 * j) * 16 + (piece ^ (line & 15))] = xv[j];
 #pragma unroll
-                for (int r = 0; r < RF; ++r) acc[m][r] = mfma(xv[m], av[r], acc[m][r]);
-        }
-        if (k < end) {
-            // the last, partial step; the pool's rows are padded to 8 values
-            const int64_t left = end - k - kg * 8;
-            u32x4 xv[MT], av[RF];
+            for (int j = 0; j < RF; ++j)
+                lds[kX + (line + 16 * j) * 16 + (piece ^ (line & 15))] = line + 16 * j < t.rank ? av[j] : (u32x4){0, 0, 0, 0};
+            __syncthreads();
+            k += 128;
+            if (k < end) load();
+            if (first < t.rows) {
 #pragma unroll
-            for (int m = 0; m < MT; ++m) xv[m] = load8_part(x[m] + k, left);
+                for (int step = 0; step < 4; ++step) {
+                    if ((step & ((kWaves >> shift) - 1)) != turn) continue;
+                    const int at = i * 16 + ((step * 4 + q) ^ i);
+                    const u32x4 row = lds[first * 16 + at];
 #pragma unroll
-            for (int r = 0; r < RF; ++r) {
-                av[r] = (u32x4){0, 0, 0, 0};
-                if (live[r] && left > 0) av[r] = *(const u32x4*)(a[r] + k);
+                    for (int r = 0; r < RF; ++r) acc[r] = mfma(row, lds[kX + r * 256 + at], acc[r]);
+                }
             }
-#pragma unroll
-            for (int m = 0; m < MT; ++m)
-#pragma unroll
-                for (int r = 0; r < RF; ++r) acc[m][r] = mfma(xv[m], av[r], acc[m][r]);
+            __syncthreads();
         }
     }
+    float* const sums = (float*)lds;
 #pragma unroll
-    for (int m = 0; m < MT; ++m)
+    for (int r = 0; r < RF; ++r)
 #pragma unroll
-        for (int r = 0; r < RF; ++r)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) part[wave][m * 16 + kg * 4 + j][r * 16 + i] = acc[m][r][j];
+        for (int j = 0; j < 4; ++j) sums[(wave * 16 + q * 4 + j) * (RF * 16 + 4) + r * 16 + i] = acc[r][j];
     __syncthreads();
-    float* const out = p.h + ((int64_t)blockIdx.y * p.M + row0) * p.R;
-    for (int e = threadIdx.x; e < rows * p.R; e += 64 * kWaves) {
+    float* const out = p.h + ((int64_t)blockIdx.y * p.M + t.row) * p.R;
+    for (int e = tid; e < t.rows * p.R; e += 64 * kWaves) {
         const int m = e / p.R, r = e - m * p.R;
+        float v = 0.f;
         // a row of x that is not finite times the rank's missing rows of A is nothing all the same
-        out[e] = r < t.rank ? (part[0][m][r] + part[1][m][r]) + (part[2][m][r] + part[3][m][r]) : 0.f;
+        if (r < t.rank)
+            for (int w = m >> 4; w < kWaves; w += 1 << shift) v += sums[(w * 16 + (m & 15)) * (RF * 16 + 4) + r];
+        out[e] = v;
     }
 }
 
-// Eight values of a row of the wide output or of its base.
+// 16 bytes of a row of the wide output and of its base: the first n of their values, or all.
 template <typename T>
-__device__ __forceinline__ void load_wide(const T* p, int64_t n, float* v);
-template <>
-__device__ __forceinline__ void load_wide<bf16_t>(const bf16_t* p, int64_t n, float* v) {
-    const u32x4 w = load8_part((const uint16_t*)p, n);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[2 * i] = bf16_low(w[i]), v[2 * i + 1] = bf16_high(w[i]);
-}
-template <>
-__device__ __forceinline__ void load_wide<float>(const float* p, int64_t n, float* v) {
-    if (n >= 8) {
-        const f32x4 a = ((const Unaligned16f*)p)->v, b = ((const Unaligned16f*)(p + 4))->v;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[i] = a[i], v[i + 4] = b[i];
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
-    }
-}
+struct Wide;
 
-__device__ __forceinline__ void store_wide(bf16_t* p, int64_t n, const float* v) {
-    const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    if (n >= 8) {
-        ((Unaligned16*)p)->v = w;
-    } else {
+template <>
+struct Wide<bf16_t> {
+    static constexpr int kParts = 2, kValues = 8;
+    u32x4 w;
+    __device__ __forceinline__ void load(const bf16_t* p) { w = load8((const uint16_t*)p); }
+    __device__ __forceinline__ void load(const bf16_t* p, int64_t n) { w = load8_part((const uint16_t*)p, n); }
+    __device__ __forceinline__ void clear() { w = (u32x4){0, 0, 0, 0}; }
+    __device__ __forceinline__ void add(const float* d) {
+        const f32x4 a = *(const f32x4*)d, b = *(const f32x4*)(d + 4);
+        w = (u32x4){pack_bf16(bf16_low(w[0]) + a[0], bf16_high(w[0]) + a[1]), pack_bf16(bf16_low(w[1]) + a[2], bf16_high(w[1]) + a[3]),
+                    pack_bf16(bf16_low(w[2]) + b[0], bf16_high(w[2]) + b[1]), pack_bf16(bf16_low(w[3]) + b[2], bf16_high(w[3]) + b[3])};
+    }
+    __device__ __forceinline__ void store(bf16_t* p) const { ((Unaligned16*)p)->v = w; }
+    __device__ __forceinline__ void store(bf16_t* p, int64_t n) const {
+        if (n >= 8) return store(p);
 #pragma unroll
         for (int i = 0; i < 7; ++i)
             if (i < n) p[i].bits = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
     }
-}
-__device__ __forceinline__ void store_wide(float* p, int64_t n, const float* v) {
-    if (n >= 8) {
-        ((Unaligned16f*)p)->v = (f32x4){v[0], v[1], v[2], v[3]};
-        ((Unaligned16f*)(p + 4))->v = (f32x4){v[4], v[5], v[6], v[7]};
-    } else {
+};
+
+template <>
+struct Wide<float> {
+    static constexpr int kParts = 3, kValues = 4;
+    f32x4 w;
+    __device__ __forceinline__ void load(const float* p) { w = ((const Unaligned16f*)p)->v; }
+    __device__ __forceinline__ void load(const float* p, int64_t n) {
+        if (n >= 4) return load(p);
 #pragma unroll
-        for (int i = 0; i < 7; ++i)
-            if (i < n) p[i] = v[i];
+        for (int i = 0; i < 4; ++i) w[i] = i < n ? p[i] : 0.f;
+    }
+    __device__ __forceinline__ void clear() { w = (f32x4){0, 0, 0, 0}; }
+    __device__ __forceinline__ void add(const float* d) { w += *(const f32x4*)d; }
+    __device__ __forceinline__ void store(float* p) const { ((Unaligned16f*)p)->v = w; }
+    __device__ __forceinline__ void store(float* p, int64_t n) const {
+        if (n >= 4) return store(p);
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) p[i] = w[i];
+    }
+};
+
+constexpr int kTimes = 4;  // rows to a lane in a strip of 16 rows of 256 bytes
+
+// A tile's rows of s h as operands of the expansion, and copies of them for the next kernels: 16 rows to a wave, of which
+// the lane has row i and r = 32 c + 8 q .. + 7.
+template <int RC, int PARTS>
+__device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, int first, bool copy, int i, int q, u32x4 (&h)[RC][PARTS]) {
+    const int at = min(first + i, t.rows - 1);
+    const int64_t row = (int64_t)t.row + at;
+    const bool live = first + i < t.rows;
+#pragma unroll
+    for (int c = 0; c < RC; ++c) {
+        const int r = c * 32 + q * 8;
+        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+        if (r < p.R) {
+            const float* from = p.h + row * p.R + r;
+#pragma unroll 4
+            for (int s = 0; s < p.splits; ++s) {
+                const f32x4 lo = *(const f32x4*)(from + s * p.M * p.R), hi = *(const f32x4*)(from + s * p.M * p.R + 4);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) v[j] += lo[j], v[j + 4] += hi[j];
+            }
+        }
+        if (copy && live && r < p.R && p.sum) {
+            float* const to = p.sum + row * p.R + r;
+            *(f32x4*)to = (f32x4){v[0], v[1], v[2], v[3]};
+            *(f32x4*)(to + 4) = (f32x4){v[4], v[5], v[6], v[7]};
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] *= t.scale;
+        if (copy && live && r < p.R && p.turned) {
+            float g[8];
+            u32x4 part[3];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) g[j] = v[j];
+            split8<3>(g, part);
+#pragma unroll
+            for (int k = 0; k < 3; ++k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    p.turned[lora_operand(blockIdx.x, at, k, r + j, p.R)] = (uint16_t)(part[k][j / 2] >> (16 * (j & 1)));
+        }
+        split8<PARTS>(v, h[c]);
     }
 }
 
-// y = base + s h B^T for a tile's rows and `strips` strips of 64 columns to each wave.  The MFMA's rows are columns of y
-// and its columns rows of y, so a lane ends up with values of one row; its fragments take the columns in the order that
-// makes them 8 in a row.  The pool is [adapter][N][R].
+// y = base + s h B^T.  A workgroup takes a tile and p.columns columns of y in strips of 256 bytes, a wave 16 rows.  The
+// strip's rows of the pool [adapter][N][R] are in LDS for all waves.  The MFMA's rows are columns of y and its columns
+// rows of y, so a lane ends up with four values in a row of 16 rows; they turn around in the wave's own part of LDS, so
+// that base and y are read and written in rows of 256 bytes (a copy of 9216 x 9216 bf16 values runs at 4.8 TB/s so, at
+// 4.2 in 16 rows of 64 bytes).  The next strip's loads are on their way while this one is multiplied.
 template <typename T, int RC>
 __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) {
+    constexpr int kParts = Wide<T>::kParts, kValues = Wide<T>::kValues, kStrip = 16 * kValues;
+    constexpr int kPieces = kStrip * RC * 4 / (64 * kWaves);  // of 16 bytes of the pool to a thread
+    constexpr int kRow = kStrip + 4;
+    __shared__ __align__(16) float turn[kWaves * 16 * kRow];
+    __shared__ u32x4 pool_lds[kStrip * (RC * 4 + 1) + 1];  // the last piece is zero
     const LoraTile t = p.tiles[blockIdx.x];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, i = lane & 15, q = lane >> 4;
-    if (t.rank == 0 && p.base == p.y && p.ldb == p.ldy) return;
-    const int frags = (t.rows + 15) / 16;
-    u32x4 hi[4][RC], lo[4][RC], mask[RC];
+    if (t.rank == 0 && p.base == p.y && p.ldb == p.ldy && !p.sum) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
+    const int first = wave * 16;
+    const bool busy = first < t.rows;
+    const int pieces = p.R / 8, stride = pieces | 1;  // of a pool row, in memory and, on all banks, in LDS
+    const uint16_t* const pool = p.pool + (int64_t)max(t.adapter, 0) * p.N * p.R;
+    int64_t n0 = (int64_t)blockIdx.y * p.columns;
+    const int64_t end = min((int64_t)(blockIdx.y + 1) * p.columns, p.N);
+
+    // of this thread: its rows of y 16 wave + q + 4 j and columns there, its pieces of the pool
+    const int col = i * kValues;
+    const T* base[kTimes];
+    T* y[kTimes];
+#pragma unroll
+    for (int j = 0; j < kTimes; ++j) {
+        const int64_t row = (int64_t)t.row + min(first + q + 4 * j, t.rows - 1);
+        base[j] = p.base ? (const T*)p.base + row * p.ldb + col : nullptr;
+        y[j] = (T*)p.y + row * p.ldy + col;
+    }
+    int slot[kPieces];
+#pragma unroll
+    for (int j = 0; j < kPieces; ++j) {
+        const int e = tid + 64 * kWaves * j, n = e / pieces;
+        slot[j] = n < kStrip ? n * stride + e - n * pieces : -1;
+    }
+    Wide<T> wide[kTimes];
+    u32x4 piece[kPieces];
+    auto load_wide = [&](int64_t n) __attribute__((always_inline)) {
+        if (!p.base) {
+#pragma unroll
+            for (int j = 0; j < kTimes; ++j) wide[j].clear();
+        } else if (n + kStrip <= p.N) {
+#pragma unroll
+            for (int j = 0; j < kTimes; ++j) wide[j].load(base[j] + n);
+        } else {
+#pragma unroll
+            for (int j = 0; j < kTimes; ++j)
+                if (wide[j].clear(); n + col < p.N) wide[j].load(base[j] + n, p.N - n - col);
+        }
+    };
+    auto load_pool = [&](int64_t n) __attribute__((always_inline)) {
+        const int64_t last = (p.N - n) * pieces - 1;
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j)
+            piece[j] = *(const u32x4*)(pool + n * p.R + min((int64_t)(slot[j] < 0 ? 0 : tid + 64 * kWaves * j), last) * 8);
+    };
+    if (busy) load_wide(n0);
+    if (t.rank > 0) load_pool(n0);
+    u32x4 h[RC][kParts];
+    if (busy) load_h<RC, kParts>(p, t, first, blockIdx.y == 0, i, q, h);
+
+    // where the lane's operand pieces lie: those beyond R are the zero one
+    constexpr int kZero = kStrip * (RC * 4 + 1);
+    if (tid == 0) pool_lds[kZero] = (u32x4){0, 0, 0, 0};
+    int operand[RC], next[RC];
 #pragma unroll
     for (int c = 0; c < RC; ++c) {
+        const bool there = c * 4 + q < pieces;
+        operand[c] = there ? i * stride + c * 4 + q : kZero;
+        next[c] = there ? 16 * stride : 0;
+    }
+    float* const mine = turn + wave * 16 * kRow;
+    for (; n0 < end; n0 += kStrip) {
+        if (t.rank > 0) {
+#pragma unroll
+            for (int j = 0; j < kPieces; ++j) {
+                if (t.rank < p.R) {
+                    const int left = t.rank - (tid + 64 * kWaves * j) % pieces * 8;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) piece[j][e] &= (2 * e < left ? 0xFFFFu : 0u) | (2 * e + 1 < left ? 0xFFFF0000u : 0u);
+                }
+                if (slot[j] >= 0) pool_lds[slot[j]] = piece[j];
+            }
+            __syncthreads();
+            if (n0 + kStrip < end) load_pool(n0 + kStrip);
+            if (busy) {
+                f32x4 acc[kValues];
+#pragma unroll
+                for (int f = 0; f < kValues; ++f) {
+                    acc[f] = (f32x4){0, 0, 0, 0};
+#pragma unroll
+                    for (int c = 0; c < RC; ++c) {
+                        const u32x4 b = pool_lds[operand[c] + f * next[c]];
+#pragma unroll
+                        for (int k = kParts - 1; k >= 0; --k) acc[f] = mfma(b, h[c][k], acc[f]);
+                    }
+                }
+#pragma unroll
+                for (int f = 0; f < kValues; ++f) *(f32x4*)(mine + i * kRow + 16 * f + 4 * q) = acc[f];
+                // the wave's own rows of LDS: its accesses stay in order, and the compiler keeps them so
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int j = 0; j < kTimes; ++j) wide[j].add(mine + (q + 4 * j) * kRow + col);
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+                __builtin_amdgcn_wave_barrier();
+            }
+        }
+        if (busy) {
+            const bool whole = n0 + kStrip <= p.N;
+#pragma unroll
+            for (int j = 0; j < kTimes; ++j) {
+                if (first + q + 4 * j < t.rows) {
+                    if (whole)
+                        wide[j].store(y[j] + n0);
+                    else if (n0 + col < p.N)
+                        wide[j].store(y[j] + n0, p.N - n0 - col);
+                }
+            }
+            if (n0 + kStrip < end) load_wide(n0 + kStrip);
+        }
+        if (t.rank > 0) __syncthreads();
+    }
+}
+
+// The same for tiles of few rows, which are bound by latency and by the pool: every wave has the tile's 16 rows (or every
+// second one the first, where it has more) and strips of its own, and takes the pool's rows straight from memory.
+template <typename T, int RC>
+__global__ __launch_bounds__(64 * kWaves) void lora_expand_few_kernel(LoraExpand p) {
+    constexpr int kParts = Wide<T>::kParts, kValues = Wide<T>::kValues, kStrip = 16 * kValues, kRow = kStrip + 4;
+    __shared__ __align__(16) float turn[kWaves * 16 * kRow];
+    const LoraTile t = p.tiles[blockIdx.x];
+    if (t.rank == 0 && p.base == p.y && p.ldb == p.ldy && !p.sum) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
+    const int shift = t.rows > 32 ? 2 : t.rows > 16 ? 1 : 0;  // log2 of the row groups
+    const int first = (wave & ((1 << shift) - 1)) * 16, beside = wave >> shift, step = (kWaves >> shift) * kStrip;
+    if (first >= t.rows) return;
+    const uint16_t* const pool = p.pool + (int64_t)max(t.adapter, 0) * p.N * p.R;
+    int64_t n0 = (int64_t)blockIdx.y * p.columns + beside * kStrip;
+    const int64_t end = min((int64_t)(blockIdx.y + 1) * p.columns, p.N);
+    const int col = i * kValues;
+    Wide<T> wide[kTimes];
+    u32x4 b[kValues][RC], mask[RC], h[RC][kParts];
+    auto load = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kTimes; ++j) {
+            wide[j].clear();
+            if (p.base && n0 + col < p.N && first + q + 4 * j < t.rows)
+                wide[j].load((const T*)p.base + ((int64_t)t.row + first + q + 4 * j) * p.ldb + n0 + col, p.N - n0 - col);
+        }
+        if (t.rank > 0) {
+#pragma unroll
+            for (int f = 0; f < kValues; ++f)
+#pragma unroll
+                for (int c = 0; c < RC; ++c) {
+                    const int r = c * 32 + q * 8;
+                    b[f][c] = *(const u32x4*)(pool + min(n0 + 16 * f + i, p.N - 1) * p.R + (r < p.R ? r : 0));
+                }
+        }
+    };
+    if (n0 < end) load();
+    load_h<RC, kParts>(p, t, first, blockIdx.y == 0 && beside == 0, i, q, h);
+#pragma unroll
+    for (int c = 0; c < RC; ++c)
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int r = c * 32 + q * 8 + 2 * j;
             mask[c][j] = (r < t.rank ? 0xFFFFu : 0u) | (r + 1 < t.rank ? 0xFFFF0000u : 0u);
         }
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            if (m >= frags) break;
-            const int row = min(m * 16 + i, t.rows - 1), r = c * 32 + q * 8;
-            float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-            if (r < p.R) {
-                const float* from = p.h + ((int64_t)t.row + row) * p.R + r;
-                for (int s = 0; s < p.splits; ++s, from += p.M * p.R) {
-                    const f32x4 a = *(const f32x4*)from, b = *(const f32x4*)(from + 4);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] += a[j], v[j + 4] += b[j];
-                }
-                if (p.sum && blockIdx.y == 0 && wave == 0 && m * 16 + i < t.rows) {
-                    float* const to = p.sum + ((int64_t)t.row + row) * p.R + r;
-                    *(f32x4*)to = (f32x4){v[0], v[1], v[2], v[3]};
-                    *(f32x4*)(to + 4) = (f32x4){v[4], v[5], v[6], v[7]};
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] *= t.scale;
-            split8(v, hi[m][c], lo[m][c]);
-        }
-    }
-    const uint16_t* const pool = p.pool + (int64_t)max(t.adapter, 0) * p.N * p.R;
-    for (int s = 0; s < p.strips; ++s) {
-        const int64_t n0 = (((int64_t)blockIdx.y * p.strips + s) * kWaves + wave) * 64;
-        if (n0 >= p.N) break;
-        // fragment f = 2 pair + half: its row i is column n0 + 32 pair + 8 (i / 4) + 4 half + i % 4
-        f32x4 acc[4][4];
-#pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            if (m >= frags) break;
-            const int64_t row = t.row + min(m * 16 + i, t.rows - 1);
-#pragma unroll
-            for (int pair = 0; pair < 2; ++pair) {
-                const int64_t n = n0 + 32 * pair + 8 * q;
-                float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-                if (p.base && n < p.N) load_wide<T>((const T*)p.base + row * p.ldb + n, p.N - n, v);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) acc[m][2 * pair][j] = v[j], acc[m][2 * pair + 1][j] = v[j + 4];
-            }
-        }
+    float* const mine = turn + wave * 16 * kRow;
+    while (n0 < end) {
         if (t.rank > 0) {
-            u32x4 b[4][RC];
+            f32x4 acc[kValues];
 #pragma unroll
-            for (int f = 0; f < 4; ++f) {
-                const int64_t n = min(n0 + 32 * (f / 2) + 8 * (i / 4) + 4 * (f & 1) + i % 4, p.N - 1);
+            for (int f = 0; f < kValues; ++f) {
+                acc[f] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-                for (int c = 0; c < RC; ++c) {
-                    const int r = c * 32 + q * 8;
-                    b[f][c] = *(const u32x4*)(pool + n * p.R + (r < p.R ? r : 0)) & mask[c];
-                }
+                for (int c = 0; c < RC; ++c)
+#pragma unroll
+                    for (int k = kParts - 1; k >= 0; --k) acc[f] = mfma(b[f][c] & mask[c], h[c][k], acc[f]);
             }
 #pragma unroll
-            for (int m = 0; m < 4; ++m) {
-                if (m >= frags) break;
+            for (int f = 0; f < kValues; ++f) *(f32x4*)(mine + i * kRow + 16 * f + 4 * q) = acc[f];
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
 #pragma unroll
-                for (int f = 0; f < 4; ++f)
-#pragma unroll
-                    for (int c = 0; c < RC; ++c) {
-                        acc[m][f] = mfma(b[f][c], lo[m][c], acc[m][f]);
-                        acc[m][f] = mfma(b[f][c], hi[m][c], acc[m][f]);
-                    }
-            }
+            for (int j = 0; j < kTimes; ++j) wide[j].add(mine + (q + 4 * j) * kRow + col);
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
         }
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            if (m >= frags || m * 16 + i >= t.rows) break;
-            const int64_t row = t.row + m * 16 + i;
-#pragma unroll
-            for (int pair = 0; pair < 2; ++pair) {
-                const int64_t n = n0 + 32 * pair + 8 * q;
-                float v[8];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] = acc[m][2 * pair][j], v[j + 4] = acc[m][2 * pair + 1][j];
-                if (n < p.N) store_wide((T*)p.y + row * p.ldy + n, p.N - n, v);
-            }
-        }
+        for (int j = 0; j < kTimes; ++j)
+            if (n0 + col < p.N && first + q + 4 * j < t.rows)
+                wide[j].store((T*)p.y + ((int64_t)t.row + first + q + 4 * j) * p.ldy + n0 + col, p.N - n0 - col);
+        n0 += step;
+        if (n0 < end) load();
     }
 }
 
-// Pools with the other side contiguous, for the backward pass: A [R][K] -> [K][R], B [N][R] -> [R][N padded to 8].  A
-// thread turns a block of 8 x 8.
-__global__ __launch_bounds__(256) void lora_transpose_kernel(LoraTranspose p) {
-    const int64_t a_blocks = (int64_t)(p.R / 8) * (p.K / 8), b_blocks = (int64_t)(p.R / 8) * (p.ldt / 8);
+// What the backward pass reads the other way round: A [R][K] -> [K][R], B [N][R] -> [R][N padded to 8], and s h [M][R] as
+// three bf16 parts in the order of lora_operand.  A thread turns a block of 8 x 8.
+__global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
+    const int64_t r_blocks = p.R / 8, a_blocks = r_blocks * (p.K / 8), b_blocks = r_blocks * (p.ldn / 8);
+    const int64_t pools = (a_blocks + b_blocks) * p.adapters;
     int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t adapter = blockIdx.y;
-    u32x4 v[8];
-    if (at < a_blocks) {
-        const int r = (int)(at % (p.R / 8)) * 8;
-        const int64_t k = at / (p.R / 8) * 8;
-        const uint16_t* const from = p.a + adapter * p.R * p.K + r * p.K + k;
+    if (at < pools) {
+        const int64_t adapter = at / (a_blocks + b_blocks);
+        at -= adapter * (a_blocks + b_blocks);
+        u32x4 v[8];
+        if (at < a_blocks) {
+            const int64_t k = at / r_blocks * 8, r = at % r_blocks * 8;
+            const uint16_t* const from = p.a + (adapter * p.R + r) * p.K + k;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = *(const u32x4*)(from + j * p.K);
-        transpose8(v);
-        uint16_t* const to = p.at + adapter * p.R * p.K + k * p.R + r;
+            for (int j = 0; j < 8; ++j) v[j] = *(const u32x4*)(from + j * p.K);
+            transpose8(v);
+            uint16_t* const to = p.at + (adapter * p.K + k) * p.R + r;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) *(u32x4*)(to + j * p.R) = v[j];
+            for (int j = 0; j < 8; ++j) *(u32x4*)(to + j * p.R) = v[j];
+        } else {
+            at -= a_blocks;
+            const int64_t r = at / (p.ldn / 8) * 8, n = at % (p.ldn / 8) * 8;
+            const uint16_t* const from = p.b + (adapter * p.N + n) * p.R + r;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                v[j] = (u32x4){0, 0, 0, 0};
+                if (n + j < p.N) v[j] = *(const u32x4*)(from + j * p.R);
+            }
+            transpose8(v);
+            uint16_t* const to = p.bt + (adapter * p.R + r) * p.ldn + n;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) *(u32x4*)(to + j * p.ldn) = v[j];
+        }
         return;
     }
-    at -= a_blocks;
-    if (at >= b_blocks) return;
-    const int64_t n = at % (p.ldt / 8) * 8;
-    const int r = (int)(at / (p.ldt / 8)) * 8;
-    const uint16_t* const from = p.b + adapter * p.N * p.R + n * p.R + r;
+    at -= pools;
+    const int64_t tile = at / (8 * r_blocks);
+    if (tile >= p.count) return;
+    const LoraTile t = p.tiles[tile];
+    const int in_tile = (int)(at - tile * 8 * r_blocks), first = in_tile % 8 * 8, r = in_tile / 8 * 8;
+    if (first >= t.rows || t.rank == 0) return;
+    float v[8][8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        v[j] = (u32x4){0, 0, 0, 0};
-        if (n + j < p.N) v[j] = *(const u32x4*)(from + j * p.R);
-    }
-    transpose8(v);
-    uint16_t* const to = p.bt + (adapter * p.R + r) * p.ldt + n;
+        const float* const from = p.h + ((int64_t)t.row + min(first + j, t.rows - 1)) * p.R + r;
+        const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) *(u32x4*)(to + j * p.ldt) = v[j];
+        for (int e = 0; e < 4; ++e) v[e][j] = lo[e] * t.scale, v[e + 4][j] = hi[e] * t.scale;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        u32x4 part[3];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[e][j] = r + e < t.rank ? v[e][j] : 0.f;
+        split8<3>(v[e], part);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *(u32x4*)(p.turned + lora_operand(tile, first, k, r + e, p.R)) = part[k];
+    }
 }
 
 // Partial sums [split][R][width] over a split's rows of s narrow^T wide: of g and x (dA) in the first workgroups of a
@@ -345,7 +547,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
     const bool second = at_chunk >= p.chunks_x;
     const LoraGradSide side = p.side[second];
     const int chunk = at_chunk - (second ? p.chunks_x : 0);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, kg = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kg = lane >> 4;
     const int r0 = blockIdx.y * RF * 16;
     const int64_t col = (int64_t)chunk * 128 + c * 8;
     const int64_t left = side.width - col;
@@ -355,35 +557,45 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
     for (int r = 0; r < RF; ++r)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[r][j] = (f32x4){0, 0, 0, 0};
+    const bool wide_whole = side.width - (int64_t)chunk * 128 >= 128;
     for (int step = 2 * split.begin + wave; step < 2 * split.end; step += kWaves) {
         const LoraTile t = p.tiles[step / 2];
-        const int first = (step & 1) * 32 + kg * 8;  // this lane's rows of the tile
-        u32x4 z[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            z[j] = (u32x4){0, 0, 0, 0};
-            if (first + j < t.rows) z[j] = load8_part(side.wide + ((int64_t)t.row + first + j) * side.ld + col, left);
-        }
-        u32x4 hi[RF], lo[RF];
+        const int first = (step & 1) * 32;
+        if (first >= t.rows) continue;
+        const int mine = first + kg * 8;  // this lane's first row of the tile
+        u32x4 z[8], part[RF][3];
 #pragma unroll
         for (int r = 0; r < RF; ++r) {
-            const int at = r0 + r * 16 + c;
-            float v[8];
+            const int frag = min(r0 / 16 + r, (p.R - 1) / 16);
+#pragma unroll
+            for (int k = 0; k < 3; ++k) part[r][k] = *(const u32x4*)(side.narrow + lora_operand(step / 2, first, k, frag * 16, p.R) + lane * 8);
+        }
+        if (wide_whole && first + 32 <= t.rows) {
+            const uint16_t* const from = side.wide + ((int64_t)t.row + mine) * side.ld + col;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) z[j] = load8(from + j * side.ld);
+        } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                v[j] = 0.f;
-                if (first + j < t.rows && at < t.rank) v[j] = side.narrow[((int64_t)t.row + first + j) * p.R + at] * t.scale;
+                z[j] = (u32x4){0, 0, 0, 0};
+                if (mine + j < t.rows) z[j] = load8_part(side.wide + ((int64_t)t.row + mine + j) * side.ld + col, left);
             }
-            split8(v, hi[r], lo[r]);
+            // rows beyond the tile are another's, or none
+#pragma unroll
+            for (int r = 0; r < RF; ++r)
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        part[r][k][j] &= (mine + 2 * j < t.rows ? 0xFFFFu : 0u) | (mine + 2 * j + 1 < t.rows ? 0xFFFF0000u : 0u);
         }
         transpose8(z);
 #pragma unroll
         for (int r = 0; r < RF; ++r)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                acc[r][j] = mfma(lo[r], z[j], acc[r][j]);
-                acc[r][j] = mfma(hi[r], z[j], acc[r][j]);
-            }
+            for (int k = 2; k >= 0; --k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[r][j] = mfma(part[r][k], z[j], acc[r][j]);
     }
     // the waves' sums, in order
     for (int w = 0; w < kWaves; ++w) {
@@ -434,58 +646,53 @@ __global__ __launch_bounds__(256) void lora_grad_sum_kernel(LoraGrad p) {
     }
 }
 
-template <int MT>
-void shrink(const LoraShrink& p, dim3 grid, hipStream_t stream) {
-    if (p.R <= 16)
-        lora_shrink_kernel<MT, 1><<<grid, 64 * kWaves, 0, stream>>>(p);
-    else if (p.R <= 32)
-        lora_shrink_kernel<MT, 2><<<grid, 64 * kWaves, 0, stream>>>(p);
-    else if (p.R <= 64)
-        lora_shrink_kernel<MT, 4><<<grid, 64 * kWaves, 0, stream>>>(p);
-    else
-        lora_shrink_kernel<MT, 8><<<grid, 64 * kWaves, 0, stream>>>(p);
-}
-
 template <typename T>
-void expand(const LoraExpand& p, dim3 grid, hipStream_t stream) {
+void expand(const LoraExpand& p, dim3 grid, bool few, hipStream_t stream) {
     if (p.R <= 32)
-        lora_expand_kernel<T, 1><<<grid, 64 * kWaves, 0, stream>>>(p);
+        few ? lora_expand_few_kernel<T, 1><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 1><<<grid, 64 * kWaves, 0, stream>>>(p);
     else if (p.R <= 64)
-        lora_expand_kernel<T, 2><<<grid, 64 * kWaves, 0, stream>>>(p);
+        few ? lora_expand_few_kernel<T, 2><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 2><<<grid, 64 * kWaves, 0, stream>>>(p);
     else
-        lora_expand_kernel<T, 4><<<grid, 64 * kWaves, 0, stream>>>(p);
+        few ? lora_expand_few_kernel<T, 4><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 4><<<grid, 64 * kWaves, 0, stream>>>(p);
 }
 
 }  // namespace
 
 int lora_splits(int tiles, int64_t K, int cus) {
-    // halves of the K range until the waves of two-row-fragment workgroups are 8 to a compute unit, a wave keeping
-    // at least 4 steps of 32
+    // halves of the K range until the workgroups are 2 to a compute unit, each keeping at least 2 chunks of 128
     int splits = 1;
-    while (splits < kLoraMaxSplits && (int64_t)tiles * 2 * kWaves * splits < 8 * (int64_t)cus && K >= (int64_t)splits * 2 * kWaves * 4 * 32)
-        splits *= 2;
+    while (splits < kLoraMaxSplits && (int64_t)tiles * splits < 2 * (int64_t)cus && K >= (int64_t)splits * 2 * 2 * 128) splits *= 2;
     return splits;
 }
 
 hipError_t launch_lora_shrink(LoraShrink p, int tiles, int splits, hipStream_t stream) {
-    const int64_t steps = (p.K + 31) / 32;
-    p.steps = (int)((steps + splits * kWaves - 1) / (splits * kWaves));
-    shrink<2>(p, dim3(tiles * 2, splits), stream);
+    const int64_t steps = (p.K + 127) / 128;
+    p.steps = (int)((steps + splits - 1) / splits);
+    const dim3 grid(tiles, splits);
+    if (p.R <= 16)
+        lora_shrink_kernel<1><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else if (p.R <= 32)
+        lora_shrink_kernel<2><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else if (p.R <= 64)
+        lora_shrink_kernel<4><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else
+        lora_shrink_kernel<8><<<grid, 64 * kWaves, 0, stream>>>(p);
     return hipGetLastError();
 }
 
 hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream) {
-    // four strips to a wave where that leaves 4 workgroups to a compute unit
-    const int64_t blocks = (p.N + 64 * kWaves - 1) / (64 * kWaves);
-    p.strips = (int)std::max<int64_t>(1, std::min<int64_t>(4, tiles * blocks / (4 * (int64_t)cus)));
-    const dim3 grid(tiles, (unsigned)((blocks + p.strips - 1) / p.strips));
-    f32 ? expand<float>(p, grid, stream) : expand<bf16_t>(p, grid, stream);
+    // 1024 columns to a workgroup, fewer where that leaves less than 8 workgroups to a compute unit
+    p.columns = 1024;
+    while (p.columns > 512 && tiles * ((p.N + p.columns - 1) / p.columns) < 8 * (int64_t)cus) p.columns /= 2;
+    const dim3 grid(tiles, (unsigned)((p.N + p.columns - 1) / p.columns));
+    const bool few = p.M < 24 * (int64_t)tiles;
+    f32 ? expand<float>(p, grid, few, stream) : expand<bf16_t>(p, grid, few, stream);
     return hipGetLastError();
 }
 
-hipError_t launch_lora_transpose(const LoraTranspose& p, int adapters, hipStream_t stream) {
-    const int64_t blocks = (int64_t)(p.R / 8) * (p.K / 8 + p.ldt / 8);
-    lora_transpose_kernel<<<dim3((unsigned)((blocks + 255) / 256), adapters), 256, 0, stream>>>(p);
+hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream) {
+    const int64_t blocks = (int64_t)(p.R / 8) * ((p.K / 8 + p.ldn / 8) * p.adapters + 8 * p.count);
+    lora_turn_kernel<<<(unsigned)((blocks + 255) / 256), 256, 0, stream>>>(p);
     return hipGetLastError();
 }
 

@@ -80,8 +80,8 @@ size_t padded(int64_t bytes) { return ((size_t)bytes + 255) / 256 * 256; }
 struct Layout {
     int splits = 1;         // of the shrink's contraction
     int level = 0;          // of the gradients' splits
-    size_t h = 0, sum = 0, at = 0, bt = 0, grad_x = 0, grad_y = 0, bytes = 0;
-    int64_t ldt = 0;
+    size_t g = 0, g_turned = 0, h_turned = 0, at = 0, bt = 0, grad_x = 0, grad_y = 0, bytes = 0;
+    int64_t ldn = 0;        // rows of the turned B
 };
 
 Layout forward_layout(orbit_lora p, int64_t K, int R, int cus, bool h_given) {
@@ -94,21 +94,22 @@ Layout forward_layout(orbit_lora p, int64_t K, int R, int cus, bool h_given) {
 Layout backward_layout(orbit_lora p, int64_t K, int64_t N, int R, int cus) {
     Layout l;
     const int64_t n = p->adapters;
-    l.ldt = (N + 7) / 8 * 8;
+    l.ldn = (N + 7) / 8 * 8;
     l.splits = lora_splits((int)p->tiles, N, cus);
     const int64_t chunks = ((K + 127) / 128 + (N + 127) / 128) * (R > 64 ? 2 : 1);
     l.level = kLoraLevels - 1;
-    while (l.level > 0 && p->splits[l.level] * chunks < 4 * (int64_t)cus) --l.level;
+    while (l.level > 0 && p->splits[l.level] * chunks < 2 * (int64_t)cus) --l.level;
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t here = at;
         at += padded(bytes);
         return here;
     };
-    l.h = take(l.splits * p->rows * R * (int64_t)sizeof(float));
-    l.sum = l.splits > 1 ? take(p->rows * R * (int64_t)sizeof(float)) : l.h;
+    l.g = take(l.splits * p->rows * R * (int64_t)sizeof(float));
+    l.g_turned = take(lora_operand_bytes(p->tiles, R));
+    l.h_turned = take(lora_operand_bytes(p->tiles, R));
     l.at = take(n * K * R * 2);
-    l.bt = take(n * R * l.ldt * 2);
+    l.bt = take(n * R * l.ldn * 2);
     l.grad_x = take(p->splits[l.level] * R * K * (int64_t)sizeof(float));
     l.grad_y = take(p->splits[l.level] * R * N * (int64_t)sizeof(float));
     l.bytes = at;
@@ -295,40 +296,47 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
     const Layout l = backward_layout(p, K, N, R, info.cus);
     if (!workspace || !aligned(workspace, 16) || workspace_bytes < l.bytes)
         return fail(ORBIT_EINVAL, "%s: takes a workspace of %zu bytes, aligned to 16", who, l.bytes);
-    if (p->splits[l.level] * (((K + 127) / 128) + ((N + 127) / 128)) > (int64_t)1 << 23)
-        return fail(ORBIT_EUNSUPPORTED, "%s: the gradients' launch grid is too large", who);
+    // launch grids hold fewer than 2^32 threads
+    if (p->splits[l.level] * ((K + 127) / 128 + (N + 127) / 128) > (int64_t)1 << 23 ||
+        (R / 8) * ((K / 8 + l.ldn / 8) * p->adapters + 8 * p->tiles) > (int64_t)1 << 31)
+        return fail(ORBIT_EUNSUPPORTED, "%s: the launch grids are too large", who);
     unsigned char* const ws = (unsigned char*)workspace;
     hipStream_t hs = (hipStream_t)stream;
     hipError_t e;
     LoraGrad d{};
     if (p->rows) {
-        LoraTranspose t{};
+        LoraTurn t{};
         t.a = A;
         t.b = B;
         t.at = (uint16_t*)(ws + l.at);
         t.bt = (uint16_t*)(ws + l.bt);
         t.K = K;
         t.N = N;
-        t.ldt = l.ldt;
+        t.ldn = l.ldn;
         t.R = R;
-        e = launch_lora_transpose(t, p->adapters, hs);
+        t.adapters = p->adapters;
+        t.tiles = (const LoraTile*)lists;
+        t.count = p->tiles;
+        t.h = h;
+        t.turned = (uint16_t*)(ws + l.h_turned);
+        e = launch_lora_turn(t, hs);
         if (e != hipSuccess) return hip_fail(e, who);
         LoraShrink s{};
-        s.tiles = (const LoraTile*)lists;
+        s.tiles = t.tiles;
         s.x = dY;
         s.ldx = ldd;
         s.M = p->rows;
         s.K = N;
         s.pool = t.bt;
-        s.ldp = l.ldt;
+        s.ldp = l.ldn;
         s.R = R;
-        s.h = (float*)(ws + l.h);
+        s.h = (float*)(ws + l.g);
         e = launch_lora_shrink(s, (int)p->tiles, l.splits, hs);
         if (e != hipSuccess) return hip_fail(e, who);
         LoraExpand x{};
-        x.tiles = s.tiles;
+        x.tiles = t.tiles;
         x.h = s.h;
-        x.sum = l.splits > 1 ? (float*)(ws + l.sum) : nullptr;
+        x.turned = (uint16_t*)(ws + l.g_turned);
         x.splits = l.splits;
         x.R = R;
         x.M = p->rows;
@@ -340,12 +348,12 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
         x.ldy = lddx;
         e = launch_lora_expand(x, (int)p->tiles, false, info.cus, hs);
         if (e != hipSuccess) return hip_fail(e, who);
-        d.tiles = s.tiles;
+        d.tiles = t.tiles;
     }
     d.list = (const LoraSplit*)(lists + p->at_splits[l.level]);
     d.first = (const int32_t*)(lists + p->at_first[l.level]);
-    d.side[0] = {X, ldx, K, (const float*)(ws + l.sum), (float*)(ws + l.grad_x), dA};
-    d.side[1] = {dY, ldd, N, h, (float*)(ws + l.grad_y), dB};
+    d.side[0] = {X, ldx, K, (const uint16_t*)(ws + l.g_turned), (float*)(ws + l.grad_x), dA};
+    d.side[1] = {dY, ldd, N, (const uint16_t*)(ws + l.h_turned), (float*)(ws + l.grad_y), dB};
     d.R = R;
     e = launch_lora_grad(d, (int)p->splits[l.level], p->adapters, hs);
     return e == hipSuccess ? ORBIT_OK : hip_fail(e, who);
