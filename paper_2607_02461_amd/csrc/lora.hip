@@ -20,6 +20,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device.h"
 #include "vec.h"
@@ -93,23 +94,23 @@ __device__ __forceinline__ int64_t lora_operand(int64_t tile, int row, int k, in
 }
 
 // h partial sums [split][M][R] of rows x [M][K] and pool [adapter][R][K]: a workgroup takes a tile and a split of K, in
-// chunks of 128 that all its waves bring to LDS, the next one's loads on their way while this one is multiplied.  A wave
-// has 16 rows; in a tile with fewer rows, several have the same and every second or fourth step of 32.
+// chunks of 128 that all its waves bring to LDS, the loads of the next two on their way while one is multiplied.  Each wave
+// takes 32 of a chunk's 128 for all rows, so that LDS is read once, and their sums are added at the end.
 template <int RF>
 __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) {
     constexpr int kX = 64 * 16, kA = RF * 16 * 16;                    // pieces of 16 bytes: 16 to a row
-    constexpr int kSums = kWaves * 16 * (RF * 16 + 4) / 4;            // the same space holds the waves' sums at the end
-    __shared__ u32x4 lds[kX + kA > kSums ? kX + kA : kSums];
+    constexpr int kSumRow = RF * 16 + 4, kSums = kWaves * 16 * kSumRow / 4;
+    __shared__ u32x4 lds[kX + kA > kSums ? kX + kA : kSums];          // at the end the waves' sums of 16 rows
     const LoraTile t = p.tiles[blockIdx.x];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
-    const int shift = t.rows > 32 ? 2 : t.rows > 16 ? 1 : 0;          // log2 of the row groups
-    const int first = (wave & ((1 << shift) - 1)) * 16, turn = wave >> shift;
 
-    f32x4 acc[RF];
+    f32x4 acc[4][RF];
 #pragma unroll
-    for (int r = 0; r < RF; ++r) acc[r] = (f32x4){0, 0, 0, 0};
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int r = 0; r < RF; ++r) acc[m][r] = (f32x4){0, 0, 0, 0};
     if (t.rank > 0) {
-        // this thread's piece of a row, and its rows tid / 16 + 16 j
+        // this thread's piece of a row, and its rows tid / 16 + 16 j (the last one again beyond the tile's and the rank's)
         const int piece = tid & 15, line = tid >> 4;
         const uint16_t* x[4];
         const uint16_t* a[RF];
@@ -118,67 +119,88 @@ __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) 
 #pragma unroll
         for (int j = 0; j < RF; ++j) a[j] = p.pool + ((int64_t)t.adapter * p.R + min(line + 16 * j, t.rank - 1)) * p.ldp + piece * 8;
         int64_t k = (int64_t)blockIdx.y * p.steps * 128;
-        const int64_t end = min(k + (int64_t)p.steps * 128, p.K);
-        u32x4 xv[4], av[RF];
-        auto load = [&]() __attribute__((always_inline)) {
-            if (k + 128 <= end) {
+        const int64_t end = max(k, min(k + (int64_t)p.steps * 128, p.K));
+        u32x4 xv[2][4], av[2][RF];
+        auto load = [&](int d, int64_t at) __attribute__((always_inline)) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (16 * j < t.rows) xv[j] = load8(x[j] + k);
+            for (int j = 0; j < 4; ++j) xv[d][j] = load8(x[j] + at);
 #pragma unroll
-                for (int j = 0; j < RF; ++j) av[j] = *(const u32x4*)(a[j] + k);
-            } else {
-                // the pool's rows are padded to 8 values
-                const int64_t left = end - k - piece * 8;
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    if (16 * j < t.rows) xv[j] = load8_part(x[j] + k, left);
-#pragma unroll
-                for (int j = 0; j < RF; ++j) {
-                    av[j] = (u32x4){0, 0, 0, 0};
-                    if (left > 0) av[j] = *(const u32x4*)(a[j] + k);
-                }
-            }
+            for (int j = 0; j < RF; ++j) av[d][j] = *(const u32x4*)(a[j] + at);
         };
-        if (k < end) load();
-        while (k < end) {
+        auto stage = [&](int d) __attribute__((always_inline)) {
             // piece c of row r lies at c ^ r % 16: rows read at one piece fall on different banks
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (16 * j < t.rows) lds[(line + 16 * j) * 16 + (piece ^ (line & 15))] = xv[j];
+            for (int j = 0; j < 4; ++j) lds[(line + 16 * j) * 16 + (piece ^ line)] = xv[d][j];
 #pragma unroll
-            for (int j = 0; j < RF; ++j)
-                lds[kX + (line + 16 * j) * 16 + (piece ^ (line & 15))] = line + 16 * j < t.rank ? av[j] : (u32x4){0, 0, 0, 0};
+            for (int j = 0; j < RF; ++j) lds[kX + (line + 16 * j) * 16 + (piece ^ line)] = line + 16 * j < t.rank ? av[d][j] : (u32x4){0, 0, 0, 0};
             __syncthreads();
-            k += 128;
-            if (k < end) load();
-            if (first < t.rows) {
+        };
+        const int mine = i * 16 + ((wave * 4 + q) ^ i);
+        auto multiply = [&]() __attribute__((always_inline)) {
+            u32x4 row[4];
 #pragma unroll
-                for (int step = 0; step < 4; ++step) {
-                    if ((step & ((kWaves >> shift) - 1)) != turn) continue;
-                    const int at = i * 16 + ((step * 4 + q) ^ i);
-                    const u32x4 row = lds[first * 16 + at];
+            for (int m = 0; m < 4; ++m) row[m] = lds[m * 256 + mine];
 #pragma unroll
-                    for (int r = 0; r < RF; ++r) acc[r] = mfma(row, lds[kX + r * 256 + at], acc[r]);
-                }
+            for (int r = 0; r < RF; ++r) {
+                const u32x4 of_a = lds[kX + r * 256 + mine];
+#pragma unroll
+                for (int m = 0; m < 4; ++m) acc[m][r] = mfma(row[m], of_a, acc[m][r]);
             }
             __syncthreads();
+        };
+        // every load in this loop comes whether it is needed or not (the last chunk's again), and nothing leaves the loop
+        // halfway: after a branch around a load the compiler waits for all of them
+        const int n = (int)((end - k) / 128);
+        if (n > 0) {
+            load(0, k);
+            load(1, k + 128 * min(1, n - 1));
+            int c = 0;
+            for (; c < n - 1; c += 2) {
+                stage(0);
+                load(0, k + 128 * (int64_t)min(c + 2, n - 1));
+                multiply();
+                stage(1);
+                load(1, k + 128 * (int64_t)min(c + 3, n - 1));
+                multiply();
+            }
+            if (c < n) {
+                stage(0);
+                multiply();
+            }
+            k += 128 * (int64_t)n;
+        }
+        if (k < end) {
+            // a partial chunk; the pool's rows are padded to 8 values
+            const int64_t left = end - k - piece * 8;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xv[0][j] = load8_part(x[j] + k, left);
+#pragma unroll
+            for (int j = 0; j < RF; ++j) {
+                av[0][j] = (u32x4){0, 0, 0, 0};
+                if (left > 0) av[0][j] = *(const u32x4*)(a[j] + k);
+            }
+            stage(0);
+            multiply();
         }
     }
     float* const sums = (float*)lds;
-#pragma unroll
-    for (int r = 0; r < RF; ++r)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sums[(wave * 16 + q * 4 + j) * (RF * 16 + 4) + r * 16 + i] = acc[r][j];
-    __syncthreads();
     float* const out = p.h + ((int64_t)blockIdx.y * p.M + t.row) * p.R;
-    for (int e = tid; e < t.rows * p.R; e += 64 * kWaves) {
-        const int m = e / p.R, r = e - m * p.R;
-        float v = 0.f;
-        // a row of x that is not finite times the rank's missing rows of A is nothing all the same
-        if (r < t.rank)
-            for (int w = m >> 4; w < kWaves; w += 1 << shift) v += sums[(w * 16 + (m & 15)) * (RF * 16 + 4) + r];
-        out[e] = v;
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+        if (m * 16 >= t.rows) break;
+        if (m) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < RF; ++r)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) sums[(wave * 16 + q * 4 + j) * kSumRow + r * 16 + i] = acc[m][r][j];
+        __syncthreads();
+        const int rows = min(t.rows - m * 16, 16);
+        for (int e = tid; e < rows * p.R; e += 64 * kWaves) {
+            const int row = e / p.R, r = e - row * p.R;
+            const float* const v = sums + row * kSumRow + r;
+            // a row of x that is not finite times the rank's missing rows of A is nothing all the same
+            out[m * 16 * p.R + e] = r < t.rank ? (v[0] + v[16 * kSumRow]) + (v[32 * kSumRow] + v[48 * kSumRow]) : 0.f;
+        }
     }
 }
 
@@ -277,34 +299,37 @@ __device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, i
 // strip's rows of the pool [adapter][N][R] are in LDS for all waves.  The MFMA's rows are columns of y and its columns
 // rows of y, so a lane ends up with four values in a row of 16 rows; they turn around in the wave's own part of LDS, so
 // that base and y are read and written in rows of 256 bytes (a copy of 9216 x 9216 bf16 values runs at 4.8 TB/s so, at
-// 4.2 in 16 rows of 64 bytes).  The next strip's loads are on their way while this one is multiplied.
-template <typename T, int RC>
+// 4.2 in 16 rows of 64 bytes).  The next strip's loads are on their way while this one is multiplied, and go out ahead of
+// this one's stores, since loads and stores are waited for in the order of their issue.
+template <typename T, int RC, bool BASE>
 __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) {
     constexpr int kParts = Wide<T>::kParts, kValues = Wide<T>::kValues, kStrip = 16 * kValues;
     constexpr int kPieces = kStrip * RC * 4 / (64 * kWaves);  // of 16 bytes of the pool to a thread
     constexpr int kRow = kStrip + 4;
+    constexpr int kZero = kStrip * (RC * 4 + 1);              // the last piece is zero
     __shared__ __align__(16) float turn[kWaves * 16 * kRow];
-    __shared__ u32x4 pool_lds[kStrip * (RC * 4 + 1) + 1];  // the last piece is zero
+    __shared__ u32x4 pool_lds[kZero + 1];
     const LoraTile t = p.tiles[blockIdx.x];
     if (t.rank == 0 && p.base == p.y && p.ldb == p.ldy && !p.sum) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
     const int first = wave * 16;
-    const bool busy = first < t.rows;
     const int pieces = p.R / 8, stride = pieces | 1;  // of a pool row, in memory and, on all banks, in LDS
     const uint16_t* const pool = p.pool + (int64_t)max(t.adapter, 0) * p.N * p.R;
     int64_t n0 = (int64_t)blockIdx.y * p.columns;
     const int64_t end = min((int64_t)(blockIdx.y + 1) * p.columns, p.N);
+    const int64_t last = n0 + (end - n0) / kStrip * kStrip - kStrip;  // the last whole strip (below n0: there is none)
 
-    // of this thread: its rows of y 16 wave + q + 4 j and columns there, its pieces of the pool
+    // of this thread: rows 16 wave + q + 4 j of the tile (its last one again beyond its rows), 16 bytes of their columns
     const int col = i * kValues;
     const T* base[kTimes];
     T* y[kTimes];
 #pragma unroll
     for (int j = 0; j < kTimes; ++j) {
         const int64_t row = (int64_t)t.row + min(first + q + 4 * j, t.rows - 1);
-        base[j] = p.base ? (const T*)p.base + row * p.ldb + col : nullptr;
+        if (BASE) base[j] = (const T*)p.base + row * p.ldb + col;
         y[j] = (T*)p.y + row * p.ldy + col;
     }
+    // and pieces of the strip's pool rows, which lie one behind the other in memory
     int slot[kPieces];
 #pragma unroll
     for (int j = 0; j < kPieces; ++j) {
@@ -314,31 +339,26 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
     Wide<T> wide[kTimes];
     u32x4 piece[kPieces];
     auto load_wide = [&](int64_t n) __attribute__((always_inline)) {
-        if (!p.base) {
 #pragma unroll
-            for (int j = 0; j < kTimes; ++j) wide[j].clear();
-        } else if (n + kStrip <= p.N) {
-#pragma unroll
-            for (int j = 0; j < kTimes; ++j) wide[j].load(base[j] + n);
-        } else {
-#pragma unroll
-            for (int j = 0; j < kTimes; ++j)
-                if (wide[j].clear(); n + col < p.N) wide[j].load(base[j] + n, p.N - n - col);
+        for (int j = 0; j < kTimes; ++j) {
+            if (BASE)
+                wide[j].load(base[j] + n);
+            else
+                wide[j].clear();
         }
     };
     auto load_pool = [&](int64_t n) __attribute__((always_inline)) {
-        const int64_t last = (p.N - n) * pieces - 1;
+        const int64_t most = (p.N - n) * pieces - 1;
 #pragma unroll
         for (int j = 0; j < kPieces; ++j)
-            piece[j] = *(const u32x4*)(pool + n * p.R + min((int64_t)(slot[j] < 0 ? 0 : tid + 64 * kWaves * j), last) * 8);
+            piece[j] = *(const u32x4*)(pool + n * p.R + min((int64_t)(slot[j] < 0 ? 0 : tid + 64 * kWaves * j), most) * 8);
     };
-    if (busy) load_wide(n0);
+    if (last >= n0) load_wide(n0);
     if (t.rank > 0) load_pool(n0);
     u32x4 h[RC][kParts];
-    if (busy) load_h<RC, kParts>(p, t, first, blockIdx.y == 0, i, q, h);
+    load_h<RC, kParts>(p, t, first, blockIdx.y == 0, i, q, h);
 
     // where the lane's operand pieces lie: those beyond R are the zero one
-    constexpr int kZero = kStrip * (RC * 4 + 1);
     if (tid == 0) pool_lds[kZero] = (u32x4){0, 0, 0, 0};
     int operand[RC], next[RC];
 #pragma unroll
@@ -348,56 +368,73 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
         next[c] = there ? 16 * stride : 0;
     }
     float* const mine = turn + wave * 16 * kRow;
-    for (; n0 < end; n0 += kStrip) {
+    auto stage = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < kPieces; ++j) {
+            if (t.rank < p.R) {
+                const int left = t.rank - (tid + 64 * kWaves * j) % pieces * 8;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) piece[j][e] &= (2 * e < left ? 0xFFFFu : 0u) | (2 * e + 1 < left ? 0xFFFF0000u : 0u);
+            }
+            if (slot[j] >= 0) pool_lds[slot[j]] = piece[j];
+        }
+        __syncthreads();
+    };
+    auto add = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int f = 0; f < kValues; ++f) {
+            f32x4 acc = {0, 0, 0, 0};
+#pragma unroll
+            for (int c = 0; c < RC; ++c) {
+                const u32x4 b = pool_lds[operand[c] + f * next[c]];
+#pragma unroll
+                for (int k = kParts - 1; k >= 0; --k) acc = mfma(b, h[c][k], acc);
+            }
+            *(f32x4*)(mine + i * kRow + 16 * f + 4 * q) = acc;
+        }
+        // the wave's own rows of LDS: its accesses stay in order, and the compiler keeps them so
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < kTimes; ++j) wide[j].add(mine + (q + 4 * j) * kRow + col);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    };
+    // a whole tile's strips have no test between their loads and stores, after which the compiler would wait for all
+    auto strips = [&](auto whole) __attribute__((always_inline)) {
+        for (; n0 <= last; n0 += kStrip) {
+            const int64_t then = min(n0 + kStrip, last);
+            if (t.rank > 0) {
+                stage();
+                load_pool(n0 < last ? then : min(n0 + kStrip, p.N - 1));
+                add();
+            }
+            Wide<T> out[kTimes];
+#pragma unroll
+            for (int j = 0; j < kTimes; ++j) out[j] = wide[j];
+            load_wide(then);
+#pragma unroll
+            for (int j = 0; j < kTimes; ++j)
+                if (whole.value || first + q + 4 * j < t.rows) out[j].store(y[j] + n0);
+            if (t.rank > 0) __syncthreads();
+        }
+    };
+    if (t.rows == kLoraTileRows)
+        strips(std::true_type{});
+    else
+        strips(std::false_type{});
+    if (n0 < end) {
+        // the last columns; their part of the pool is here or on its way
+#pragma unroll
+        for (int j = 0; j < kTimes; ++j)
+            if (wide[j].clear(); BASE && n0 + col < p.N) wide[j].load(base[j] + n0, p.N - n0 - col);
         if (t.rank > 0) {
-#pragma unroll
-            for (int j = 0; j < kPieces; ++j) {
-                if (t.rank < p.R) {
-                    const int left = t.rank - (tid + 64 * kWaves * j) % pieces * 8;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) piece[j][e] &= (2 * e < left ? 0xFFFFu : 0u) | (2 * e + 1 < left ? 0xFFFF0000u : 0u);
-                }
-                if (slot[j] >= 0) pool_lds[slot[j]] = piece[j];
-            }
-            __syncthreads();
-            if (n0 + kStrip < end) load_pool(n0 + kStrip);
-            if (busy) {
-                f32x4 acc[kValues];
-#pragma unroll
-                for (int f = 0; f < kValues; ++f) {
-                    acc[f] = (f32x4){0, 0, 0, 0};
-#pragma unroll
-                    for (int c = 0; c < RC; ++c) {
-                        const u32x4 b = pool_lds[operand[c] + f * next[c]];
-#pragma unroll
-                        for (int k = kParts - 1; k >= 0; --k) acc[f] = mfma(b, h[c][k], acc[f]);
-                    }
-                }
-#pragma unroll
-                for (int f = 0; f < kValues; ++f) *(f32x4*)(mine + i * kRow + 16 * f + 4 * q) = acc[f];
-                // the wave's own rows of LDS: its accesses stay in order, and the compiler keeps them so
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-#pragma unroll
-                for (int j = 0; j < kTimes; ++j) wide[j].add(mine + (q + 4 * j) * kRow + col);
-                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-                __builtin_amdgcn_wave_barrier();
-            }
+            stage();
+            add();
         }
-        if (busy) {
-            const bool whole = n0 + kStrip <= p.N;
 #pragma unroll
-            for (int j = 0; j < kTimes; ++j) {
-                if (first + q + 4 * j < t.rows) {
-                    if (whole)
-                        wide[j].store(y[j] + n0);
-                    else if (n0 + col < p.N)
-                        wide[j].store(y[j] + n0, p.N - n0 - col);
-                }
-            }
-            if (n0 + kStrip < end) load_wide(n0 + kStrip);
-        }
-        if (t.rank > 0) __syncthreads();
+        for (int j = 0; j < kTimes; ++j)
+            if (first + q + 4 * j < t.rows && n0 + col < p.N) wide[j].store(y[j] + n0, p.N - n0 - col);
     }
 }
 
@@ -540,7 +577,7 @@ __global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
 // 8 rows of 8 columns, which transposed are 8 operands with the rows as contraction, each for columns 8 apart.
 template <int RF>
 __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
-    __shared__ float part[RF * 16][128 + 4];
+    __shared__ float sums[RF * 16][128 + 4];
     const uint32_t index = blockIdx.x / (uint32_t)p.chunks;
     const int at_chunk = (int)(blockIdx.x - index * (uint32_t)p.chunks);
     const LoraSplit split = p.list[index];
@@ -558,45 +595,65 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[r][j] = (f32x4){0, 0, 0, 0};
     const bool wide_whole = side.width - (int64_t)chunk * 128 >= 128;
-    for (int step = 2 * split.begin + wave; step < 2 * split.end; step += kWaves) {
-        const LoraTile t = p.tiles[step / 2];
-        const int first = (step & 1) * 32;
-        if (first >= t.rows) continue;
-        const int mine = first + kg * 8;  // this lane's first row of the tile
-        u32x4 z[8], part[RF][3];
+    u32x4 z[8], part[RF][3];
+    LoraTile t;
+    int mine;  // the lane's first row of the tile
+    auto load = [&](int step, auto whole) __attribute__((always_inline)) {
+        t = p.tiles[step / 2];
+        mine = (step & 1) * 32 + kg * 8;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint16_t* const from = side.wide + ((int64_t)t.row + min(mine + j, t.rows - 1)) * side.ld + col;
+            z[j] = whole.value ? load8(from) : load8_part(from, left);
+        }
 #pragma unroll
         for (int r = 0; r < RF; ++r) {
             const int frag = min(r0 / 16 + r, (p.R - 1) / 16);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) part[r][k] = *(const u32x4*)(side.narrow + lora_operand(step / 2, first, k, frag * 16, p.R) + lane * 8);
+            for (int k = 0; k < 3; ++k) part[r][k] = *(const u32x4*)(side.narrow + lora_operand(step / 2, (step & 1) * 32, k, frag * 16, p.R) + lane * 8);
         }
-        if (wide_whole && first + 32 <= t.rows) {
-            const uint16_t* const from = side.wide + ((int64_t)t.row + mine) * side.ld + col;
+    };
+    auto steps = [&](auto whole) __attribute__((always_inline)) {
+        const int end = 2 * split.end;
+        int step = 2 * split.begin + wave;
+        if (step >= end) return;
+        load(step, whole);
+        for (; step < end; step += kWaves) {
+            u32x4 cols[8], rows[RF][3];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) z[j] = load8(from + j * side.ld);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                z[j] = (u32x4){0, 0, 0, 0};
-                if (mine + j < t.rows) z[j] = load8_part(side.wide + ((int64_t)t.row + mine + j) * side.ld + col, left);
-            }
-            // rows beyond the tile are another's, or none
+            for (int j = 0; j < 8; ++j) cols[j] = z[j];
 #pragma unroll
             for (int r = 0; r < RF; ++r)
 #pragma unroll
-                for (int k = 0; k < 3; ++k)
+                for (int k = 0; k < 3; ++k) rows[r][k] = part[r][k];
+            const int mine_now = mine, rows_now = t.rows;
+            load(min(step + kWaves, end - 1), whole);
+            if ((step & 1) * 32 + 32 > rows_now) {
+                // rows beyond the tile are another's, or none
 #pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        part[r][k][j] &= (mine + 2 * j < t.rows ? 0xFFFFu : 0u) | (mine + 2 * j + 1 < t.rows ? 0xFFFF0000u : 0u);
+                for (int j = 0; j < 8; ++j)
+                    if (mine_now + j >= rows_now) cols[j] = (u32x4){0, 0, 0, 0};
+#pragma unroll
+                for (int r = 0; r < RF; ++r)
+#pragma unroll
+                    for (int k = 0; k < 3; ++k)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j)
+                            rows[r][k][j] &= (mine_now + 2 * j < rows_now ? 0xFFFFu : 0u) | (mine_now + 2 * j + 1 < rows_now ? 0xFFFF0000u : 0u);
+            }
+            transpose8(cols);
+#pragma unroll
+            for (int r = 0; r < RF; ++r)
+#pragma unroll
+                for (int k = 2; k >= 0; --k)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) acc[r][j] = mfma(rows[r][k], cols[j], acc[r][j]);
         }
-        transpose8(z);
-#pragma unroll
-        for (int r = 0; r < RF; ++r)
-#pragma unroll
-            for (int k = 2; k >= 0; --k)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) acc[r][j] = mfma(part[r][k], z[j], acc[r][j]);
-    }
+    };
+    if (wide_whole)
+        steps(std::true_type{});
+    else
+        steps(std::false_type{});
     // the waves' sums, in order
     for (int w = 0; w < kWaves; ++w) {
         if (wave == w) {
@@ -606,7 +663,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
                 for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int j = 0; j < 8; ++j) {
-                        float& to = part[r * 16 + kg * 4 + k][c * 8 + j];
+                        float& to = sums[r * 16 + kg * 4 + k][c * 8 + j];
                         to = w ? to + acc[r][j][k] : acc[r][j][k];
                     }
         }
@@ -615,7 +672,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
     float* const out = side.part + ((int64_t)index * p.R + r0) * side.width;
     for (int e = threadIdx.x; e < RF * 16 * 128; e += 64 * kWaves) {
         const int r = e >> 7, n = e & 127;
-        if (r0 + r < p.R && (int64_t)chunk * 128 + n < side.width) out[r * side.width + (int64_t)chunk * 128 + n] = part[r][n];
+        if (r0 + r < p.R && (int64_t)chunk * 128 + n < side.width) out[r * side.width + (int64_t)chunk * 128 + n] = sums[r][n];
     }
 }
 
@@ -646,14 +703,24 @@ __global__ __launch_bounds__(256) void lora_grad_sum_kernel(LoraGrad p) {
     }
 }
 
+template <typename T, int RC>
+void expand(const LoraExpand& p, dim3 grid, bool few, hipStream_t stream) {
+    if (few)
+        lora_expand_few_kernel<T, RC><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else if (p.base)
+        lora_expand_kernel<T, RC, true><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else
+        lora_expand_kernel<T, RC, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+}
+
 template <typename T>
 void expand(const LoraExpand& p, dim3 grid, bool few, hipStream_t stream) {
     if (p.R <= 32)
-        few ? lora_expand_few_kernel<T, 1><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 1><<<grid, 64 * kWaves, 0, stream>>>(p);
+        expand<T, 1>(p, grid, few, stream);
     else if (p.R <= 64)
-        few ? lora_expand_few_kernel<T, 2><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 2><<<grid, 64 * kWaves, 0, stream>>>(p);
+        expand<T, 2>(p, grid, few, stream);
     else
-        few ? lora_expand_few_kernel<T, 4><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 4><<<grid, 64 * kWaves, 0, stream>>>(p);
+        expand<T, 4>(p, grid, few, stream);
 }
 
 }  // namespace
