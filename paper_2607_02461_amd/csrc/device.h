@@ -231,7 +231,22 @@ struct LoraExpand {
     void* y;               // [M][ldy] fp32 or bf16
     int64_t ldy;
     uint16_t* turned;      // s h as three bf16 parts for the gradients (lora_operand_bytes), or null
-    int columns;           // to a workgroup, a multiple of 512 (set by the launcher)
+    int columns;           // to a workgroup, a multiple of 128 (set by the launcher)
+};
+
+constexpr int kLoraFewRows = 4;  // of the largest tile for which both products run in one kernel
+
+struct LoraRows {
+    const LoraTile* tiles;   // of at most kLoraFewRows rows
+    const uint16_t *x, *a, *b;  // bf16 [M][ldx], [adapter][R][K], [adapter][N][R]
+    int64_t ldx, K, N;
+    int R;
+    const void* base;        // as for LoraExpand
+    int64_t ldb;
+    void* y;
+    int64_t ldy;
+    float* h;                // fp32 [M][R], x A^T, or null
+    int columns;             // to a workgroup (set by the launcher)
 };
 
 struct LoraTurn {
@@ -269,6 +284,7 @@ hipError_t launch_lora_shrink(LoraShrink p, int tiles, int splits, hipStream_t s
 // Bytes of one narrow matrix in three bf16 parts, in the order of the gradients' operands: tiles of 64 rows.
 inline int64_t lora_operand_bytes(int64_t tiles, int R) { return tiles * kLoraTileRows * ((R + 15) / 16 * 16) * 3 * 2; }
 hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream);
+hipError_t launch_lora_rows(LoraRows p, int tiles, int tile_rows, bool f32, int cus, hipStream_t stream);
 hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream);
 hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, hipStream_t stream);
 

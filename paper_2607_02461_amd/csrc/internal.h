@@ -76,6 +76,7 @@ struct orbit_lora_s {
     int64_t rows = 0;
     int32_t adapters = 0, max_rank = 0;
     int64_t tiles = 0;
+    int32_t tile_rows = 0;  // of the largest tile
     std::vector<unsigned char> lists;
     size_t at_splits[kLoraLevels] = {}, at_first[kLoraLevels] = {};  // byte offsets; the tiles are at 0
     int64_t splits[kLoraLevels] = {};

@@ -438,76 +438,135 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
     }
 }
 
-// The same for tiles of few rows, which are bound by latency and by the pool: every wave has the tile's 16 rows (or every
-// second one the first, where it has more) and strips of its own, and takes the pool's rows straight from memory.
-template <typename T, int RC>
-__global__ __launch_bounds__(64 * kWaves) void lora_expand_few_kernel(LoraExpand p) {
-    constexpr int kParts = Wide<T>::kParts, kValues = Wide<T>::kValues, kStrip = 16 * kValues, kRow = kStrip + 4;
-    __shared__ __align__(16) float turn[kWaves * 16 * kRow];
+// Both products in one kernel for tiles of at most ROWS rows, the single tokens of many requests: bound by launches and
+// latency, and by the pools, which every workgroup streams in rows of 1 KB.  A workgroup takes a tile and p.columns
+// columns; its waves make h for themselves (A comes from L2 for all but the first), each for R / 8 rows of A, in fp32
+// with the lanes along K; then 2^k >= R / 8 lanes share a row of B.
+constexpr int kRowWaves = 8, kAhead = 4;  // waves to a workgroup, and groups of rows of B that a wave has on their way
+
+template <int LANES>
+__device__ __forceinline__ float sum_lanes(float v) {
+#pragma unroll
+    for (int apart = 1; apart < LANES; apart *= 2) v += __shfl_xor(v, apart);
+    return v;
+}
+
+__device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, a), __builtin_bit_cast(bf16x2_t, b), c, false);
+}
+
+template <typename T>
+__device__ __forceinline__ float wide_value(const T* p);
+template <>
+__device__ __forceinline__ float wide_value<bf16_t>(const bf16_t* p) { return bf16_low(p->bits); }
+template <>
+__device__ __forceinline__ float wide_value<float>(const float* p) { return *p; }
+__device__ __forceinline__ void set_wide(bf16_t* p, float v) { p->bits = (uint16_t)pack_bf16(v, v); }
+__device__ __forceinline__ void set_wide(float* p, float v) { *p = v; }
+
+template <typename T, int RPW, int ROWS>
+__global__ __launch_bounds__(64 * kRowWaves) void lora_rows_kernel(LoraRows p) {
+    constexpr int kLanes = RPW, kGroups = 64 / kLanes;  // lanes to a row of B: 8 values of r each
+    __shared__ float hs[ROWS][RPW * kRowWaves];
     const LoraTile t = p.tiles[blockIdx.x];
-    if (t.rank == 0 && p.base == p.y && p.ldb == p.ldy && !p.sum) return;
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, q = lane >> 4;
-    const int shift = t.rows > 32 ? 2 : t.rows > 16 ? 1 : 0;  // log2 of the row groups
-    const int first = (wave & ((1 << shift) - 1)) * 16, beside = wave >> shift, step = (kWaves >> shift) * kStrip;
-    if (first >= t.rows) return;
-    const uint16_t* const pool = p.pool + (int64_t)max(t.adapter, 0) * p.N * p.R;
-    int64_t n0 = (int64_t)blockIdx.y * p.columns + beside * kStrip;
+    if (t.rank == 0 && p.base == p.y && p.ldb == p.ldy && !p.h) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t adapter = max(t.adapter, 0);
+
+    const int sub = lane & (kLanes - 1), group = lane / kLanes;
+    const uint16_t* const b = p.b + adapter * p.N * p.R + min(sub * 8, p.R - 8);
     const int64_t end = min((int64_t)(blockIdx.y + 1) * p.columns, p.N);
-    const int col = i * kValues;
-    Wide<T> wide[kTimes];
-    u32x4 b[kValues][RC], mask[RC], h[RC][kParts];
+    int64_t n0 = (int64_t)blockIdx.y * p.columns + wave * kAhead * kGroups;
+    u32x4 bv[kAhead];
+    float wide[kAhead][ROWS];
     auto load = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < kTimes; ++j) {
-            wide[j].clear();
-            if (p.base && n0 + col < p.N && first + q + 4 * j < t.rows)
-                wide[j].load((const T*)p.base + ((int64_t)t.row + first + q + 4 * j) * p.ldb + n0 + col, p.N - n0 - col);
-        }
-        if (t.rank > 0) {
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t n = min(n0 + u * kGroups + group, p.N - 1);
+            bv[u] = *(const u32x4*)(b + n * p.R);
 #pragma unroll
-            for (int f = 0; f < kValues; ++f)
-#pragma unroll
-                for (int c = 0; c < RC; ++c) {
-                    const int r = c * 32 + q * 8;
-                    b[f][c] = *(const u32x4*)(pool + min(n0 + 16 * f + i, p.N - 1) * p.R + (r < p.R ? r : 0));
-                }
+            for (int m = 0; m < ROWS; ++m) wide[u][m] = p.base ? wide_value((const T*)p.base + (t.row + min(m, t.rows - 1)) * p.ldb + n) : 0.f;
         }
     };
-    if (n0 < end) load();
-    load_h<RC, kParts>(p, t, first, blockIdx.y == 0 && beside == 0, i, q, h);
+    load();
+
+    float acc[RPW][ROWS];
 #pragma unroll
-    for (int c = 0; c < RC; ++c)
+    for (int r = 0; r < RPW; ++r)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int r = c * 32 + q * 8 + 2 * j;
-            mask[c][j] = (r < t.rank ? 0xFFFFu : 0u) | (r + 1 < t.rank ? 0xFFFF0000u : 0u);
-        }
-    float* const mine = turn + wave * 16 * kRow;
-    while (n0 < end) {
-        if (t.rank > 0) {
-            f32x4 acc[kValues];
+        for (int m = 0; m < ROWS; ++m) acc[r][m] = 0.f;
+    if (t.rank > 0) {
+        constexpr int kBatch = RPW + ROWS <= 5 ? 3 : RPW + ROWS <= 12 ? 2 : 1;  // chunks of 512 whose loads go out together
+        const uint16_t* x[ROWS];
+        const uint16_t* a[RPW];
 #pragma unroll
-            for (int f = 0; f < kValues; ++f) {
-                acc[f] = (f32x4){0, 0, 0, 0};
+        for (int m = 0; m < ROWS; ++m) x[m] = p.x + (t.row + min(m, t.rows - 1)) * p.ldx;
 #pragma unroll
-                for (int c = 0; c < RC; ++c)
+        for (int r = 0; r < RPW; ++r) a[r] = p.a + (adapter * p.R + min(wave * RPW + r, t.rank - 1)) * p.K;
+        for (int64_t k0 = 0; k0 < p.K; k0 += 512 * kBatch) {
+            u32x4 xv[kBatch][ROWS], av[kBatch][RPW];
 #pragma unroll
-                    for (int k = kParts - 1; k >= 0; --k) acc[f] = mfma(b[f][c] & mask[c], h[c][k], acc[f]);
+            for (int d = 0; d < kBatch; ++d) {
+                const int64_t k = min(k0 + d * 512 + lane * 8, p.K - 8);
+#pragma unroll
+                for (int m = 0; m < ROWS; ++m) xv[d][m] = load8(x[m] + k);
+#pragma unroll
+                for (int r = 0; r < RPW; ++r) av[d][r] = *(const u32x4*)(a[r] + k);
             }
 #pragma unroll
-            for (int f = 0; f < kValues; ++f) *(f32x4*)(mine + i * kRow + 16 * f + 4 * q) = acc[f];
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+            for (int d = 0; d < kBatch; ++d) {
+                const bool there = k0 + d * 512 + lane * 8 < p.K;
 #pragma unroll
-            for (int j = 0; j < kTimes; ++j) wide[j].add(mine + (q + 4 * j) * kRow + col);
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-            __builtin_amdgcn_wave_barrier();
+                for (int r = 0; r < RPW; ++r)
+#pragma unroll
+                    for (int m = 0; m < ROWS; ++m) {
+                        float v = acc[r][m];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) v = dot2(av[d][r][e], xv[d][m][e], v);
+                        acc[r][m] = there ? v : acc[r][m];
+                    }
+            }
         }
 #pragma unroll
-        for (int j = 0; j < kTimes; ++j)
-            if (n0 + col < p.N && first + q + 4 * j < t.rows)
-                wide[j].store((T*)p.y + ((int64_t)t.row + first + q + 4 * j) * p.ldy + n0 + col, p.N - n0 - col);
-        n0 += step;
+        for (int r = 0; r < RPW; ++r)
+#pragma unroll
+            for (int m = 0; m < ROWS; ++m) acc[r][m] = wave * RPW + r < t.rank ? sum_lanes<64>(acc[r][m]) : 0.f;
+    }
+#pragma unroll
+    for (int r = 0; r < RPW; ++r)
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m)
+            if (lane == 0) hs[m][wave * RPW + r] = acc[r][m];
+    __syncthreads();
+    if (p.h && blockIdx.y == 0)
+        for (int e = threadIdx.x; e < t.rows * p.R; e += 64 * kRowWaves) p.h[(int64_t)t.row * p.R + e] = hs[e / p.R][e % p.R];
+    float h[ROWS][8];
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) h[m][j] = sub * 8 + j < t.rank ? hs[m][sub * 8 + j] * t.scale : 0.f;
+
+    while (n0 < end) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int64_t n = n0 + u * kGroups + group;
+            float v[ROWS];
+#pragma unroll
+            for (int m = 0; m < ROWS; ++m) v[m] = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                // what lies beyond the rank need not be a number
+                const float w = sub * 8 + j < t.rank ? (j & 1 ? bf16_high(bv[u][j / 2]) : bf16_low(bv[u][j / 2])) : 0.f;
+#pragma unroll
+                for (int m = 0; m < ROWS; ++m) v[m] += w * h[m][j];
+            }
+#pragma unroll
+            for (int m = 0; m < ROWS; ++m) {
+                const float y = wide[u][m] + sum_lanes<kLanes>(v[m]);
+                if (sub == 0 && n < end && m < t.rows) set_wide((T*)p.y + (t.row + m) * p.ldy + n, y);
+            }
+        }
+        n0 += kRowWaves * kAhead * kGroups;
         if (n0 < end) load();
     }
 }
@@ -703,24 +762,28 @@ __global__ __launch_bounds__(256) void lora_grad_sum_kernel(LoraGrad p) {
     }
 }
 
-template <typename T, int RC>
-void expand(const LoraExpand& p, dim3 grid, bool few, hipStream_t stream) {
-    if (few)
-        lora_expand_few_kernel<T, RC><<<grid, 64 * kWaves, 0, stream>>>(p);
-    else if (p.base)
-        lora_expand_kernel<T, RC, true><<<grid, 64 * kWaves, 0, stream>>>(p);
+template <typename T>
+void expand(const LoraExpand& p, dim3 grid, hipStream_t stream) {
+    if (p.R <= 32)
+        p.base ? lora_expand_kernel<T, 1, true><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 1, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+    else if (p.R <= 64)
+        p.base ? lora_expand_kernel<T, 2, true><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 2, false><<<grid, 64 * kWaves, 0, stream>>>(p);
     else
-        lora_expand_kernel<T, RC, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+        p.base ? lora_expand_kernel<T, 4, true><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_expand_kernel<T, 4, false><<<grid, 64 * kWaves, 0, stream>>>(p);
 }
 
-template <typename T>
-void expand(const LoraExpand& p, dim3 grid, bool few, hipStream_t stream) {
-    if (p.R <= 32)
-        expand<T, 1>(p, grid, few, stream);
+template <typename T, int ROWS>
+void rows(const LoraRows& p, dim3 grid, hipStream_t stream) {
+    if (p.R <= 8)
+        lora_rows_kernel<T, 1, ROWS><<<grid, 64 * kRowWaves, 0, stream>>>(p);
+    else if (p.R <= 16)
+        lora_rows_kernel<T, 2, ROWS><<<grid, 64 * kRowWaves, 0, stream>>>(p);
+    else if (p.R <= 32)
+        lora_rows_kernel<T, 4, ROWS><<<grid, 64 * kRowWaves, 0, stream>>>(p);
     else if (p.R <= 64)
-        expand<T, 2>(p, grid, few, stream);
+        lora_rows_kernel<T, 8, ROWS><<<grid, 64 * kRowWaves, 0, stream>>>(p);
     else
-        expand<T, 4>(p, grid, few, stream);
+        lora_rows_kernel<T, 16, ROWS><<<grid, 64 * kRowWaves, 0, stream>>>(p);
 }
 
 }  // namespace
@@ -748,12 +811,26 @@ hipError_t launch_lora_shrink(LoraShrink p, int tiles, int splits, hipStream_t s
 }
 
 hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream) {
-    // 1024 columns to a workgroup, fewer where that leaves less than 8 workgroups to a compute unit
+    // 1024 columns to a workgroup, fewer where that leaves less than 4 workgroups to a compute unit
     p.columns = 1024;
-    while (p.columns > 512 && tiles * ((p.N + p.columns - 1) / p.columns) < 8 * (int64_t)cus) p.columns /= 2;
+    while (p.columns > 128 && tiles * ((p.N + p.columns - 1) / p.columns) < 4 * (int64_t)cus) p.columns /= 2;
     const dim3 grid(tiles, (unsigned)((p.N + p.columns - 1) / p.columns));
-    const bool few = p.M < 24 * (int64_t)tiles;
-    f32 ? expand<float>(p, grid, few, stream) : expand<bf16_t>(p, grid, few, stream);
+    f32 ? expand<float>(p, grid, stream) : expand<bf16_t>(p, grid, stream);
+    return hipGetLastError();
+}
+
+hipError_t launch_lora_rows(LoraRows p, int tiles, int tile_rows, bool f32, int cus, hipStream_t stream) {
+    // a workgroup to a compute unit, but no fewer columns than its waves take at once
+    int lanes = 1;
+    while (lanes * 8 < p.R) lanes *= 2;
+    const int64_t once = kRowWaves * kAhead * (64 / lanes), most = (p.N + once - 1) / once;
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(most, (cus + tiles - 1) / tiles));
+    p.columns = (int)((most + blocks - 1) / blocks * once);
+    const dim3 grid(tiles, (unsigned)((p.N + p.columns - 1) / p.columns));
+    if (tile_rows <= 1)
+        f32 ? rows<float, 1>(p, grid, stream) : rows<bf16_t, 1>(p, grid, stream);
+    else
+        f32 ? rows<float, kLoraFewRows>(p, grid, stream) : rows<bf16_t, kLoraFewRows>(p, grid, stream);
     return hipGetLastError();
 }
 

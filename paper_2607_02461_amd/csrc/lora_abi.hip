@@ -42,6 +42,7 @@ void fill(orbit_lora p, int64_t segments, const int64_t* starts, const int32_t* 
             t.rank = none ? 0 : ranks[a];
             t.scale = none ? 0.f : scales[a];
             of[none ? n : a].push_back(t);
+            p->tile_rows = std::max(p->tile_rows, t.rows);
         }
     };
     if (segments == 0 || starts[0] > 0) add(0, segments ? starts[0] : p->rows, -1);
@@ -86,6 +87,7 @@ struct Layout {
 
 Layout forward_layout(orbit_lora p, int64_t K, int R, int cus, bool h_given) {
     Layout l;
+    if (p->tile_rows <= kLoraFewRows) return l;
     l.splits = lora_splits((int)p->tiles, K, cus);
     if (l.splits > 1 || !h_given) l.bytes = padded(l.splits * p->rows * R * (int64_t)sizeof(float));
     return l;
@@ -245,6 +247,24 @@ orbit_status lora_add(orbit_lora p, const uint16_t* X, int64_t ldx, const uint16
     const Layout l = forward_layout(p, K, R, info.cus, h != nullptr);
     if (l.bytes && (!workspace || !aligned(workspace, 16) || workspace_bytes < l.bytes))
         return fail(ORBIT_EINVAL, "%s: takes a workspace of %zu bytes, aligned to 16", who, l.bytes);
+    if (p->tile_rows <= kLoraFewRows) {
+        LoraRows r{};
+        r.tiles = (const LoraTile*)lists;
+        r.x = X;
+        r.a = A;
+        r.b = B;
+        r.ldx = ldx;
+        r.K = K;
+        r.N = N;
+        r.R = R;
+        r.base = base;
+        r.ldb = ldb;
+        r.y = Y;
+        r.ldy = ldy;
+        r.h = h;
+        const hipError_t e = launch_lora_rows(r, (int)p->tiles, p->tile_rows, dtype == ORBIT_OUT_F32, info.cus, (hipStream_t)stream);
+        return e == hipSuccess ? ORBIT_OK : hip_fail(e, who);
+    }
     LoraShrink s{};
     s.tiles = (const LoraTile*)lists;
     s.x = X;
