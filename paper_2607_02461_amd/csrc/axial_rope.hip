@@ -45,39 +45,55 @@ __device__ __forceinline__ float group_sum(float v, int lanes) {
     return v;
 }
 
-// A lane's eight values: two fours in a row, or pairs' first halves and their second halves.
-template <typename T, bool HALVES>
-struct Row8 {
-    Vec8<T> v;
-    __device__ __forceinline__ void load(const T* p, int, int) { v.load(p); }
-    __device__ __forceinline__ void get(float* f) const { v.get(f); }
-    static __device__ __forceinline__ void store(T* p, int, int, const float* f) { Vec8<T>::store(p, f); }
-};
+// How a head's values lie in its lanes, eight to a lane, so that a load or store of the wave is whole lines: eight in a
+// row of bf16 (kRow), or two fours, of pairs' first halves and their second ones (kHalves), or of the head's first half
+// and its second one where values of 4 bytes are read or written (kApart).
+enum { kRow, kHalves, kApart };
 
-template <typename T>
-struct Row8<T, true> {
-    Vec4<T> a, b;
+template <typename T, int LAY, bool NT>
+struct Row8 {
+    Vec4<T, NT> a, b;
     __device__ __forceinline__ void load(const T* p, int lo, int hi) { a.load(p + lo), b.load(p + hi); }
     __device__ __forceinline__ void get(float* f) const { a.get(f), b.get(f + 4); }
     static __device__ __forceinline__ void store(T* p, int lo, int hi, const float* f) {
-        Vec4<T>::store(p + lo, f);
-        Vec4<T>::store(p + hi, f + 4);
+        Vec4<T, NT>::store(p + lo, f);
+        Vec4<T, NT>::store(p + hi, f + 4);
     }
 };
 
-// What a lane does in every row: chunk c of a head, and where its eight values lie in the row.
-template <bool HALVES>
+template <bool NT>
+struct Row8<bf16_t, kRow, NT> {
+    Vec8<NT> v;
+    __device__ __forceinline__ void load(const bf16_t* p, int lo, int) { v.load(p + lo); }
+    __device__ __forceinline__ void get(float* f) const { v.get(f); }
+    static __device__ __forceinline__ void store(bf16_t* p, int lo, int, const float* f) { Vec8<NT>::store(p + lo, f); }
+};
+
+// What a lane does in every row: where its two fours of values begin, and the first of its four pairs, or of the two
+// pairs of either four.
+template <int LAY>
 struct Lane {
-    int c, lo, hi;
-    bool live, turned;
+    int lo, hi, pair, pair_hi;
+    bool live, turned, turned_hi;
     __device__ __forceinline__ Lane(const RopeParams& p, int lane) {
-        c = lane & (p.lanes - 1);
+        int c = lane & (p.lanes - 1);
         live = c * 8 < p.D;
         if (!live) c = 0;  // loads what lane 0 of the group does, adds nothing to a sum and stores nothing
-        turned = c * 4 < p.pairs;
-        const bool apart = HALVES && turned;
-        lo = apart ? 4 * c : 8 * c;
-        hi = apart ? p.pairs + 4 * c : 8 * c + 4;
+        if (LAY == kApart) {
+            lo = 4 * c, hi = p.D / 2 + 4 * c;
+            pair = 2 * c, pair_hi = p.D / 4 + 2 * c;
+            turned = pair < p.pairs, turned_hi = pair_hi < p.pairs;
+        } else {
+            turned = turned_hi = 4 * c < p.pairs;
+            pair = 4 * c, pair_hi = 4 * c + 2;
+            if (LAY == kHalves) {
+                // what is not turned lies behind the pairs, and in two halves too
+                lo = 4 * c + (turned ? 0 : p.pairs);
+                hi = lo + (turned ? p.pairs : p.D / 2 - p.pairs);
+            } else {
+                lo = 8 * c, hi = 8 * c + 4;
+            }
+        }
     }
 };
 
@@ -89,13 +105,14 @@ __device__ __forceinline__ void load_weights(const RopeTensor& t, int lo, int hi
     }
 }
 
-// Cosines and sines of the lane's four pairs for one token; NaN where a position lies outside its axis's table.
-__device__ __forceinline__ void load_angles(const RopeParams& p, int c, int64_t b, int64_t l, float* cs, float* sn) {
+// Where the lane's four pairs find their cosines and sines for one token; -1 where a position lies outside its axis's
+// table.
+template <int LAY>
+__device__ __forceinline__ void find_angles(const RopeParams& p, const Lane<LAY>& me, int64_t b, int64_t l, int* at) {
     const int32_t* pos = p.pos + b * p.pos_batch + l * p.axes;
-    int at[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int pair = 4 * c + i;
+        const int pair = min((i < 2 ? me.pair : me.pair_hi) + (i & 1), p.pairs - 1);
         int axis = 0, length = p.length[0], base = p.base[0], width = p.width[0];
         for (int a = 1; a < p.axes; ++a) {
             const bool mine = pair >= p.first[a];
@@ -107,19 +124,24 @@ __device__ __forceinline__ void load_angles(const RopeParams& p, int c, int64_t 
         const int where = pos[axis];
         at[i] = (uint32_t)where < (uint32_t)length ? base + where * width + pair : -1;
     }
+}
+
+// Cosines and sines there; NaN at -1.
+__device__ __forceinline__ void load_angles(const RopeParams& p, const int* at, float* cs, float* sn) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const f32x2 v = ((const f32x2*)p.table)[at[i] < 0 ? 0 : at[i]];
+        const f32x2 v = ((const f32x2*)p.table)[max(at[i], 0)];
         cs[i] = at[i] < 0 ? __builtin_nanf("") : v.x;
         sn[i] = at[i] < 0 ? __builtin_nanf("") : v.y;
     }
 }
 
-template <bool HALVES>
-__device__ __forceinline__ void turn(float* v, const float* cs, const float* sn, float sign, bool turned) {
+template <int LAY>
+__device__ __forceinline__ void turn(float* v, const float* cs, const float* sn, float sign, const Lane<LAY>& me) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int j = HALVES ? i : 2 * i, k = HALVES ? i + 4 : 2 * i + 1;
+        const int j = LAY == kHalves ? i : 2 * i, k = LAY == kHalves ? i + 4 : 2 * i + 1;
+        const bool turned = i < 2 ? me.turned : me.turned_hi;
         const float s = sign * sn[i];
         const float a = v[j] * cs[i] - v[k] * s, b = v[j] * s + v[k] * cs[i];
         v[j] = turned ? a : v[j];
@@ -150,22 +172,23 @@ __device__ __forceinline__ T* row_of(const HeadRows& r, const Item& it, int head
     return (T*)r.p + it.b * r.b + it.l * r.l + head * r.h;
 }
 
-template <typename TI, typename TO, bool NORM, bool HALVES>
+template <typename TI, typename TO, bool NORM, int LAY, bool NT>
 __global__ __launch_bounds__(64 * kWaves) void axial_rope_kernel(RopeParams p) {
     const RopeTensor& t = p.t[blockIdx.y];
     const int lane = threadIdx.x & 63;
     const uint32_t item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= t.items) return;
-    const Lane<HALVES> me(p, lane);
+    const Lane<LAY> me(p, lane);
     const Item it(p, t, item, lane);
-    Row8<TI, HALVES> x[kRows];
+    int at[4];
+    if (p.pairs) find_angles(p, me, it.b, it.l, at);
+    Row8<TI, LAY, NT> x[kRows];
 #pragma unroll
     for (int u = 0; u < kRows; ++u)
-        if (u < t.rows)
-            x[u].load(row_of<const TI>(t.x, it, min(it.head + u * t.wave_heads, t.heads - 1)) + (HALVES ? 0 : me.lo), me.lo, me.hi);
+        if (u < t.rows) x[u].load(row_of<const TI>(t.x, it, min(it.head + u * t.wave_heads, t.heads - 1)), me.lo, me.hi);
     float w[8], cs[4], sn[4];
     if (NORM) load_weights(t, me.lo, me.hi, w);
-    if (p.pairs) load_angles(p, me.turned ? me.c : 0, it.b, it.l, cs, sn);
+    if (p.pairs) load_angles(p, at, cs, sn);
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
         if (u >= t.rows) break;
@@ -181,39 +204,40 @@ __global__ __launch_bounds__(64 * kWaves) void axial_rope_kernel(RopeParams p) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= r * w[i];
         }
-        if (p.pairs) turn<HALVES>(v, cs, sn, p.sign, me.turned);
-        if (me.live && it.live && head < t.heads)
-            Row8<TO, HALVES>::store(row_of<TO>(t.y, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi, v);
+        if (p.pairs) turn(v, cs, sn, p.sign, me);
+        if (me.live && it.live && head < t.heads) Row8<TO, LAY, NT>::store(row_of<TO>(t.y, it, head), me.lo, me.hi, v);
     }
 }
 
 // Persistent: the workgroup's sums of the weight's gradient stay in its lanes' registers, eight columns each, until
 // its last row, and leave as one row of partial sums.  They are added in a fixed order, so the result does not
 // depend on which workgroup ends first.
-template <typename TX, typename TG, bool HALVES>
+template <typename TX, typename TG, int LAY, bool NT>
 __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_backward_kernel(RopeParams p) {
     __shared__ float part[kWaves][512];
     const RopeTensor& t = p.t[blockIdx.y];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const Lane<HALVES> me(p, lane);
+    const Lane<LAY> me(p, lane);
     float w[8], dw[8];
     load_weights(t, me.lo, me.hi, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) dw[i] = 0.f;
     for (uint32_t item = blockIdx.x * kWaves + wave; item < t.items; item += gridDim.x * kWaves) {
         const Item it(p, t, item, lane);
-        Row8<TX, HALVES> x[kBackRows];
-        Row8<TG, HALVES> g[kBackRows];
+        int at[4];
+        if (p.pairs) find_angles(p, me, it.b, it.l, at);
+        Row8<TX, LAY, NT> x[kBackRows];
+        Row8<TG, LAY, NT> g[kBackRows];
 #pragma unroll
         for (int u = 0; u < kBackRows; ++u) {
             if (u < t.rows) {
                 const int head = min(it.head + u * t.wave_heads, t.heads - 1);
-                x[u].load(row_of<const TX>(t.x, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi);
-                g[u].load(row_of<const TG>(t.g, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi);
+                x[u].load(row_of<const TX>(t.x, it, head), me.lo, me.hi);
+                g[u].load(row_of<const TG>(t.g, it, head), me.lo, me.hi);
             }
         }
         float cs[4], sn[4];
-        if (p.pairs) load_angles(p, me.turned ? me.c : 0, it.b, it.l, cs, sn);
+        if (p.pairs) load_angles(p, at, cs, sn);
 #pragma unroll
         for (int u = 0; u < kBackRows; ++u) {
             if (u >= t.rows) break;
@@ -222,7 +246,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_backward_kernel(Rope
             float xv[8], gv[8];
             x[u].get(xv);
             g[u].get(gv);
-            if (p.pairs) turn<HALVES>(gv, cs, sn, -1.f, me.turned);
+            if (p.pairs) turn(gv, cs, sn, -1.f, me);
             float sum = 0.f, dot = 0.f;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -239,7 +263,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_backward_kernel(Rope
                 dx[i] = r * (gv[i] * w[i] - xv[i] * m);
                 if (live) dw[i] += gv[i] * (xv[i] * r);
             }
-            if (live) Row8<TX, HALVES>::store(row_of<TX>(t.y, it, head) + (HALVES ? 0 : me.lo), me.lo, me.hi, dx);
+            if (live) Row8<TX, LAY, NT>::store(row_of<TX>(t.y, it, head), me.lo, me.hi, dx);
         }
     }
     if (!t.dw) return;
@@ -294,20 +318,37 @@ void divide(const RopeParams& p, RopeTensor& t, int most, int cus) {
     t.items = (uint32_t)(token_groups * t.chunks);
 }
 
+// Non-temporal loads and stores where a call moves more than the memory-side cache keeps for the next kernel, in pieces
+// of whole lines.  Measured plain / non-temporal, us: 100 MB 18.4 / 20.8, 227 MB 51.7 / 46.2, 340 MB 62.6 / 58, 671 MB
+// 117 / 108; but in pieces of 64 bytes 66.8 / 75.
+bool streams(const RopeParams& p, int bytes_each, int smallest) {
+    int64_t heads = 0;
+    for (int i = 0; i < p.tensors; ++i) heads += p.t[i].heads;
+    return (int64_t)p.tokens * heads * p.D * bytes_each > (int64_t)160 << 20 && (!p.halves || p.pairs * smallest >= 128);
+}
+
 template <typename TI, typename TO, bool NORM>
 void launch(const RopeParams& p, dim3 grid, hipStream_t stream) {
+    constexpr int kPlain = sizeof(TI) + sizeof(TO) == 4 ? kRow : kApart;
+    const bool nt = streams(p, sizeof(TI) + sizeof(TO), std::min(sizeof(TI), sizeof(TO)));
     if (p.halves)
-        axial_rope_kernel<TI, TO, NORM, true><<<grid, 64 * kWaves, 0, stream>>>(p);
+        nt ? axial_rope_kernel<TI, TO, NORM, kHalves, true><<<grid, 64 * kWaves, 0, stream>>>(p)
+           : axial_rope_kernel<TI, TO, NORM, kHalves, false><<<grid, 64 * kWaves, 0, stream>>>(p);
     else
-        axial_rope_kernel<TI, TO, NORM, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+        nt ? axial_rope_kernel<TI, TO, NORM, kPlain, true><<<grid, 64 * kWaves, 0, stream>>>(p)
+           : axial_rope_kernel<TI, TO, NORM, kPlain, false><<<grid, 64 * kWaves, 0, stream>>>(p);
 }
 
 template <typename TX, typename TG>
 void launch_backward(const RopeParams& p, dim3 grid, hipStream_t stream) {
+    constexpr int kPlain = sizeof(TX) + sizeof(TG) == 4 ? kRow : kApart;
+    const bool nt = streams(p, 2 * sizeof(TX) + sizeof(TG), std::min(sizeof(TX), sizeof(TG)));
     if (p.halves)
-        qk_norm_rope_backward_kernel<TX, TG, true><<<grid, 64 * kWaves, 0, stream>>>(p);
+        nt ? qk_norm_rope_backward_kernel<TX, TG, kHalves, true><<<grid, 64 * kWaves, 0, stream>>>(p)
+           : qk_norm_rope_backward_kernel<TX, TG, kHalves, false><<<grid, 64 * kWaves, 0, stream>>>(p);
     else
-        qk_norm_rope_backward_kernel<TX, TG, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+        nt ? qk_norm_rope_backward_kernel<TX, TG, kPlain, true><<<grid, 64 * kWaves, 0, stream>>>(p)
+           : qk_norm_rope_backward_kernel<TX, TG, kPlain, false><<<grid, 64 * kWaves, 0, stream>>>(p);
 }
 
 }  // namespace

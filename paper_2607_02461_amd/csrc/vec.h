@@ -1,4 +1,5 @@
-// Vectors of bf16 and fp32 values as the kernels load, convert and store them.
+// Vectors of bf16 and fp32 values as the kernels load, convert and store them.  NT: non-temporally, of data that the
+// caches do not hold to the end of a call.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -24,55 +25,54 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, bf16x2_t));
 }
 
+template <bool NT, typename V>
+__device__ __forceinline__ V load_vec(const void* p) {
+    return NT ? __builtin_nontemporal_load((const V*)p) : *(const V*)p;
+}
+
+template <bool NT, typename V>
+__device__ __forceinline__ void store_vec(void* p, V v) {
+    if (NT)
+        __builtin_nontemporal_store(v, (V*)p);
+    else
+        *(V*)p = v;
+}
+
 // Four values in a row: 8 bytes of bf16 or 16 of fp32.
-template <typename T>
+template <typename T, bool NT>
 struct Vec4;
 
-template <>
-struct Vec4<bf16_t> {
+template <bool NT>
+struct Vec4<bf16_t, NT> {
     u32x2 r;
-    __device__ __forceinline__ void load(const bf16_t* p) { r = *(const u32x2*)p; }
+    __device__ __forceinline__ void load(const bf16_t* p) { r = load_vec<NT, u32x2>(p); }
     __device__ __forceinline__ void get(float* v) const {
         v[0] = bf16_low(r.x), v[1] = bf16_high(r.x), v[2] = bf16_low(r.y), v[3] = bf16_high(r.y);
     }
     static __device__ __forceinline__ void store(bf16_t* p, const float* v) {
-        *(u32x2*)p = (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+        store_vec<NT>(p, (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])});
     }
 };
 
-template <>
-struct Vec4<float> {
+template <bool NT>
+struct Vec4<float, NT> {
     f32x4 r;
-    __device__ __forceinline__ void load(const float* p) { r = *(const f32x4*)p; }
+    __device__ __forceinline__ void load(const float* p) { r = load_vec<NT, f32x4>(p); }
     __device__ __forceinline__ void get(float* v) const { v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w; }
-    static __device__ __forceinline__ void store(float* p, const float* v) { *(f32x4*)p = (f32x4){v[0], v[1], v[2], v[3]}; }
+    static __device__ __forceinline__ void store(float* p, const float* v) { store_vec<NT>(p, (f32x4){v[0], v[1], v[2], v[3]}); }
 };
 
-// Eight values in a row.
-template <typename T>
-struct Vec8;
-
-template <>
-struct Vec8<bf16_t> {
+// Eight bf16 values in a row.
+template <bool NT>
+struct Vec8 {
     u32x4 r;
-    __device__ __forceinline__ void load(const bf16_t* p) { r = *(const u32x4*)p; }
+    __device__ __forceinline__ void load(const bf16_t* p) { r = load_vec<NT, u32x4>(p); }
     __device__ __forceinline__ void get(float* v) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[2 * i] = bf16_low(r[i]), v[2 * i + 1] = bf16_high(r[i]);
     }
     static __device__ __forceinline__ void store(bf16_t* p, const float* v) {
-        *(u32x4*)p = (u32x4){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-    }
-};
-
-template <>
-struct Vec8<float> {
-    Vec4<float> a, b;
-    __device__ __forceinline__ void load(const float* p) { a.load(p), b.load(p + 4); }
-    __device__ __forceinline__ void get(float* v) const { a.get(v), b.get(v + 4); }
-    static __device__ __forceinline__ void store(float* p, const float* v) {
-        Vec4<float>::store(p, v);
-        Vec4<float>::store(p + 4, v + 4);
+        store_vec<NT>(p, (u32x4){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
     }
 };
 
