@@ -10,7 +10,7 @@ import ctypes
 import numpy as np
 import torch
 
-from . import ORBIT_OUT_BF16, ORBIT_OUT_F32, _c_void_p, _call, _check, _expect, _i32, _output, _rows, lib
+from . import ORBIT_OUT_BF16, ORBIT_OUT_F32, _c_void_p, _call, _check, _expect, _output, _ptr, _rows, lib
 
 
 class LoraPlan:
@@ -105,7 +105,7 @@ def lora_add(plan: LoraPlan, X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, 
         _expect(h, "h", torch.float32, (M, R), dev)
     ws = plan._workspace(K, N, R, 0, dev)
     _call("lora_add", dev, plan._h, X.data_ptr(), ldx, A.data_ptr(), B.data_ptr(), K, N, R, pb, ldb,
-          ORBIT_OUT_BF16 if base.dtype == torch.bfloat16 else ORBIT_OUT_F32, out.data_ptr(), ldy, None if h is None else h.data_ptr(),
+          ORBIT_OUT_BF16 if base.dtype == torch.bfloat16 else ORBIT_OUT_F32, out.data_ptr(), ldy, _ptr(h),
           ws.data_ptr(), ws.numel())
     return out
 

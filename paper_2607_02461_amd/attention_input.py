@@ -9,18 +9,19 @@ contiguous: views of the projection's output and of attention layouts are taken 
 """
 
 import ctypes
+import struct
 
 import numpy as np
 import torch
 
-from . import ORBIT_OUT_BF16, ORBIT_OUT_F32, _c_void_p, _call, _check, _expect, _i64, lib
+from . import ORBIT_OUT_BF16, ORBIT_OUT_F32, _c_void_p, _call, _check, _expect, _ptr, lib
 
 _TYPES = {torch.float32: ORBIT_OUT_F32, torch.bfloat16: ORBIT_OUT_BF16}
 
 
-class _Heads(ctypes.Structure):
-    _fields_ = [("data", _c_void_p), ("batch", _i64), ("token", _i64), ("head", _i64), ("heads", ctypes.c_int32),
-                ("dtype", ctypes.c_int32)]
+# orbit_heads as bytes: data, strides of batch, token and head, heads, dtype.  A call on a single token takes a few
+# microseconds on the device, so the host's part is kept short here too (a ctypes structure costs three times this).
+_pack_heads = struct.Struct("Pqqqii").pack
 
 
 class RopePlan:
@@ -82,23 +83,22 @@ def _heads(t, name, like=None, dtype=None):
     """(t's rows for the library, its [batch, token, head, D]).  `like`: the shape it must have, on `like`'s device."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a tensor on a GPU")
-    if t.dtype not in _TYPES or (dtype is not None and t.dtype != dtype):
+    kind = _TYPES.get(t.dtype)
+    if kind is None or (dtype is not None and t.dtype != dtype):
         raise ValueError(f"{name} must be {dtype or 'bf16 or fp32'}, got {t.dtype}")
-    shape, stride = t.shape, t.stride()
+    shape = t.shape
     if like is not None and (shape != like.shape or t.device != like.device):
         raise ValueError(f"{name} must have the shape {tuple(like.shape)} on {like.device}, got {tuple(shape)} on {t.device}")
-    if len(shape) == 3:
-        B, sb = 1, 0
-        L, H, D = shape
-        sl, sh, sd = stride
-    elif len(shape) == 4:
-        B, L, H, D = shape
-        sb, sl, sh, sd = stride
+    if len(shape) == 4:
+        sb, sl, sh, sd = t.stride()
+    elif len(shape) == 3:
+        sl, sh, sd = t.stride()
+        sb, shape = 0, (1, *shape)
     else:
         raise ValueError(f"{name} must be [batch, token, head, D] or [token, head, D]")
     if sd != 1:
         raise ValueError(f"{name}'s last dimension must be contiguous")
-    return _Heads(t.data_ptr(), sb, sl, sh, H, _TYPES[t.dtype]), (B, L, H, D)
+    return _pack_heads(t.data_ptr(), sb, sl, sh, shape[2], kind), shape
 
 
 def _rows_apart(t, name):
@@ -115,7 +115,8 @@ def _output(out, like, name, dtype):
     """(out, its rows): the caller's output, checked, or a new one of `like`'s shape."""
     if out is None:
         out = torch.empty(like.shape, dtype=dtype, device=like.device)
-        return out, _heads(out, name)[0]
+        L, H, D = like.shape[-3:]
+        return out, _pack_heads(out.data_ptr(), L * H * D, H * D, D, H, _TYPES[dtype])
     rows = _heads(out, name, like, dtype)[0]
     _rows_apart(out, name)
     return out, rows
@@ -145,7 +146,7 @@ def axial_rope(plan: RopePlan, x: torch.Tensor, positions: torch.Tensor, inverse
     hx, (B, L, H, D) = _heads(x, "x")
     out, hy = _output(out, x, "out", x.dtype)
     pos, pos_batch = _positions(plan, positions, B, L, x.device)
-    _call("axial_rope", x.device, plan._h, ctypes.byref(hx), ctypes.byref(hy), B, L, D, pos, pos_batch, 1 if inverse else 0)
+    _call("axial_rope", x.device, plan._h, hx, hy, B, L, D, pos, pos_batch, 1 if inverse else 0)
     return out
 
 
@@ -189,9 +190,8 @@ def qk_norm_rope(plan: RopePlan, q: torch.Tensor, k: torch.Tensor, positions: to
         raise ValueError("k_weight or k_out is given without k")
     pos, pos_batch = _positions(plan, positions, B, L, q.device)
     w_dtype = _weights(q_weight, k_weight, D, q.device)
-    _call("qk_norm_rope", q.device, plan and plan._h, ctypes.byref(hq), hk and ctypes.byref(hk), ctypes.byref(hqo),
-          hko and ctypes.byref(hko), B, L, D, pos, pos_batch, None if q_weight is None else q_weight.data_ptr(),
-          None if k_weight is None else k_weight.data_ptr(), w_dtype, eps)
+    _call("qk_norm_rope", q.device, plan and plan._h, hq, hk, hqo, hko, B, L, D, pos, pos_batch, _ptr(q_weight), _ptr(k_weight),
+          w_dtype, eps)
     return q_out, k_out
 
 
@@ -231,8 +231,6 @@ def qk_norm_rope_backward(plan: RopePlan, dq: torch.Tensor, dk: torch.Tensor, q:
     if dwq is not None or dwk is not None:
         ws_bytes = _backward_workspace(D, q.device)
         ws = torch.empty((ws_bytes,), dtype=torch.uint8, device=q.device)
-    _call("qk_norm_rope_backward", q.device, plan and plan._h, ctypes.byref(hdq), hdk and ctypes.byref(hdk), ctypes.byref(hq),
-          hk and ctypes.byref(hk), ctypes.byref(hqg), hkg and ctypes.byref(hkg), B, L, D, pos, pos_batch,
-          None if q_weight is None else q_weight.data_ptr(), None if k_weight is None else k_weight.data_ptr(), w_dtype, eps,
-          None if dwq is None else dwq.data_ptr(), None if dwk is None else dwk.data_ptr(), None if ws is None else ws.data_ptr(), ws_bytes)
+    _call("qk_norm_rope_backward", q.device, plan and plan._h, hdq, hdk, hq, hk, hqg, hkg, B, L, D, pos, pos_batch, _ptr(q_weight),
+          _ptr(k_weight), w_dtype, eps, _ptr(dwq), _ptr(dwk), _ptr(ws), ws_bytes)
     return q_grad, k_grad, dwq, dwk

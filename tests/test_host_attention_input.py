@@ -6,7 +6,11 @@ import numpy as np
 import pytest
 
 import paper_2607_02461_amd as oq
-from paper_2607_02461_amd.attention_input import _Heads
+
+
+class Heads(ctypes.Structure):   # orbit_heads of the C header
+    _fields_ = [("data", ctypes.c_void_p), ("batch", ctypes.c_int64), ("token", ctypes.c_int64), ("head", ctypes.c_int64),
+                ("heads", ctypes.c_int32), ("dtype", ctypes.c_int32)]
 
 
 @pytest.mark.parametrize("dims,lengths,word", [
@@ -41,7 +45,7 @@ def test_device_calls_validate_before_launch():
     plan = oq.rope_plan((16, 16), (4, 4))
 
     def heads(data=fake, strides=(0, 64, 32), n=2, dtype=1):
-        return ctypes.byref(_Heads(data, *strides, n, dtype))
+        return ctypes.byref(Heads(data, *strides, n, dtype))
 
     def rope(plan=plan.handle, x=heads(), y=heads(), B=1, L=3, D=32, pos=fake, inverse=0):
         st = lib.axial_rope(plan, x, y, B, L, D, pos, 0, inverse, None)
