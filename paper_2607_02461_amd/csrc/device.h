@@ -211,20 +211,20 @@ struct LoraSplit {  // tiles [begin, end) of one adapter
 struct LoraShrink {
     const LoraTile* tiles;
     const uint16_t* x;     // bf16 [M][ldx]
-    int64_t ldx, M, K;
+    int64_t ldx, K;
     const uint16_t* pool;  // bf16 [adapter][R][ldp], 16-byte aligned, ldp a multiple of 8 and at least K
     int64_t ldp;
     int R;
     int steps;             // chunks of 128 to a split (set by the launcher)
-    float* h;              // fp32 [split][M][R], every element written
+    float* h;              // sums in the order of the expansion (lora_sum_bytes), every one of a tile's rows written
 };
 
 struct LoraExpand {
     const LoraTile* tiles;
-    const float* h;        // fp32 [splits][M][R]
-    float* sum;            // fp32 [M][R], the splits' sum, or null
+    const float* h;        // the shrink's sums
+    float* sum;            // fp32 [M][R], h itself, or null
     int splits, R;
-    int64_t M, N;
+    int64_t N;
     const uint16_t* pool;  // bf16 [adapter][N][R], 16-byte aligned
     const void* base;      // [M][ldb] of y's type, or null (zeros); may be y
     int64_t ldb;
@@ -274,6 +274,7 @@ struct LoraGrad {
     const int32_t* first;  // [adapters + 1]: splits of each adapter
     LoraGradSide side[2];
     int R;
+    int direct;            // the list has one split for each adapter, whose sums are the result
     int chunks, chunks_x, sum_blocks_x;  // workgroups of a split and of its first side, and of the first side's sums (set by
                                          // the launcher)
 };
@@ -281,11 +282,14 @@ struct LoraGrad {
 // Splits of a contraction over K for this many tiles: at most kLoraMaxSplits.
 int lora_splits(int tiles, int64_t K, int cus);
 hipError_t launch_lora_shrink(LoraShrink p, int tiles, int splits, hipStream_t stream);
+// Bytes of one split's sums.
+inline int64_t lora_sum_bytes(int64_t tiles, int R) { return tiles * kLoraTileRows * ((R + 31) / 32 * 32) * (int64_t)sizeof(float); }
 // Bytes of one narrow matrix in three bf16 parts, in the order of the gradients' operands: tiles of 64 rows.
 inline int64_t lora_operand_bytes(int64_t tiles, int R) { return tiles * kLoraTileRows * ((R + 15) / 16 * 16) * 3 * 2; }
 hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream);
 hipError_t launch_lora_rows(LoraRows p, int tiles, int tile_rows, bool f32, int cus, hipStream_t stream);
 hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream);
-hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, hipStream_t stream);
+// together: a workgroup's waves share columns, else they share rows (direct: they do).
+hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, bool together, hipStream_t stream);
 
 }  // namespace orbit

@@ -70,13 +70,15 @@ struct orbit_rope_s {
 };
 
 // Requests' rows and adapters, as the kernels' lists (device.h): tiles, adapter by adapter and those of none last; the
-// tiles of one adapter in splits of 4 << level tiles, each level with its splits' first index per adapter.
-constexpr int kLoraLevels = 5;
+// tiles of one adapter in splits of 4 << level tiles, each level with its splits' first index per adapter; the last level
+// has one split for each adapter.
+constexpr int kLoraLevels = 6;
 struct orbit_lora_s {
     int64_t rows = 0;
     int32_t adapters = 0, max_rank = 0;
     int64_t tiles = 0;
     int32_t tile_rows = 0;  // of the largest tile
+    int32_t most_tiles = 0; // of one adapter
     std::vector<unsigned char> lists;
     size_t at_splits[kLoraLevels] = {}, at_first[kLoraLevels] = {};  // byte offsets; the tiles are at 0
     int64_t splits[kLoraLevels] = {};

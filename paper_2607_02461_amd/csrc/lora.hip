@@ -82,6 +82,13 @@ __device__ __forceinline__ void transpose8(u32x4 (&v)[8]) {
 
 constexpr int kWaves = 4;
 
+// Where the sums of 16 rows and 32 r's begin, of a split of a tile: 64 lanes of 4 values twice, the order of an operand of
+// the expansion in fp32.
+__device__ __forceinline__ int64_t lora_sum(int split, int64_t tiles, int64_t tile, int rows, int c, int R) {
+    const int wide = (R + 31) / 32;
+    return (((split * tiles + tile) * 4 + rows) * wide + c) * 512;
+}
+
 // Where value (row of a tile, r) of part k lies in what the gradients' kernel reads, in the order of its operands: per 32
 // rows, part and 16 r's, 64 lanes of 8 rows.
 __device__ __forceinline__ int64_t lora_operand(int64_t tile, int row, int k, int r, int R) {
@@ -89,7 +96,7 @@ __device__ __forceinline__ int64_t lora_operand(int64_t tile, int row, int k, in
     return (block * 64 + row % 32 / 8 * 16 + r % 16) * 8 + row % 8;
 }
 
-// h partial sums [split][M][R] of rows x [M][K] and pool [adapter][R][K]: a workgroup takes a tile and a split of K, in
+// h partial sums (lora_sum) of rows x [M][K] and pool [adapter][R][K]: a workgroup takes a tile and a split of K, in
 // chunks of 128 that all its waves bring to LDS, the loads of the next two on their way while one is multiplied.  Each wave
 // takes 32 of a chunk's 128 for all rows, so that LDS is read once, and their sums are added at the end.
 template <int RF>
@@ -180,7 +187,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) 
         }
     }
     float* const sums = (float*)lds;
-    float* const out = p.h + ((int64_t)blockIdx.y * p.M + t.row) * p.R;
+    const int columns = (p.R + 31) / 32 * 32;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
         if (m * 16 >= t.rows) break;
@@ -190,12 +197,13 @@ __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) 
 #pragma unroll
             for (int j = 0; j < 4; ++j) sums[(wave * 16 + q * 4 + j) * kSumRow + r * 16 + i] = acc[m][r][j];
         __syncthreads();
-        const int rows = min(t.rows - m * 16, 16);
-        for (int e = tid; e < rows * p.R; e += 64 * kWaves) {
-            const int row = e / p.R, r = e - row * p.R;
+        float* const out = p.h + lora_sum(blockIdx.y, gridDim.x, blockIdx.x, m, 0, p.R);
+        for (int e = tid; e < columns * 16; e += 64 * kWaves) {
+            // value e % 4 of lane e / 4 % 64, in the half e / 256 % 2 of its 8, of 32 r's e / 512
+            const int row = e / 4 % 16, r = e / 512 * 32 + e / 64 % 4 * 8 + e / 256 % 2 * 4 + e % 4;
             const float* const v = sums + row * kSumRow + r;
             // a row of x that is not finite times the rank's missing rows of A is nothing all the same
-            out[m * 16 * p.R + e] = r < t.rank ? (v[0] + v[16 * kSumRow]) + (v[32 * kSumRow] + v[48 * kSumRow]) : 0.f;
+            out[e] = r < t.rank ? (v[0] + v[16 * kSumRow]) + (v[32 * kSumRow] + v[48 * kSumRow]) : 0.f;
         }
     }
 }
@@ -250,46 +258,61 @@ struct Wide<float> {
 
 constexpr int kTimes = 4;  // rows to a lane in a strip of 16 rows of 256 bytes
 
-// A tile's rows of s h as operands of the expansion, and copies of them for the next kernels: 16 rows to a wave, of which
-// the lane has row i and r = 32 c + 8 q .. + 7.
+// 16 rows of a tile of s h as operands of the expansion: the lane has row i and r = 32 c + 8 q .. + 7.
 template <int RC, int PARTS>
-__device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, int first, bool copy, int i, int q, u32x4 (&h)[RC][PARTS]) {
-    const int at = min(first + i, t.rows - 1);
-    const int64_t row = (int64_t)t.row + at;
-    const bool live = first + i < t.rows;
+__device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, int rows, int lane, u32x4 (&h)[RC][PARTS]) {
 #pragma unroll
     for (int c = 0; c < RC; ++c) {
-        const int r = c * 32 + q * 8;
-        float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-        if (r < p.R) {
-            const float* from = p.h + row * p.R + r;
+        f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+        if (c * 32 < p.R) {
 #pragma unroll 4
             for (int s = 0; s < p.splits; ++s) {
-                const f32x4 lo = *(const f32x4*)(from + s * p.M * p.R), hi = *(const f32x4*)(from + s * p.M * p.R + 4);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) v[j] += lo[j], v[j + 4] += hi[j];
+                const float* const from = p.h + lora_sum(s, gridDim.x, blockIdx.x, rows, c, p.R) + lane * 4;
+                lo += *(const f32x4*)from;
+                hi += *(const f32x4*)(from + 256);
             }
         }
-        if (copy && live && r < p.R && p.sum) {
-            float* const to = p.sum + row * p.R + r;
-            *(f32x4*)to = (f32x4){v[0], v[1], v[2], v[3]};
-            *(f32x4*)(to + 4) = (f32x4){v[4], v[5], v[6], v[7]};
-        }
+        float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= t.scale;
-        if (copy && live && r < p.R && p.turned) {
-            float g[8];
-            u32x4 part[3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) g[j] = v[j];
-            split8<3>(g, part);
-#pragma unroll
-            for (int k = 0; k < 3; ++k)
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    p.turned[lora_operand(blockIdx.x, at, k, r + j, p.R)] = (uint16_t)(part[k][j / 2] >> (16 * (j & 1)));
-        }
+        for (int j = 0; j < 4; ++j) v[j] = lo[j] * t.scale, v[j + 4] = hi[j] * t.scale;
         split8<PARTS>(v, h[c]);
+    }
+}
+
+// The same rows for what comes after the expansion: h itself [M][R], and s h in three parts in the order of lora_operand,
+// for which they turn around in the wave's part of LDS.
+__device__ __forceinline__ void copy_h(const LoraExpand& p, const LoraTile& t, int rows, int lane, float* turn, int stride) {
+    const int i = lane & 15, q = lane >> 4;
+    for (int c = 0; c * 32 < p.R; ++c) {
+        f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
+        for (int s = 0; s < p.splits; ++s) {
+            const float* const from = p.h + lora_sum(s, gridDim.x, blockIdx.x, rows, c, p.R) + lane * 4;
+            lo += *(const f32x4*)from;
+            hi += *(const f32x4*)(from + 256);
+        }
+        if (p.sum && rows * 16 + i < t.rows && c * 32 + q * 8 < p.R) {
+            float* const to = p.sum + ((int64_t)t.row + rows * 16 + i) * p.R + c * 32 + q * 8;
+            *(f32x4*)to = lo;
+            *(f32x4*)(to + 4) = hi;
+        }
+        if (!p.turned || rows * 16 >= t.rows) continue;
+        *(f32x4*)(turn + i * stride + q * 8) = lo * t.scale;
+        *(f32x4*)(turn + i * stride + q * 8 + 4) = hi * t.scale;
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        // lane: r = 16 (lane / 32) + lane % 16 of the 32, rows 8 (lane / 16 % 2) .. + 7 of the 16
+        const int r = lane / 32 * 16 + i, first = lane / 16 % 2 * 8;
+        float v[8];
+        u32x4 part[3];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = turn[(first + j) * stride + r];
+        split8<3>(v, part);
+        if (c * 32 + r < p.R) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) *(u32x4*)(p.turned + lora_operand(blockIdx.x, rows * 16 + first, k, c * 32 + r, p.R)) = part[k];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -354,7 +377,8 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
     if (last >= n0) load_wide(n0);
     if (t.rank > 0) load_pool(n0);
     u32x4 h[RC][kParts];
-    load_h<RC, kParts>(p, t, first, blockIdx.y == 0, i, q, h);
+    load_h<RC, kParts>(p, t, wave, lane, h);
+    if (blockIdx.y == 0 && (p.sum || p.turned)) copy_h(p, t, wave, lane, turn + wave * 16 * kRow, kRow);
 
     // where the lane's operand pieces lie: those beyond R are the zero one
     if (tid == 0) pool_lds[kZero] = (u32x4){0, 0, 0, 0};
@@ -572,12 +596,14 @@ __global__ __launch_bounds__(64 * kRowWaves) void lora_rows_kernel(LoraRows p) {
 // What the backward pass reads the other way round: A [R][K] -> [K][R], B [N][R] -> [R][N padded to 8], and s h [M][R] as
 // three bf16 parts in the order of lora_operand.  A thread turns a block of 8 x 8.
 __global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
-    const int64_t r_blocks = p.R / 8, a_blocks = r_blocks * (p.K / 8), b_blocks = r_blocks * (p.ldn / 8);
-    const int64_t pools = (a_blocks + b_blocks) * p.adapters;
-    int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    // (fewer than 2^31 blocks of 8 x 8 in all)
+    const uint32_t r_blocks = p.R / 8, a_blocks = r_blocks * (uint32_t)(p.K / 8), b_blocks = r_blocks * (uint32_t)(p.ldn / 8);
+    const uint32_t pools = (a_blocks + b_blocks) * p.adapters;
+    uint32_t at = blockIdx.x * 256 + threadIdx.x;
     if (at < pools) {
-        const int64_t adapter = at / (a_blocks + b_blocks);
-        at -= adapter * (a_blocks + b_blocks);
+        const uint32_t of = at / (a_blocks + b_blocks);
+        at -= of * (a_blocks + b_blocks);
+        const int64_t adapter = of;
         u32x4 v[8];
         if (at < a_blocks) {
             const int64_t k = at / r_blocks * 8, r = at % r_blocks * 8;
@@ -590,7 +616,8 @@ __global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
             for (int j = 0; j < 8; ++j) *(u32x4*)(to + j * p.R) = v[j];
         } else {
             at -= a_blocks;
-            const int64_t r = at / (p.ldn / 8) * 8, n = at % (p.ldn / 8) * 8;
+            const uint32_t n_blocks = (uint32_t)(p.ldn / 8);
+            const int64_t r = at / n_blocks * 8, n = at % n_blocks * 8;
             const uint16_t* const from = p.b + (adapter * p.N + n) * p.R + r;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -605,7 +632,7 @@ __global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
         return;
     }
     at -= pools;
-    const int64_t tile = at / (8 * r_blocks);
+    const uint32_t tile = at / (8 * r_blocks);
     if (tile >= p.count) return;
     const LoraTile t = p.tiles[tile];
     const int in_tile = (int)(at - tile * 8 * r_blocks), first = in_tile % 8 * 8, r = in_tile / 8 * 8;
@@ -630,18 +657,22 @@ __global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
 }
 
 // Partial sums [split][R][width] over a split's rows of s narrow^T wide: of g and x (dA) in the first workgroups of a
-// split, of h and dy (dB) in the rest.  A wave takes every fourth step of 32 rows of 128 columns: a lane loads
-// 8 rows of 8 columns, which transposed are 8 operands with the rows as contraction, each for columns 8 apart.
-template <int RF>
+// split, of h and dy (dB) in the rest.  A wave takes steps of 32 rows of 128 columns: a lane loads 8 rows of 8 columns,
+// which transposed are 8 operands with the rows as contraction, each for columns 8 apart.  TOGETHER: the workgroup's waves
+// take every fourth step of the same columns and add their sums in LDS; else they have columns of their own and store
+// their sums themselves, which is faster where a wave has few steps.
+template <int RF, bool TOGETHER>
 __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
-    __shared__ float sums[RF * 16][128 + 4];
+    __shared__ float sums[TOGETHER ? RF * 16 : 1][128 + 4];
     const uint32_t index = blockIdx.x / (uint32_t)p.chunks;
     const int at_chunk = (int)(blockIdx.x - index * (uint32_t)p.chunks);
     const LoraSplit split = p.list[index];
     const bool second = at_chunk >= p.chunks_x;
     const LoraGradSide side = p.side[second];
-    const int chunk = at_chunk - (second ? p.chunks_x : 0);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, kg = lane >> 4;
+    const int chunk = (at_chunk - (second ? p.chunks_x : 0)) * (TOGETHER ? 1 : kWaves) + (TOGETHER ? 0 : wave);
+    if (!TOGETHER && (int64_t)chunk * 128 >= side.width) return;
+    const int every = TOGETHER ? kWaves : 1;
     const int r0 = blockIdx.y * RF * 16;
     const int64_t col = (int64_t)chunk * 128 + c * 8;
     const int64_t left = side.width - col;
@@ -672,10 +703,10 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
     };
     auto steps = [&](auto whole) __attribute__((always_inline)) {
         const int end = 2 * split.end;
-        int step = 2 * split.begin + wave;
+        int step = 2 * split.begin + (TOGETHER ? wave : 0);
         if (step >= end) return;
         load(step, whole);
-        for (; step < end; step += kWaves) {
+        for (; step < end; step += every) {
             u32x4 cols[8], rows[RF][3];
 #pragma unroll
             for (int j = 0; j < 8; ++j) cols[j] = z[j];
@@ -684,7 +715,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
 #pragma unroll
                 for (int k = 0; k < 3; ++k) rows[r][k] = part[r][k];
             const int mine_now = mine, rows_now = t.rows;
-            load(min(step + kWaves, end - 1), whole);
+            load(min(step + every, end - 1), whole);
             if ((step & 1) * 32 + 32 > rows_now) {
                 // rows beyond the tile are another's, or none
 #pragma unroll
@@ -711,6 +742,28 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
         steps(std::true_type{});
     else
         steps(std::false_type{});
+    if (!TOGETHER) {
+        // the lane has 8 columns in a row of rows q * 4 + k of each 16
+#pragma unroll
+        for (int r = 0; r < RF; ++r)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int at = r0 + r * 16 + kg * 4 + k;
+                if (at >= p.R) continue;
+                if (p.direct && second) {
+                    // [width][R]
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < left) side.out[((int64_t)index * side.width + col + j) * p.R + at] = acc[r][j][k];
+                } else {
+                    float* const to = (p.direct ? side.out : side.part) + ((int64_t)index * p.R + at) * side.width + col;
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (j < left) to[j] = acc[r][j][k];
+                }
+            }
+        return;
+    }
     // the waves' sums, in order
     for (int w = 0; w < kWaves; ++w) {
         if (wave == w) {
@@ -787,9 +840,10 @@ void rows(const LoraRows& p, dim3 grid, hipStream_t stream) {
 }  // namespace
 
 int lora_splits(int tiles, int64_t K, int cus) {
-    // halves of the K range until the workgroups are 2 to a compute unit, each keeping at least 2 chunks of 128
+    // halves of the K range until the workgroups are 2 to a compute unit, each keeping at least 6 chunks of 128: every
+    // workgroup of the expansion reads all splits of its tile
     int splits = 1;
-    while (splits < kLoraMaxSplits && (int64_t)tiles * splits < 2 * (int64_t)cus && K >= (int64_t)splits * 2 * 2 * 128) splits *= 2;
+    while (splits < kLoraMaxSplits && (int64_t)tiles * splits < 2 * (int64_t)cus && K >= (int64_t)splits * 2 * 6 * 128) splits *= 2;
     return splits;
 }
 
@@ -838,19 +892,20 @@ hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream) {
     return hipGetLastError();
 }
 
-hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, hipStream_t stream) {
-    p.chunks_x = (int)((p.side[0].width + 127) / 128);
-    p.chunks = p.chunks_x + (int)((p.side[1].width + 127) / 128);
+hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, bool together, hipStream_t stream) {
+    const int each = together ? 128 : 128 * kWaves;
+    p.chunks_x = (int)((p.side[0].width + each - 1) / each);
+    p.chunks = p.chunks_x + (int)((p.side[1].width + each - 1) / each);
     if (splits > 0) {
         const dim3 grid((unsigned)(p.chunks * splits), p.R > 64 ? 2 : 1);
         if (p.R <= 16)
-            lora_grad_kernel<1><<<grid, 64 * kWaves, 0, stream>>>(p);
+            together ? lora_grad_kernel<1, true><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_grad_kernel<1, false><<<grid, 64 * kWaves, 0, stream>>>(p);
         else if (p.R <= 32)
-            lora_grad_kernel<2><<<grid, 64 * kWaves, 0, stream>>>(p);
+            together ? lora_grad_kernel<2, true><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_grad_kernel<2, false><<<grid, 64 * kWaves, 0, stream>>>(p);
         else
-            lora_grad_kernel<4><<<grid, 64 * kWaves, 0, stream>>>(p);
+            together ? lora_grad_kernel<4, true><<<grid, 64 * kWaves, 0, stream>>>(p) : lora_grad_kernel<4, false><<<grid, 64 * kWaves, 0, stream>>>(p);
         const hipError_t e = hipGetLastError();
-        if (e != hipSuccess) return e;
+        if (e != hipSuccess || p.direct) return e;
     }
     p.sum_blocks_x = (int)((p.side[0].width + 255) / 256);
     const int sums = p.sum_blocks_x + (int)((p.side[1].width + 255) / 256);

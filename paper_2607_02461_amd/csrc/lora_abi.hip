@@ -49,6 +49,7 @@ void fill(orbit_lora p, int64_t segments, const int64_t* starts, const int32_t* 
     for (int64_t s = 0; s < segments; ++s) add(starts[s], s + 1 < segments ? starts[s + 1] : p->rows, adapters[s]);
     for (auto& list : of) tiles.insert(tiles.end(), list.begin(), list.end());
     p->tiles = (int64_t)tiles.size();
+    for (int a = 0; a < n; ++a) p->most_tiles = std::max(p->most_tiles, (int32_t)of[a].size());
 
     std::vector<unsigned char>& blob = p->lists;
     auto append = [&](const void* data, size_t bytes) {
@@ -59,13 +60,17 @@ void fill(orbit_lora p, int64_t segments, const int64_t* starts, const int32_t* 
     };
     append(tiles.data(), tiles.size() * sizeof(LoraTile));
     for (int level = 0; level < kLoraLevels; ++level) {
+        const bool whole = level == kLoraLevels - 1;
         const int step = 4 << level;
         std::vector<LoraSplit> list;
         std::vector<int32_t> first(1, 0);
         int32_t at = 0;
         for (int a = 0; a < n; ++a) {
             const int32_t end = at + (int32_t)of[a].size();
-            for (int32_t t = at; t < end; t += step) list.push_back({t, std::min(t + step, end)});
+            if (whole)
+                list.push_back({at, end});
+            else
+                for (int32_t t = at; t < end; t += step) list.push_back({t, std::min(t + step, end)});
             at = end;
             first.push_back((int32_t)list.size());
         }
@@ -81,15 +86,16 @@ size_t padded(int64_t bytes) { return ((size_t)bytes + 255) / 256 * 256; }
 struct Layout {
     int splits = 1;         // of the shrink's contraction
     int level = 0;          // of the gradients' splits
+    bool together = false, direct = false;
     size_t g = 0, g_turned = 0, h_turned = 0, at = 0, bt = 0, grad_x = 0, grad_y = 0, bytes = 0;
     int64_t ldn = 0;        // rows of the turned B
 };
 
-Layout forward_layout(orbit_lora p, int64_t K, int R, int cus, bool h_given) {
+Layout forward_layout(orbit_lora p, int64_t K, int R, int cus) {
     Layout l;
     if (p->tile_rows <= kLoraFewRows) return l;
     l.splits = lora_splits((int)p->tiles, K, cus);
-    if (l.splits > 1 || !h_given) l.bytes = padded(l.splits * p->rows * R * (int64_t)sizeof(float));
+    l.bytes = padded(l.splits * lora_sum_bytes(p->tiles, R));
     return l;
 }
 
@@ -98,22 +104,31 @@ Layout backward_layout(orbit_lora p, int64_t K, int64_t N, int R, int cus) {
     const int64_t n = p->adapters;
     l.ldn = (N + 7) / 8 * 8;
     l.splits = lora_splits((int)p->tiles, N, cus);
+    // Gradients: an adapter's rows in one go where no adapter has more than 8 tiles.  Else workgroups whose waves share
+    // columns, with as many tiles each as leaves two workgroups to a compute unit, or, where that is 4 tiles or fewer,
+    // waves with columns of their own.
     const int64_t chunks = ((K + 127) / 128 + (N + 127) / 128) * (R > 64 ? 2 : 1);
-    l.level = kLoraLevels - 1;
-    while (l.level > 0 && p->splits[l.level] * chunks < 2 * (int64_t)cus) --l.level;
+    if (p->most_tiles <= 8) {
+        l.level = kLoraLevels - 1;
+    } else {
+        l.level = kLoraLevels - 2;
+        while (l.level > 0 && p->splits[l.level] * chunks < 2 * (int64_t)cus) --l.level;
+        l.together = l.level > 0;
+    }
+    l.direct = l.level == kLoraLevels - 1;
     size_t at = 0;
     auto take = [&](int64_t bytes) {
         const size_t here = at;
         at += padded(bytes);
         return here;
     };
-    l.g = take(l.splits * p->rows * R * (int64_t)sizeof(float));
+    l.g = take(l.splits * lora_sum_bytes(p->tiles, R));
     l.g_turned = take(lora_operand_bytes(p->tiles, R));
     l.h_turned = take(lora_operand_bytes(p->tiles, R));
     l.at = take(n * K * R * 2);
     l.bt = take(n * R * l.ldn * 2);
-    l.grad_x = take(p->splits[l.level] * R * K * (int64_t)sizeof(float));
-    l.grad_y = take(p->splits[l.level] * R * N * (int64_t)sizeof(float));
+    l.grad_x = take(l.direct ? 0 : p->splits[l.level] * R * K * (int64_t)sizeof(float));
+    l.grad_y = take(l.direct ? 0 : p->splits[l.level] * R * N * (int64_t)sizeof(float));
     l.bytes = at;
     return l;
 }
@@ -219,7 +234,7 @@ orbit_status lora_add_workspace_size(orbit_lora p, int64_t K, int64_t N, int32_t
     DeviceInfo info;
     st = current_device(&dev, &info);
     if (st != ORBIT_OK) return st;
-    *bytes = backward ? backward_layout(p, K, N, R, info.cus).bytes : forward_layout(p, K, R, info.cus, false).bytes;
+    *bytes = backward ? backward_layout(p, K, N, R, info.cus).bytes : forward_layout(p, K, R, info.cus).bytes;
     return ORBIT_OK;
 }
 
@@ -244,7 +259,7 @@ orbit_status lora_add(orbit_lora p, const uint16_t* X, int64_t ldx, const uint16
     const unsigned char* lists = nullptr;
     st = lists_on(who, p, dev, &lists);
     if (st != ORBIT_OK) return st;
-    const Layout l = forward_layout(p, K, R, info.cus, h != nullptr);
+    const Layout l = forward_layout(p, K, R, info.cus);
     if (l.bytes && (!workspace || !aligned(workspace, 16) || workspace_bytes < l.bytes))
         return fail(ORBIT_EINVAL, "%s: takes a workspace of %zu bytes, aligned to 16", who, l.bytes);
     if (p->tile_rows <= kLoraFewRows) {
@@ -269,21 +284,19 @@ orbit_status lora_add(orbit_lora p, const uint16_t* X, int64_t ldx, const uint16
     s.tiles = (const LoraTile*)lists;
     s.x = X;
     s.ldx = ldx;
-    s.M = p->rows;
     s.K = K;
     s.pool = A;
     s.ldp = K;
     s.R = R;
-    s.h = l.bytes ? (float*)workspace : h;
+    s.h = (float*)workspace;
     hipError_t e = launch_lora_shrink(s, (int)p->tiles, l.splits, (hipStream_t)stream);
     if (e != hipSuccess) return hip_fail(e, who);
     LoraExpand x{};
     x.tiles = s.tiles;
     x.h = s.h;
-    x.sum = l.bytes ? h : nullptr;
+    x.sum = h;
     x.splits = l.splits;
     x.R = R;
-    x.M = p->rows;
     x.N = N;
     x.pool = B;
     x.base = base;
@@ -345,8 +358,7 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
         s.tiles = t.tiles;
         s.x = dY;
         s.ldx = ldd;
-        s.M = p->rows;
-        s.K = N;
+            s.K = N;
         s.pool = t.bt;
         s.ldp = l.ldn;
         s.R = R;
@@ -359,8 +371,7 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
         x.turned = (uint16_t*)(ws + l.g_turned);
         x.splits = l.splits;
         x.R = R;
-        x.M = p->rows;
-        x.N = K;
+            x.N = K;
         x.pool = t.at;
         x.base = base;
         x.ldb = ldb;
@@ -375,7 +386,8 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
     d.side[0] = {X, ldx, K, (const uint16_t*)(ws + l.g_turned), (float*)(ws + l.grad_x), dA};
     d.side[1] = {dY, ldd, N, (const uint16_t*)(ws + l.h_turned), (float*)(ws + l.grad_y), dB};
     d.R = R;
-    e = launch_lora_grad(d, (int)p->splits[l.level], p->adapters, hs);
+    d.direct = l.direct;
+    e = launch_lora_grad(d, (int)p->splits[l.level], p->adapters, l.together, hs);
     return e == hipSuccess ? ORBIT_OK : hip_fail(e, who);
 }
 
