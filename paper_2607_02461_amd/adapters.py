@@ -32,14 +32,15 @@ class LoraPlan:
         return self
 
     def _workspace(self, K, N, R, backward, dev):
-        """A new workspace; its size depends on the sizes alone."""
+        """(a new workspace or None, its bytes); the plan and the sizes alone decide them."""
         key = (K, N, R, backward, dev)
         if key not in self._bytes:
             n = ctypes.c_size_t(0)
             with torch.cuda.device(dev):
                 _check("lora_add_workspace_size", lib().lora_add_workspace_size(self._h, K, N, R, backward, ctypes.byref(n)))
             self._bytes[key] = n.value
-        return torch.empty((self._bytes[key],), dtype=torch.uint8, device=dev)
+        n = self._bytes[key]
+        return torch.empty((n,), dtype=torch.uint8, device=dev) if n else None, n
 
     def __del__(self):
         if getattr(self, "_h", None):
@@ -103,10 +104,10 @@ def lora_add(plan: LoraPlan, X: torch.Tensor, A: torch.Tensor, B: torch.Tensor, 
     out, ldy = _output(out, M, N, base.dtype, dev)
     if h is not None:
         _expect(h, "h", torch.float32, (M, R), dev)
-    ws = plan._workspace(K, N, R, 0, dev)
+    ws, ws_bytes = plan._workspace(K, N, R, 0, dev)
     _call("lora_add", dev, plan._h, X.data_ptr(), ldx, A.data_ptr(), B.data_ptr(), K, N, R, pb, ldb,
           ORBIT_OUT_BF16 if base.dtype == torch.bfloat16 else ORBIT_OUT_F32, out.data_ptr(), ldy, _ptr(h),
-          ws.data_ptr(), ws.numel())
+          _ptr(ws), ws_bytes)
     return out
 
 
@@ -123,7 +124,7 @@ def lora_add_backward(plan: LoraPlan, dY: torch.Tensor, X: torch.Tensor, A: torc
     out, lddx = _output(out, M, K, torch.bfloat16, dev)
     dA = torch.empty(A.shape, dtype=torch.float32, device=dev)
     dB = torch.empty(B.shape, dtype=torch.float32, device=dev)
-    ws = plan._workspace(K, N, R, 1, dev)
+    ws, ws_bytes = plan._workspace(K, N, R, 1, dev)
     _call("lora_add_backward", dev, plan._h, pd, ldd, X.data_ptr(), ldx, A.data_ptr(), B.data_ptr(), h.data_ptr(), K, N, R, pb, ldb,
-          out.data_ptr(), lddx, dA.data_ptr(), dB.data_ptr(), ws.data_ptr(), ws.numel())
+          out.data_ptr(), lddx, dA.data_ptr(), dB.data_ptr(), _ptr(ws), ws_bytes)
     return out, dA, dB

@@ -289,7 +289,7 @@ inline int64_t lora_operand_bytes(int64_t tiles, int R) { return tiles * kLoraTi
 hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream);
 hipError_t launch_lora_rows(LoraRows p, int tiles, int tile_rows, bool f32, int cus, hipStream_t stream);
 hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream);
-// together: a workgroup's waves share columns, else they share rows (direct: they do).
+// together: a workgroup's waves share columns (direct: always), else they share rows.
 hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, bool together, hipStream_t stream);
 
 }  // namespace orbit

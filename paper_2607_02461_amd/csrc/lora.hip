@@ -683,59 +683,59 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[r][j] = (f32x4){0, 0, 0, 0};
     const bool wide_whole = side.width - (int64_t)chunk * 128 >= 128;
-    u32x4 z[8], part[RF][3];
-    LoraTile t;
-    int mine;  // the lane's first row of the tile
-    auto load = [&](int step, auto whole) __attribute__((always_inline)) {
-        t = p.tiles[step / 2];
-        mine = (step & 1) * 32 + kg * 8;
+    // two steps on their way; a load comes whether it is needed or not (the split's last step again), since after a branch
+    // around one the compiler waits for all of them
+    u32x4 z[2][8], part[2][RF][3];
+    int mine[2], rows[2];  // the lane's first row of the step's tile, and the tile's rows
+    auto load = [&](int d, int step, auto whole) __attribute__((always_inline)) {
+        const LoraTile t = p.tiles[step / 2];
+        mine[d] = (step & 1) * 32 + kg * 8;
+        rows[d] = t.rows;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint16_t* const from = side.wide + ((int64_t)t.row + min(mine + j, t.rows - 1)) * side.ld + col;
-            z[j] = whole.value ? load8(from) : load8_part(from, left);
+            const uint16_t* const from = side.wide + ((int64_t)t.row + min(mine[d] + j, t.rows - 1)) * side.ld + col;
+            z[d][j] = whole.value ? load8(from) : load8_part(from, left);
         }
 #pragma unroll
         for (int r = 0; r < RF; ++r) {
             const int frag = min(r0 / 16 + r, (p.R - 1) / 16);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) part[r][k] = *(const u32x4*)(side.narrow + lora_operand(step / 2, (step & 1) * 32, k, frag * 16, p.R) + lane * 8);
+            for (int k = 0; k < 3; ++k) part[d][r][k] = *(const u32x4*)(side.narrow + lora_operand(step / 2, (step & 1) * 32, k, frag * 16, p.R) + lane * 8);
         }
+    };
+    auto multiply = [&](int d, int step) __attribute__((always_inline)) {
+        if ((step & 1) * 32 + 32 > rows[d]) {
+            // rows beyond the tile are another's, or none
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (mine[d] + j >= rows[d]) z[d][j] = (u32x4){0, 0, 0, 0};
+#pragma unroll
+            for (int r = 0; r < RF; ++r)
+#pragma unroll
+                for (int k = 0; k < 3; ++k)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        part[d][r][k][j] &= (mine[d] + 2 * j < rows[d] ? 0xFFFFu : 0u) | (mine[d] + 2 * j + 1 < rows[d] ? 0xFFFF0000u : 0u);
+        }
+        transpose8(z[d]);
+#pragma unroll
+        for (int r = 0; r < RF; ++r)
+#pragma unroll
+            for (int k = 2; k >= 0; --k)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) acc[r][j] = mfma(part[d][r][k], z[d][j], acc[r][j]);
     };
     auto steps = [&](auto whole) __attribute__((always_inline)) {
         const int end = 2 * split.end;
         int step = 2 * split.begin + (TOGETHER ? wave : 0);
         if (step >= end) return;
-        load(step, whole);
-        for (; step < end; step += every) {
-            u32x4 cols[8], rows[RF][3];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) cols[j] = z[j];
-#pragma unroll
-            for (int r = 0; r < RF; ++r)
-#pragma unroll
-                for (int k = 0; k < 3; ++k) rows[r][k] = part[r][k];
-            const int mine_now = mine, rows_now = t.rows;
-            load(min(step + every, end - 1), whole);
-            if ((step & 1) * 32 + 32 > rows_now) {
-                // rows beyond the tile are another's, or none
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (mine_now + j >= rows_now) cols[j] = (u32x4){0, 0, 0, 0};
-#pragma unroll
-                for (int r = 0; r < RF; ++r)
-#pragma unroll
-                    for (int k = 0; k < 3; ++k)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            rows[r][k][j] &= (mine_now + 2 * j < rows_now ? 0xFFFFu : 0u) | (mine_now + 2 * j + 1 < rows_now ? 0xFFFF0000u : 0u);
-            }
-            transpose8(cols);
-#pragma unroll
-            for (int r = 0; r < RF; ++r)
-#pragma unroll
-                for (int k = 2; k >= 0; --k)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) acc[r][j] = mfma(rows[r][k], cols[j], acc[r][j]);
+        load(0, step, whole);
+        load(1, min(step + every, end - 1), whole);
+        for (; step < end; step += 2 * every) {
+            multiply(0, step);
+            load(0, min(step + 2 * every, end - 1), whole);
+            if (step + every < end) multiply(1, step + every);
+            load(1, min(step + 3 * every, end - 1), whole);
         }
     };
     if (wide_whole)
@@ -750,15 +750,13 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
             for (int k = 0; k < 4; ++k) {
                 const int at = r0 + r * 16 + kg * 4 + k;
                 if (at >= p.R) continue;
-                if (p.direct && second) {
-                    // [width][R]
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (j < left) side.out[((int64_t)index * side.width + col + j) * p.R + at] = acc[r][j][k];
+                float* const to = side.part + ((int64_t)index * p.R + at) * side.width + col;
+                if (left >= 8) {
+                    *(f32x4_any*)to = (f32x4){acc[r][0][k], acc[r][1][k], acc[r][2][k], acc[r][3][k]};
+                    *(f32x4_any*)(to + 4) = (f32x4){acc[r][4][k], acc[r][5][k], acc[r][6][k], acc[r][7][k]};
                 } else {
-                    float* const to = (p.direct ? side.out : side.part) + ((int64_t)index * p.R + at) * side.width + col;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
+                    for (int j = 0; j < 7; ++j)
                         if (j < left) to[j] = acc[r][j][k];
                 }
             }
@@ -779,10 +777,19 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
         }
         __syncthreads();
     }
-    float* const out = side.part + ((int64_t)index * p.R + r0) * side.width;
+    const int64_t n0 = (int64_t)chunk * 128;
+    if (p.direct && second) {
+        // [width][R]
+        for (int e = threadIdx.x; e < RF * 16 * 128; e += 64 * kWaves) {
+            const int n = e / (RF * 16), r = e % (RF * 16);
+            if (r0 + r < p.R && n0 + n < side.width) side.out[((int64_t)index * side.width + n0 + n) * p.R + r0 + r] = sums[r][n];
+        }
+        return;
+    }
+    float* const out = (p.direct ? side.out : side.part) + ((int64_t)index * p.R + r0) * side.width + n0;
     for (int e = threadIdx.x; e < RF * 16 * 128; e += 64 * kWaves) {
         const int r = e >> 7, n = e & 127;
-        if (r0 + r < p.R && (int64_t)chunk * 128 + n < side.width) out[r * side.width + (int64_t)chunk * 128 + n] = sums[r][n];
+        if (r0 + r < p.R && n0 + n < side.width) out[r * side.width + n] = sums[r][n];
     }
 }
 

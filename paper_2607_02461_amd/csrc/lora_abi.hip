@@ -104,12 +104,13 @@ Layout backward_layout(orbit_lora p, int64_t K, int64_t N, int R, int cus) {
     const int64_t n = p->adapters;
     l.ldn = (N + 7) / 8 * 8;
     l.splits = lora_splits((int)p->tiles, N, cus);
-    // Gradients: an adapter's rows in one go where no adapter has more than 8 tiles.  Else workgroups whose waves share
+    // Gradients: an adapter's rows in one go where no adapter has more than 4 tiles.  Else workgroups whose waves share
     // columns, with as many tiles each as leaves two workgroups to a compute unit, or, where that is 4 tiles or fewer,
     // waves with columns of their own.
     const int64_t chunks = ((K + 127) / 128 + (N + 127) / 128) * (R > 64 ? 2 : 1);
-    if (p->most_tiles <= 8) {
+    if (p->most_tiles <= 4) {
         l.level = kLoraLevels - 1;
+        l.together = true;
     } else {
         l.level = kLoraLevels - 2;
         while (l.level > 0 && p->splits[l.level] * chunks < 2 * (int64_t)cus) --l.level;
