@@ -372,3 +372,59 @@ def test_refusals():
     refused(lambda: oq.qk_norm_rope_backward(plan, x, x, x, None, pos, w), "without k")
     refused(lambda: oq.qk_norm_rope(None, _rows((1, 1, 1, 20), BF16, 1)[..., :12], None, None), "head size 12")
     refused(lambda: oq.qk_norm_rope(None, _rows((1, 1, 1, 520), BF16, 1), None, None), "head size 520")
+
+
+# --- large tensors: non-temporal loads and stores ---------------------------------------------------
+def _turned(x, angles, halves, sign=1.0):
+    """rope_turn in fp64 on the device."""
+    P = angles.shape[-1]
+    c, s = torch.cos(angles)[None, :, None], sign * torch.sin(angles)[None, :, None]
+    first, second = (slice(0, P), slice(P, 2 * P)) if halves else (slice(0, 2 * P, 2), slice(1, 2 * P, 2))
+    y = x.clone()
+    y[..., first], y[..., second] = x[..., first] * c - x[..., second] * s, x[..., first] * s + x[..., second] * c
+    return y
+
+
+def _device_pair_length(x, P, halves):
+    out = x.abs()
+    first, second = (slice(0, P), slice(P, 2 * P)) if halves else (slice(0, 2 * P, 2), slice(1, 2 * P, 2))
+    out[..., first] = out[..., second] = torch.hypot(x[..., first], x[..., second])
+    return out
+
+
+@pytest.mark.parametrize("dtype,out", [(BF16, BF16), (F32, BF16), (F32, F32), (BF16, F32)])
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("D,dims", [(128, (16, 56, 56)), (160, (64, 64))])
+def test_large_tensors(dtype, out, halves, D, dims):
+    # above 160 MiB in and out
+    size = {BF16: 2, F32: 4}
+    H = 9
+    L = (170 << 20) // (H * D * (size[dtype] + size[out])) + 3
+    lengths = [L] * len(dims)
+    plan = oq.rope_plan(dims, lengths, halves=halves)
+    g = torch.Generator(device=DEV).manual_seed(90)
+    pos = torch.randint(0, L, (L, len(dims)), generator=g, device=DEV, dtype=torch.int32)
+    angles = torch.cat([pos[:, a:a + 1].double() * torch.tensor(10000.0 ** (-2.0 * np.arange(d // 2) / d), device=DEV) for a, d in enumerate(dims)], dim=1)
+    q = torch.randn((1, L, H, D), generator=g, device=DEV).to(dtype)
+    w = torch.linspace(0.5, 2.0, D, device=DEV)
+    P = sum(dims) // 2
+
+    def within(got, ref, size, kind):
+        assert float(((got.double() - ref).abs() - (HALF_ULP[kind] * ref.abs() + 32 * U * size)).max()) <= 0.0
+
+    y, _ = oq.qk_norm_rope(plan, q, None, pos, w, eps=EPS, out_dtype=out)
+    x64, w64 = q.double(), w.double()
+    r = torch.rsqrt(x64.square().mean(-1, keepdim=True) + EPS)
+    n = x64 * r * w64
+    within(y, _turned(n, angles, halves), _device_pair_length(n, P, halves), out)
+    if dtype == out:
+        within(oq.axial_rope(plan, q, pos, inverse=True), _turned(x64, angles, halves, -1.0), _device_pair_length(x64, P, halves), dtype)
+    del y, n
+    dy = torch.randn((1, L, H, D), generator=g, device=DEV).to(out)
+    gq, _, dw, _ = oq.qk_norm_rope_backward(plan, dy, None, q, None, pos, w, eps=EPS)
+    t = _turned(dy.double(), angles, halves, -1.0)
+    dot = (t * w64 * x64).mean(-1, keepdim=True)
+    length = _device_pair_length(t, P, halves) * w64
+    within(gq, r * (t * w64 - x64 * r * r * dot), r * (length + x64.abs() * r * r * (length * x64.abs()).mean(-1, keepdim=True)), dtype)
+    terms = (_device_pair_length(t, P, halves) * x64.abs() * r).sum((0, 1, 2))
+    assert ((dw.double() - (t * x64 * r).sum((0, 1, 2))).abs() <= (10 * (L * H) ** 0.5 + 32) * U * terms).all()

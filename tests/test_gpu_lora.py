@@ -15,6 +15,7 @@ import torch
 
 import oracle
 import paper_2607_02461_amd as oq
+from paper_2607_02461_amd.launches import launches
 
 pytestmark = pytest.mark.gpu
 
@@ -307,3 +308,88 @@ def test_refusals():
     refused(lambda: add(x=_randn((20, 60), 1), A=_randn((2, 8, 60), 1)), "K=60")
     sixteen = oq.lora_plan(20, [0], [0], [16, 2], [1.0, 1.0])
     refused(lambda: add(plan=sixteen), "rank 16")
+
+
+# --- the kernels' other ways ----------------------------------------------------------------------
+@pytest.mark.parametrize("R,ranks", [(8, [8, 5]), (16, [16, 3]), (24, [17, 24]), (32, [32, 31]), (48, [33, 48]), (64, [64, 1]), (80, [65, 80]),
+                                     (128, [128, 100])])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_few_rows_of_many_requests(R, ranks, rows, dtype):
+    # both products in one kernel: requests of up to 4 rows, some without an adapter, an output of odd stride
+    for K, N in ((8, 3), (520, 1111), (3072, 700)):
+        M = 7 * rows
+        b = Batch(M, K, N, R, [rows * i for i in range(7)], [0, 1, -1, 1, 0, 0, 1], ranks, [0.5, -2.0], dtype)
+        whole = torch.full((M, N + 3), 7.0, dtype=dtype, device=DEV)
+        y = b.forward(out=whole[:, 1:1 + N])
+        b.check_forward(y)
+        b.check_h(b.h)
+        assert (whole[:, :1] == 7).all() and (whole[:, 1 + N:] == 7).all()
+        in_place = b.base.clone()
+        assert torch.equal(oq.lora_add(b.plan, b.x, b.A, b.B, in_place, out=in_place), y)
+        b.check_backward(*b.backward())
+        if N == 700:
+            names = [r.kernel for r in launches(lambda: b.forward(out=y))]
+            assert len(names) == 1 and "lora_rows_kernel" in names[0]
+
+
+def test_few_rows_that_are_not_finite():
+    b = Batch(6, 520, 100, 16, [0, 1, 2, 4], [0, 1, 0, 1], [16, 9], [1.0, 1.0], F32)
+    want = b.forward()
+    b.x[1, 519] = float("inf")
+    b.x[3, 0] = float("nan")
+    b.base[4, 7] = float("nan")
+    got = b.forward()
+    assert torch.equal(got[[0, 2, 5]], want[[0, 2, 5]])
+    assert not torch.isfinite(got[1]).any() and torch.isnan(got[3]).all()
+    assert torch.isnan(got[4, 7]) and torch.equal(got[4, 8:], want[4, 8:])
+
+
+@pytest.mark.parametrize("R,rank", [(8, 7), (32, 32), (64, 50), (128, 128), (72, 72)])
+@pytest.mark.parametrize("N", [384, 385, 511])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_whole_tiles(R, rank, N, dtype):
+    # tiles of 64 rows, widths in whole strips and not, a contraction of whole chunks and not
+    for K in (1024, 1096):
+        b = Batch(256, K, N, R, [0, 128], [0, 1], [rank, rank], [1.0, 0.5], dtype)
+        b.check_forward(b.forward())
+        b.check_backward(*b.backward())
+
+
+def _on_device(b):
+    """The oracle's formulas in fp64 on the device, for batches that numpy would take long over."""
+    x, dy, A, B = (torch.nan_to_num(t).double() for t in (b.x, b.dy, b.A, b.B))
+    refs = [b.base.double(), torch.zeros_like(x), torch.zeros_like(A), torch.zeros_like(B)]
+    sizes = [torch.zeros_like(r) for r in refs]
+    starts = b.lists["starts"]
+    for first, end, a in zip(starts, starts[1:] + [b.M], b.lists["adapters"]):
+        s = b.lists["scales"][a]
+        for out, f in ((refs, lambda t: t), (sizes, torch.abs)):
+            xs, ds, Aa, Ba, sc = f(x[first:end]), f(dy[first:end]), f(A[a]), f(B[a]), abs(s) if f is torch.abs else s
+            h, g = xs @ Aa.t(), ds @ Ba
+            out[0][first:end] += sc * h @ Ba.t()
+            out[1][first:end] += sc * g @ Aa
+            out[2][a] += sc * g.t() @ xs
+            out[3][a] += sc * ds.t() @ h
+    return refs, sizes
+
+
+@pytest.mark.parametrize("M,K,N,R,starts,adapters,ways", [
+    (1000, 256, 392, 16, [0, 500], [0, 1], "lora_grad_kernel<1,false>"),              # more than 4 tiles to an adapter
+    (16384 + 40, 2048, 2056, 8, [0], [0], "lora_grad_kernel<1,true>"),                # waves that share columns, partial sums
+    (16384 + 33, 2048, 2049, 64, [0, 8000], [1, 0], "lora_grad_kernel<4,true>"),
+    (300, 520, 770, 128, [0, 150], [0, 1], "lora_grad_kernel<4,true>"),               # at most 4 tiles: no partial sums
+    (1500, 520, 770, 96, [0], [0], "lora_grad_kernel<4,false>"),
+])
+def test_ways_of_the_gradients(M, K, N, R, starts, adapters, ways):
+    b = Batch(M, K, N, R, starts, adapters, [R, R - 1], [0.5, -1.0])
+    y = b.forward()
+    dx, dA, dB = b.backward()
+    refs, sizes = _on_device(b)
+    grow = (10 * max(K, N) ** 0.5 + 120) * U
+    for name, got, ref, size, bar in (("y", y, refs[0], sizes[0], HALF_ULP[BF16]), ("dx", dx, refs[1], sizes[1], HALF_ULP[BF16]),
+                                      ("dA", dA, refs[2], sizes[2], U), ("dB", dB, refs[3], sizes[3], U)):
+        more = grow + 10 * M ** 0.5 * U if name in ("dA", "dB") else grow
+        over = ((got.double() - ref).abs() - (bar * ref.abs() + (2.0 ** -16 + more) * size + 2 * U * ref.abs())).max()
+        assert float(over) <= 0.0, f"{name}: {float(over)} beyond its bar"
+    assert any(r.kernel == ways for r in launches(lambda: b.backward(out=dx)))
