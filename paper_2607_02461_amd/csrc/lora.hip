@@ -128,7 +128,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) 
 #pragma unroll
             for (int j = 0; j < 4; ++j) xv[d][j] = load8(x[j] + at);
 #pragma unroll
-            for (int j = 0; j < RF; ++j) av[d][j] = *(const u32x4*)(a[j] + at);
+            for (int j = 0; j < RF; ++j) av[d][j] = load8(a[j] + at);
         };
         auto stage = [&](int d) __attribute__((always_inline)) {
             // piece c of row r lies at c ^ r % 16: rows read at one piece fall on different banks
@@ -173,15 +173,28 @@ __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) 
             k += 128 * (int64_t)n;
         }
         if (k < end) {
-            // a partial chunk; the pool's rows are padded to 8 values
-            const int64_t left = end - k - piece * 8;
+            // a partial chunk: the 128 that end with it, those before it cleared, or all there are of fewer than 128
+            const int64_t at = max(end - 128, (int64_t)0);
+            if (p.K >= 128) {
+                load(0, at);
+            } else {
+                // the pool's rows are padded to 8 values
 #pragma unroll
-            for (int j = 0; j < 4; ++j) xv[0][j] = load8_part(x[j] + k, left);
+                for (int j = 0; j < 4; ++j) xv[0][j] = load8_part(x[j], end - piece * 8);
 #pragma unroll
-            for (int j = 0; j < RF; ++j) {
-                av[0][j] = (u32x4){0, 0, 0, 0};
-                if (left > 0) av[0][j] = *(const u32x4*)(a[j] + k);
+                for (int j = 0; j < RF; ++j) {
+                    av[0][j] = (u32x4){0, 0, 0, 0};
+                    if (piece * 8 < end) av[0][j] = *(const u32x4*)a[j];
+                }
             }
+            const int skip = (int)(k - at) - piece * 8;
+            u32x4 keep;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) keep[j] = (2 * j >= skip ? 0xFFFFu : 0u) | (2 * j + 1 >= skip ? 0xFFFF0000u : 0u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xv[0][j] &= keep;
+#pragma unroll
+            for (int j = 0; j < RF; ++j) av[0][j] &= keep;
             stage(0);
             multiply();
         }
@@ -674,15 +687,16 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
     if (!TOGETHER && (int64_t)chunk * 128 >= side.width) return;
     const int every = TOGETHER ? kWaves : 1;
     const int r0 = blockIdx.y * RF * 16;
-    const int64_t col = (int64_t)chunk * 128 + c * 8;
+    // a last chunk of fewer than 128 columns begins further left, among columns of the one before, which it leaves alone
+    const int64_t n0 = min((int64_t)chunk * 128, max(side.width - 128, (int64_t)0)), col = n0 + c * 8;
     const int64_t left = side.width - col;
+    const int skip = (int)((int64_t)chunk * 128 - n0);
 
     f32x4 acc[RF][8];
 #pragma unroll
     for (int r = 0; r < RF; ++r)
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[r][j] = (f32x4){0, 0, 0, 0};
-    const bool wide_whole = side.width - (int64_t)chunk * 128 >= 128;
     // two steps on their way; a load comes whether it is needed or not (the split's last step again), since after a branch
     // around one the compiler waits for all of them
     u32x4 z[2][8], part[2][RF][3];
@@ -738,7 +752,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
             load(1, min(step + 3 * every, end - 1), whole);
         }
     };
-    if (wide_whole)
+    if (side.width >= 128)
         steps(std::true_type{});
     else
         steps(std::false_type{});
@@ -751,13 +765,13 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
                 const int at = r0 + r * 16 + kg * 4 + k;
                 if (at >= p.R) continue;
                 float* const to = side.part + ((int64_t)index * p.R + at) * side.width + col;
-                if (left >= 8) {
+                if (left >= 8 && c * 8 >= skip) {
                     *(f32x4_any*)to = (f32x4){acc[r][0][k], acc[r][1][k], acc[r][2][k], acc[r][3][k]};
                     *(f32x4_any*)(to + 4) = (f32x4){acc[r][4][k], acc[r][5][k], acc[r][6][k], acc[r][7][k]};
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 7; ++j)
-                        if (j < left) to[j] = acc[r][j][k];
+                    for (int j = 0; j < 8; ++j)
+                        if (j < left && c * 8 + j >= skip) to[j] = acc[r][j][k];
                 }
             }
         return;
@@ -777,19 +791,18 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
         }
         __syncthreads();
     }
-    const int64_t n0 = (int64_t)chunk * 128;
     if (p.direct && second) {
         // [width][R]
         for (int e = threadIdx.x; e < RF * 16 * 128; e += 64 * kWaves) {
             const int n = e / (RF * 16), r = e % (RF * 16);
-            if (r0 + r < p.R && n0 + n < side.width) side.out[((int64_t)index * side.width + n0 + n) * p.R + r0 + r] = sums[r][n];
+            if (r0 + r < p.R && n0 + n < side.width && n >= skip) side.out[((int64_t)index * side.width + n0 + n) * p.R + r0 + r] = sums[r][n];
         }
         return;
     }
     float* const out = (p.direct ? side.out : side.part) + ((int64_t)index * p.R + r0) * side.width + n0;
     for (int e = threadIdx.x; e < RF * 16 * 128; e += 64 * kWaves) {
         const int r = e >> 7, n = e & 127;
-        if (r0 + r < p.R && n0 + n < side.width) out[r * side.width + n] = sums[r][n];
+        if (r0 + r < p.R && n0 + n < side.width && n >= skip) out[r * side.width + n] = sums[r][n];
     }
 }
 
