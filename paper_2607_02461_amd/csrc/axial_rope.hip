@@ -26,8 +26,9 @@ namespace orbit {
 namespace {
 
 constexpr int kRows = 6;       // head rows that a wave's lanes have in flight
-constexpr int kBackRows = 3;   // the same for the backward pass, which reads two tensors
+constexpr int kBackRows = 3;   // the same for the backward pass, which reads two tensors, where heads are few
 constexpr int kWaves = 4;      // waves to a workgroup
+constexpr int kBackGroups = 8; // most workgroups of the backward pass to a compute unit
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float v) {
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(64 * kWaves) void axial_rope_kernel(RopeParams p) {
 // Persistent: the workgroup's sums of the weight's gradient stay in its lanes' registers, eight columns each, until
 // its last row, and leave as one row of partial sums.  They are added in a fixed order, so the result does not
 // depend on which workgroup ends first.
-template <typename TX, typename TG, int LAY, bool NT>
+template <typename TX, typename TG, int LAY, bool NT, int ROWS>
 __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_backward_kernel(RopeParams p) {
     __shared__ float part[kWaves][512];
     const RopeTensor& t = p.t[blockIdx.y];
@@ -226,10 +227,10 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_backward_kernel(Rope
         const Item it(p, t, item, lane);
         int at[4];
         if (p.pairs) find_angles(p, me, it.b, it.l, at);
-        Row8<TX, LAY, NT> x[kBackRows];
-        Row8<TG, LAY, NT> g[kBackRows];
+        Row8<TX, LAY, NT> x[ROWS];
+        Row8<TG, LAY, NT> g[ROWS];
 #pragma unroll
-        for (int u = 0; u < kBackRows; ++u) {
+        for (int u = 0; u < ROWS; ++u) {
             if (u < t.rows) {
                 const int head = min(it.head + u * t.wave_heads, t.heads - 1);
                 x[u].load(row_of<const TX>(t.x, it, head), me.lo, me.hi);
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(64 * kWaves) void qk_norm_rope_backward_kernel(Rope
         float cs[4], sn[4];
         if (p.pairs) load_angles(p, at, cs, sn);
 #pragma unroll
-        for (int u = 0; u < kBackRows; ++u) {
+        for (int u = 0; u < ROWS; ++u) {
             if (u >= t.rows) break;
             const int head = it.head + u * t.wave_heads;
             const bool live = me.live && it.live && head < t.heads;
@@ -339,16 +340,46 @@ void launch(const RopeParams& p, dim3 grid, hipStream_t stream) {
            : axial_rope_kernel<TI, TO, NORM, kPlain, false><<<grid, 64 * kWaves, 0, stream>>>(p);
 }
 
+template <typename TX, typename TG, int LAY, bool NT>
+hipError_t launch_backward(RopeParams p, int cus, hipStream_t stream) {
+    int steps = 0;
+    for (int i = 0; i < p.tensors; ++i) {
+        divide(p, p.t[i], kRows, cus);  // no tokens: no items, and the weights' gradients are sums of nothing
+        steps = std::max(steps, p.t[i].rows);
+    }
+    // Six rows in flight where there are as many: 360 MB 134 -> 115 us; but three rows of the same registers' waves 46 -> 56.
+    const bool many = steps > 4;
+    const void* kernel = many ? (const void*)qk_norm_rope_backward_kernel<TX, TG, LAY, NT, kRows>
+                              : (const void*)qk_norm_rope_backward_kernel<TX, TG, LAY, NT, kBackRows>;
+    uint32_t items = 0;
+    for (int i = 0; i < p.tensors; ++i) {
+        divide(p, p.t[i], many ? kRows : kBackRows, cus);
+        items = std::max(items, p.t[i].items);
+    }
+    // as many workgroups as are resident at once
+    const int resident = std::min(resident_blocks(kernel, 64 * kWaves, 0), kBackGroups);
+    const int groups = (int)std::min<int64_t>((items + kWaves - 1) / kWaves, (resident * cus + p.tensors - 1) / p.tensors);
+    for (int i = 0; i < p.tensors; ++i) p.t[i].parts = groups;
+    if (groups) {
+        const dim3 grid(groups, p.tensors);
+        if (many)
+            qk_norm_rope_backward_kernel<TX, TG, LAY, NT, kRows><<<grid, 64 * kWaves, 0, stream>>>(p);
+        else
+            qk_norm_rope_backward_kernel<TX, TG, LAY, NT, kBackRows><<<grid, 64 * kWaves, 0, stream>>>(p);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    if (!p.t[0].dw && !p.t[1].dw) return hipSuccess;
+    norm_weight_grad_kernel<<<dim3((p.D + 15) / 16, p.tensors), 1024, 0, stream>>>(p);
+    return hipGetLastError();
+}
+
 template <typename TX, typename TG>
-void launch_backward(const RopeParams& p, dim3 grid, hipStream_t stream) {
+hipError_t launch_backward(const RopeParams& p, int cus, hipStream_t stream) {
     constexpr int kPlain = sizeof(TX) + sizeof(TG) == 4 ? kRow : kApart;
     const bool nt = streams(p, 2 * sizeof(TX) + sizeof(TG), std::min(sizeof(TX), sizeof(TG)));
-    if (p.halves)
-        nt ? qk_norm_rope_backward_kernel<TX, TG, kHalves, true><<<grid, 64 * kWaves, 0, stream>>>(p)
-           : qk_norm_rope_backward_kernel<TX, TG, kHalves, false><<<grid, 64 * kWaves, 0, stream>>>(p);
-    else
-        nt ? qk_norm_rope_backward_kernel<TX, TG, kPlain, true><<<grid, 64 * kWaves, 0, stream>>>(p)
-           : qk_norm_rope_backward_kernel<TX, TG, kPlain, false><<<grid, 64 * kWaves, 0, stream>>>(p);
+    if (p.halves) return nt ? launch_backward<TX, TG, kHalves, true>(p, cus, stream) : launch_backward<TX, TG, kHalves, false>(p, cus, stream);
+    return nt ? launch_backward<TX, TG, kPlain, true>(p, cus, stream) : launch_backward<TX, TG, kPlain, false>(p, cus, stream);
 }
 
 }  // namespace
@@ -369,29 +400,11 @@ hipError_t launch_axial_rope(RopeParams p, bool norm, bool in_f32, bool out_f32,
     return hipGetLastError();
 }
 
-int norm_rope_backward_groups(int cus) { return 4 * cus; }
+int norm_rope_backward_groups(int cus) { return kBackGroups * cus; }
 
-hipError_t launch_qk_norm_rope_backward(RopeParams p, bool x_f32, bool g_f32, int cus, hipStream_t stream) {
-    uint32_t items = 0;
-    bool dw = false;
-    for (int i = 0; i < p.tensors; ++i) {
-        divide(p, p.t[i], kBackRows, cus);  // no tokens: no items, and the weights' gradients are sums of nothing
-        items = std::max(items, p.t[i].items);
-        dw = dw || p.t[i].dw;
-    }
-    const int groups = (int)std::min<int64_t>((items + kWaves - 1) / kWaves, norm_rope_backward_groups(cus));
-    for (int i = 0; i < p.tensors; ++i) p.t[i].parts = groups;
-    const dim3 grid(groups, p.tensors);
-    if (!groups)
-        ;
-    else if (x_f32)
-        g_f32 ? launch_backward<float, float>(p, grid, stream) : launch_backward<float, bf16_t>(p, grid, stream);
-    else
-        g_f32 ? launch_backward<bf16_t, float>(p, grid, stream) : launch_backward<bf16_t, bf16_t>(p, grid, stream);
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || !dw) return e;
-    norm_weight_grad_kernel<<<dim3((p.D + 15) / 16, p.tensors), 1024, 0, stream>>>(p);
-    return hipGetLastError();
+hipError_t launch_qk_norm_rope_backward(const RopeParams& p, bool x_f32, bool g_f32, int cus, hipStream_t stream) {
+    if (x_f32) return g_f32 ? launch_backward<float, float>(p, cus, stream) : launch_backward<float, bf16_t>(p, cus, stream);
+    return g_f32 ? launch_backward<bf16_t, float>(p, cus, stream) : launch_backward<bf16_t, bf16_t>(p, cus, stream);
 }
 
 }  // namespace orbit

@@ -191,7 +191,7 @@ struct RopeParams {
 hipError_t launch_axial_rope(RopeParams p, bool norm, bool in_f32, bool out_f32, int cus, hipStream_t stream);
 // Rows of partial sums that the backward pass may write for each tensor.
 int norm_rope_backward_groups(int cus);
-hipError_t launch_qk_norm_rope_backward(RopeParams p, bool x_f32, bool g_f32, int cus, hipStream_t stream);
+hipError_t launch_qk_norm_rope_backward(const RopeParams& p, bool x_f32, bool g_f32, int cus, hipStream_t stream);
 
 // Low-rank adapters of many requests.
 constexpr int kLoraMaxSplits = 16;  // of the contraction of a few rows
