@@ -273,14 +273,14 @@ constexpr int kTimes = 4;  // rows to a lane in a strip of 16 rows of 256 bytes
 
 // 16 rows of a tile of s h as operands of the expansion: the lane has row i and r = 32 c + 8 q .. + 7.
 template <int RC, int PARTS>
-__device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, int rows, int lane, u32x4 (&h)[RC][PARTS]) {
+__device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, int tile, int rows, int lane, u32x4 (&h)[RC][PARTS]) {
 #pragma unroll
     for (int c = 0; c < RC; ++c) {
         f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
         if (c * 32 < p.R) {
 #pragma unroll 4
             for (int s = 0; s < p.splits; ++s) {
-                const float* const from = p.h + lora_sum(s, gridDim.x, blockIdx.x, rows, c, p.R) + lane * 4;
+                const float* const from = p.h + lora_sum(s, p.count, tile, rows, c, p.R) + lane * 4;
                 lo += *(const f32x4*)from;
                 hi += *(const f32x4*)(from + 256);
             }
@@ -294,12 +294,12 @@ __device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, i
 
 // The same rows for what comes after the expansion: h itself [M][R], and s h in three parts in the order of lora_operand,
 // for which they turn around in the wave's part of LDS.
-__device__ __forceinline__ void copy_h(const LoraExpand& p, const LoraTile& t, int rows, int lane, float* turn, int stride) {
+__device__ __forceinline__ void copy_h(const LoraExpand& p, const LoraTile& t, int tile, int rows, int lane, float* turn, int stride) {
     const int i = lane & 15, q = lane >> 4;
     for (int c = 0; c * 32 < p.R; ++c) {
         f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
         for (int s = 0; s < p.splits; ++s) {
-            const float* const from = p.h + lora_sum(s, gridDim.x, blockIdx.x, rows, c, p.R) + lane * 4;
+            const float* const from = p.h + lora_sum(s, p.count, tile, rows, c, p.R) + lane * 4;
             lo += *(const f32x4*)from;
             hi += *(const f32x4*)(from + 256);
         }
@@ -322,7 +322,7 @@ __device__ __forceinline__ void copy_h(const LoraExpand& p, const LoraTile& t, i
         split8<3>(v, part);
         if (c * 32 + r < p.R) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k) *(u32x4*)(p.turned + lora_operand(blockIdx.x, rows * 16 + first, k, c * 32 + r, p.R)) = part[k];
+            for (int k = 0; k < 3; ++k) *(u32x4*)(p.turned + lora_operand(tile, rows * 16 + first, k, c * 32 + r, p.R)) = part[k];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -343,14 +343,17 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
     constexpr int kZero = kStrip * (RC * 4 + 1);              // the last piece is zero
     __shared__ __align__(16) float turn[kWaves * 16 * kRow];
     __shared__ u32x4 pool_lds[kZero + 1];
-    const LoraTile t = p.tiles[blockIdx.x];
+    // workgroups go to the eight dies in turn: all of a tile's go to one, whose L2 then has the tile's sums
+    const int die = blockIdx.x % 8, at = blockIdx.x / 8, block = at % p.blocks, tile = at / p.blocks * 8 + die;
+    if (tile >= p.count) return;
+    const LoraTile t = p.tiles[tile];
     if (t.rank == 0 && p.base == p.y && p.ldb == p.ldy && !p.sum) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i = lane & 15, q = lane >> 4;
     const int first = wave * 16;
     const int pieces = p.R / 8, stride = pieces | 1;  // of a pool row, in memory and, on all banks, in LDS
     const uint16_t* const pool = p.pool + (int64_t)max(t.adapter, 0) * p.N * p.R;
-    int64_t n0 = (int64_t)blockIdx.y * p.columns;
-    const int64_t end = min((int64_t)(blockIdx.y + 1) * p.columns, p.N);
+    int64_t n0 = (int64_t)block * p.columns;
+    const int64_t end = min(n0 + p.columns, p.N);
     const int64_t last = n0 + (end - n0) / kStrip * kStrip - kStrip;  // the last whole strip (below n0: there is none)
 
     // of this thread: rows 16 wave + q + 4 j of the tile (its last one again beyond its rows), 16 bytes of their columns
@@ -390,8 +393,8 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
     if (last >= n0) load_wide(n0);
     if (t.rank > 0) load_pool(n0);
     u32x4 h[RC][kParts];
-    load_h<RC, kParts>(p, t, wave, lane, h);
-    if (blockIdx.y == 0 && (p.sum || p.turned)) copy_h(p, t, wave, lane, turn + wave * 16 * kRow, kRow);
+    load_h<RC, kParts>(p, t, tile, wave, lane, h);
+    if (block == 0 && (p.sum || p.turned)) copy_h(p, t, tile, wave, lane, turn + wave * 16 * kRow, kRow);
 
     // where the lane's operand pieces lie: those beyond R are the zero one
     if (tid == 0) pool_lds[kZero] = (u32x4){0, 0, 0, 0};
@@ -886,7 +889,9 @@ hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStr
     // 1024 columns to a workgroup, fewer where that leaves less than 4 workgroups to a compute unit
     p.columns = 1024;
     while (p.columns > 128 && tiles * ((p.N + p.columns - 1) / p.columns) < 4 * (int64_t)cus) p.columns /= 2;
-    const dim3 grid(tiles, (unsigned)((p.N + p.columns - 1) / p.columns));
+    p.count = tiles;
+    p.blocks = (int)((p.N + p.columns - 1) / p.columns);
+    const dim3 grid((unsigned)((tiles + 7) / 8 * 8 * p.blocks));
     f32 ? expand<float>(p, grid, stream) : expand<bf16_t>(p, grid, stream);
     return hipGetLastError();
 }
