@@ -140,15 +140,16 @@ __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) 
         };
         const int mine = i * 16 + ((wave * 4 + q) ^ i);
         auto multiply = [&]() __attribute__((always_inline)) {
-            u32x4 row[4];
+            u32x4 row[4], of_a[RF];
 #pragma unroll
             for (int m = 0; m < 4; ++m) row[m] = lds[m * 256 + mine];
 #pragma unroll
-            for (int r = 0; r < RF; ++r) {
-                const u32x4 of_a = lds[kX + r * 256 + mine];
+            for (int r = 0; r < RF; ++r) of_a[r] = lds[kX + r * 256 + mine];
+            __builtin_amdgcn_sched_barrier(0);  // (the compiler would wait for every read)
 #pragma unroll
-                for (int m = 0; m < 4; ++m) acc[m][r] = mfma(row[m], of_a, acc[m][r]);
-            }
+            for (int r = 0; r < RF; ++r)
+#pragma unroll
+                for (int m = 0; m < 4; ++m) acc[m][r] = mfma(row[m], of_a[r], acc[m][r]);
             __syncthreads();
         };
         // every load in this loop comes whether it is needed or not (the last chunk's again), and nothing leaves the loop
@@ -234,8 +235,8 @@ struct Wide<bf16_t> {
     __device__ __forceinline__ void load(const bf16_t* p) { w = load8((const uint16_t*)p); }
     __device__ __forceinline__ void load(const bf16_t* p, int64_t n) { w = load8_part((const uint16_t*)p, n); }
     __device__ __forceinline__ void clear() { w = (u32x4){0, 0, 0, 0}; }
-    __device__ __forceinline__ void add(const float* d) {
-        const f32x4 a = *(const f32x4*)d, b = *(const f32x4*)(d + 4);
+    __device__ __forceinline__ void add(const f32x4* d) {
+        const f32x4 a = d[0], b = d[1];
         w = (u32x4){pack_bf16(bf16_low(w[0]) + a[0], bf16_high(w[0]) + a[1]), pack_bf16(bf16_low(w[1]) + a[2], bf16_high(w[1]) + a[3]),
                     pack_bf16(bf16_low(w[2]) + b[0], bf16_high(w[2]) + b[1]), pack_bf16(bf16_low(w[3]) + b[2], bf16_high(w[3]) + b[3])};
     }
@@ -259,7 +260,7 @@ struct Wide<float> {
         for (int i = 0; i < 4; ++i) w[i] = i < n ? p[i] : 0.f;
     }
     __device__ __forceinline__ void clear() { w = (f32x4){0, 0, 0, 0}; }
-    __device__ __forceinline__ void add(const float* d) { w += *(const f32x4*)d; }
+    __device__ __forceinline__ void add(const f32x4* d) { w += d[0]; }
     __device__ __forceinline__ void store(float* p) const { __builtin_nontemporal_store(w, (f32x4_any*)p); }
     __device__ __forceinline__ void store(float* p, int64_t n) const {
         if (n >= 4) return store(p);
@@ -418,25 +419,42 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
         }
         __syncthreads();
     };
+    // LDS reads go out in groups ahead of the products that take them, and products of different columns follow each
+    // other: left alone, the compiler waits for every read and adds four products to one sum back to back
     auto add = [&]() __attribute__((always_inline)) {
+        constexpr int kGroup = RC == 4 ? 2 : 4;  // of 16 columns
 #pragma unroll
-        for (int f = 0; f < kValues; ++f) {
-            f32x4 acc = {0, 0, 0, 0};
+        for (int f0 = 0; f0 < kValues; f0 += kGroup) {
+            u32x4 b[kGroup][RC];
+            f32x4 acc[kGroup];
 #pragma unroll
-            for (int c = 0; c < RC; ++c) {
-                const u32x4 b = pool_lds[operand[c] + f * next[c]];
+            for (int f = 0; f < kGroup; ++f) {
+                acc[f] = (f32x4){0, 0, 0, 0};
 #pragma unroll
-                for (int k = kParts - 1; k >= 0; --k) acc = mfma(b, h[c][k], acc);
+                for (int c = 0; c < RC; ++c) b[f][c] = pool_lds[operand[c] + (f0 + f) * next[c]];
             }
-            *(f32x4*)(mine + i * kRow + 16 * f + 4 * q) = acc;
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int c = 0; c < RC; ++c)
+#pragma unroll
+                for (int k = kParts - 1; k >= 0; --k)
+#pragma unroll
+                    for (int f = 0; f < kGroup; ++f) acc[f] = mfma(b[f][c], h[c][k], acc[f]);
+#pragma unroll
+            for (int f = 0; f < kGroup; ++f) *(f32x4*)(mine + i * kRow + 16 * (f0 + f) + 4 * q) = acc[f];
         }
         // the wave's own rows of LDS: its accesses stay in order, and the compiler keeps them so
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+        f32x4 delta[kTimes][kValues / 4];
 #pragma unroll
-        for (int j = 0; j < kTimes; ++j) wide[j].add(mine + (q + 4 * j) * kRow + col);
+        for (int j = 0; j < kTimes; ++j)
+#pragma unroll
+            for (int e = 0; e < kValues / 4; ++e) delta[j][e] = *(const f32x4*)(mine + (q + 4 * j) * kRow + col + 4 * e);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int j = 0; j < kTimes; ++j) wide[j].add(delta[j]);
     };
     // a whole tile's strips have no test between their loads and stores, after which the compiler would wait for all
     auto strips = [&](auto whole) __attribute__((always_inline)) {
