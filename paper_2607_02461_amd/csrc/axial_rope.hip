@@ -324,8 +324,13 @@ void divide(const RopeParams& p, RopeTensor& t, int most, int cus) {
 // 117 / 108; but in pieces of 64 bytes 66.8 / 75.
 bool streams(const RopeParams& p, int bytes_each, int smallest) {
     int64_t heads = 0;
-    for (int i = 0; i < p.tensors; ++i) heads += p.t[i].heads;
-    return (int64_t)p.tokens * heads * p.D * bytes_each > (int64_t)160 << 20 && (!p.halves || p.pairs * smallest >= 128);
+    bool lines = !p.halves || p.pairs * smallest >= 128;
+    for (int i = 0; i < p.tensors; ++i) {
+        heads += p.t[i].heads;
+        // a token's heads, where they lie side by side, or a head
+        lines = lines && (p.D * smallest % 128 == 0 || (int64_t)p.t[i].heads * p.D * smallest % 128 == 0);
+    }
+    return lines && (int64_t)p.tokens * heads * p.D * bytes_each > (int64_t)160 << 20;
 }
 
 template <typename TI, typename TO, bool NORM>

@@ -231,6 +231,7 @@ struct LoraExpand {
     void* y;               // [M][ldy] fp32 or bf16
     int64_t ldy;
     uint16_t* turned;      // s h as three bf16 parts for the gradients (lora_operand_bytes), or null
+    int stream;            // y is stored non-temporally (set by the launcher)
     int count, blocks;     // tiles, and workgroups to a tile (set by the launcher)
     int columns;           // to a workgroup, a multiple of 128 (set by the launcher)
 };

@@ -222,9 +222,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) 
     }
 }
 
-// 16 bytes of a row of the wide output and of its base: the first n of their values, or all.  Stores are non-temporal, so
-// that y leaves the caches to what is read next (a training step with 170 MB of y 232 -> 213 us, a call with 1.8 GB 841
-// -> 818; small ones the same).
+// 16 bytes of a row of the wide output and of its base: the first n of their values, or all.  stream: a non-temporal store.
 template <typename T>
 struct Wide;
 
@@ -240,7 +238,8 @@ struct Wide<bf16_t> {
         w = (u32x4){pack_bf16(bf16_low(w[0]) + a[0], bf16_high(w[0]) + a[1]), pack_bf16(bf16_low(w[1]) + a[2], bf16_high(w[1]) + a[3]),
                     pack_bf16(bf16_low(w[2]) + b[0], bf16_high(w[2]) + b[1]), pack_bf16(bf16_low(w[3]) + b[2], bf16_high(w[3]) + b[3])};
     }
-    __device__ __forceinline__ void store(bf16_t* p) const { __builtin_nontemporal_store(w, (u32x4_any*)p); }
+    __device__ __forceinline__ void store(bf16_t* p) const { *(u32x4_any*)p = w; }
+    __device__ __forceinline__ void stream(bf16_t* p) const { __builtin_nontemporal_store(w, (u32x4_any*)p); }
     __device__ __forceinline__ void store(bf16_t* p, int64_t n) const {
         if (n >= 8) return store(p);
 #pragma unroll
@@ -261,7 +260,8 @@ struct Wide<float> {
     }
     __device__ __forceinline__ void clear() { w = (f32x4){0, 0, 0, 0}; }
     __device__ __forceinline__ void add(const f32x4* d) { w += d[0]; }
-    __device__ __forceinline__ void store(float* p) const { __builtin_nontemporal_store(w, (f32x4_any*)p); }
+    __device__ __forceinline__ void store(float* p) const { *(f32x4_any*)p = w; }
+    __device__ __forceinline__ void stream(float* p) const { __builtin_nontemporal_store(w, (f32x4_any*)p); }
     __device__ __forceinline__ void store(float* p, int64_t n) const {
         if (n >= 4) return store(p);
 #pragma unroll
@@ -457,7 +457,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
         for (int j = 0; j < kTimes; ++j) wide[j].add(delta[j]);
     };
     // a whole tile's strips have no test between their loads and stores, after which the compiler would wait for all
-    auto strips = [&](auto whole) __attribute__((always_inline)) {
+    auto strips = [&](auto whole, auto stream) __attribute__((always_inline)) {
         for (; n0 <= last; n0 += kStrip) {
             const int64_t then = min(n0 + kStrip, last);
             if (t.rank > 0) {
@@ -470,15 +470,21 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
             for (int j = 0; j < kTimes; ++j) out[j] = wide[j];
             load_wide(then);
 #pragma unroll
-            for (int j = 0; j < kTimes; ++j)
-                if (whole.value || first + q + 4 * j < t.rows) out[j].store(y[j] + n0);
+            for (int j = 0; j < kTimes; ++j) {
+                if (stream.value)
+                    out[j].stream(y[j] + n0);
+                else if (whole.value || first + q + 4 * j < t.rows)
+                    out[j].store(y[j] + n0);
+            }
             if (t.rank > 0) __syncthreads();
         }
     };
-    if (t.rows == kLoraTileRows)
-        strips(std::true_type{});
+    if (t.rows < kLoraTileRows)
+        strips(std::false_type{}, std::false_type{});
+    else if (p.stream)
+        strips(std::true_type{}, std::true_type{});
     else
-        strips(std::false_type{});
+        strips(std::true_type{}, std::false_type{});
     if (n0 < end) {
         // the last columns; their part of the pool is here or on its way
 #pragma unroll
@@ -907,6 +913,11 @@ hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStr
     // 1024 columns to a workgroup, fewer where that leaves less than 4 workgroups to a compute unit
     p.columns = 1024;
     while (p.columns > 128 && tiles * ((p.N + p.columns - 1) / p.columns) < 4 * (int64_t)cus) p.columns /= 2;
+    // Non-temporal stores leave the caches to what is read next (a training step with 170 MB of y 232 -> 213 us, a call with
+    // 1.8 GB 841 -> 818, small ones the same), where rows are whole lines: 144 MB of rows of 13424 bytes took 69 us, 48 with
+    // plain stores.
+    const int size = f32 ? 4 : 2;
+    p.stream = (uintptr_t)p.y % 128 == 0 && p.ldy * size % 128 == 0;
     p.count = tiles;
     p.blocks = (int)((p.N + p.columns - 1) / p.columns);
     const dim3 grid((unsigned)((tiles + 7) / 8 * 8 * p.blocks));
