@@ -98,7 +98,8 @@ __device__ __forceinline__ int64_t lora_operand(int64_t tile, int row, int k, in
 
 // h partial sums (lora_sum) of rows x [M][K] and pool [adapter][R][K]: a workgroup takes a tile and a split of K, in
 // chunks of 128 that all its waves bring to LDS, the loads of the next two on their way while one is multiplied.  Each wave
-// takes 32 of a chunk's 128 for all rows, so that LDS is read once, and their sums are added at the end.
+// takes 32 of a chunk's 128 for all rows, so that LDS is read once, and their sums are added at the end.  Bound by HBM:
+// 33272 rows of 5120, rank 64, 100 us (3.4 TB/s); 9216 rows of 3072, rank 32, 17.5 us (3.2 TB/s).
 template <int RF>
 __global__ __launch_bounds__(64 * kWaves) void lora_shrink_kernel(LoraShrink p) {
     constexpr int kX = 64 * 16, kA = RF * 16 * 16;                    // pieces of 16 bytes: 16 to a row
@@ -335,7 +336,8 @@ __device__ __forceinline__ void copy_h(const LoraExpand& p, const LoraTile& t, i
 // rows of y, so a lane ends up with four values in a row of 16 rows; they turn around in the wave's own part of LDS, so
 // that base and y are read and written in rows of 256 bytes (a copy of 9216 x 9216 bf16 values runs at 4.8 TB/s so, at
 // 4.2 in 16 rows of 64 bytes).  The next strip's loads are on their way while this one is multiplied, and go out ahead of
-// this one's stores, since loads and stores are waited for in the order of their issue.
+// this one's stores, since loads and stores are waited for in the order of their issue.  Bound by HBM: 33272 x 13824
+// values in fp32, rank 64, 666 us (5.5 TB/s); 9216 x 9216 in bf16, rank 32, 69 us (4.9 TB/s).
 template <typename T, int RC, bool BASE>
 __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) {
     constexpr int kParts = Wide<T>::kParts, kValues = Wide<T>::kValues, kStrip = 16 * kValues;
@@ -503,7 +505,8 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
 // Both products in one kernel for tiles of at most ROWS rows, the single tokens of many requests: bound by launches and
 // latency, and by the pools, which every workgroup streams in rows of 1 KB.  A workgroup takes a tile and p.columns
 // columns; its waves make h for themselves (A comes from L2 for all but the first), each for R / 8 rows of A, in fp32
-// with the lanes along K; then 2^k >= R / 8 lanes share a row of B.
+// with the lanes along K; then 2^k >= R / 8 lanes share a row of B.  16 rows of 16 adapters of rank 16, 3072 -> 18432:
+// 7.2 us for 13 MB, and 17 with the two kernels above and their launches.
 constexpr int kRowWaves = 8, kAhead = 4;  // waves to a workgroup, and groups of rows of B that a wave has on their way
 
 template <int LANES>
@@ -634,7 +637,8 @@ __global__ __launch_bounds__(64 * kRowWaves) void lora_rows_kernel(LoraRows p) {
 }
 
 // What the backward pass reads the other way round: A [R][K] -> [K][R], B [N][R] -> [R][N padded to 8], and s h [M][R] as
-// three bf16 parts in the order of lora_operand.  A thread turns a block of 8 x 8.
+// three bf16 parts in the order of lora_operand.  A thread turns a block of 8 x 8.  9 us for two adapters of rank 32,
+// 3072 -> 9216, and 9216 rows; turned by the kernels that use them instead, a training step takes 230 us and not 203.
 __global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
     // (fewer than 2^31 blocks of 8 x 8 in all)
     const uint32_t r_blocks = p.R / 8, a_blocks = r_blocks * (uint32_t)(p.K / 8), b_blocks = r_blocks * (uint32_t)(p.ldn / 8);
@@ -700,7 +704,8 @@ __global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
 // split, of h and dy (dB) in the rest.  A wave takes steps of 32 rows of 128 columns: a lane loads 8 rows of 8 columns,
 // which transposed are 8 operands with the rows as contraction, each for columns 8 apart.  TOGETHER: the workgroup's waves
 // take every fourth step of the same columns and add their sums in LDS; else they have columns of their own and store
-// their sums themselves, which is faster where a wave has few steps.
+// their sums themselves, which is faster where a wave has few steps.  Bound by HBM: 9216 rows, 3072 -> 9216, rank 32,
+// 49 us (4.6 TB/s of x and dy).
 template <int RF, bool TOGETHER>
 __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
     __shared__ float sums[TOGETHER ? RF * 16 : 1][128 + 4];
@@ -888,7 +893,8 @@ void rows(const LoraRows& p, dim3 grid, hipStream_t stream) {
 
 int lora_splits(int tiles, int64_t K, int cus) {
     // halves of the K range until the workgroups are 2 to a compute unit, each keeping at least 6 chunks of 128: every
-    // workgroup of the expansion reads all splits of its tile
+    // workgroup of the expansion reads all splits of its tile.  1024 rows 3072 -> 12288 of rank 32: 22.1 us, 25.9 with
+    // splits down to one chunk, 29.4 with none below 24; 256 rows 13824 -> 5120 of rank 64: 20.6, 20.6 and 30.3.
     int splits = 1;
     while (splits < kLoraMaxSplits && (int64_t)tiles * splits < 2 * (int64_t)cus && K >= (int64_t)splits * 2 * 6 * 128) splits *= 2;
     return splits;
@@ -910,8 +916,10 @@ hipError_t launch_lora_shrink(LoraShrink p, int tiles, int splits, hipStream_t s
 }
 
 hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStream_t stream) {
-    // 1024 columns to a workgroup, fewer where that leaves less than 4 workgroups to a compute unit
-    p.columns = 1024;
+    // 512 columns to a workgroup, fewer where that leaves less than 4 workgroups to a compute unit (2 or 8: the same to 1%).
+    // 9216 rows, 9216 columns in bf16, rank 32: 86 us, 90 with 256 columns, 108 with 128, 87 with 1024; 33272 rows, 13824
+    // columns in fp32, rank 64: 761, 768, 845 and 788.
+    p.columns = 512;
     while (p.columns > 128 && tiles * ((p.N + p.columns - 1) / p.columns) < 4 * (int64_t)cus) p.columns /= 2;
     // Non-temporal stores leave the caches to what is read next (a training step with 170 MB of y 232 -> 213 us, a call with
     // 1.8 GB 841 -> 818, small ones the same), where rows are whole lines: 144 MB of rows of 13424 bytes took 69 us, 48 with
