@@ -637,13 +637,14 @@ __global__ __launch_bounds__(64 * kRowWaves) void lora_rows_kernel(LoraRows p) {
 }
 
 // What the backward pass reads the other way round: A [R][K] -> [K][R], B [N][R] -> [R][N padded to 8], and s h [M][R] as
-// three bf16 parts in the order of lora_operand.  A thread turns a block of 8 x 8.  9 us for two adapters of rank 32,
-// 3072 -> 9216, and 9216 rows; turned by the kernels that use them instead, a training step takes 230 us and not 203.
-__global__ __launch_bounds__(256) void lora_turn_kernel(LoraTurn p) {
+// three bf16 parts in the order of lora_operand.  A thread turns a block of 8 x 8, and a workgroup is a wave: there are
+// few, bound by latency, and more compute units have some (a training step of 9216 rows, 3072 -> 9216, rank 32: 204 us
+// with workgroups of 256, 201.7 so; 230 where the kernels that use them turn them themselves).
+__global__ __launch_bounds__(64) void lora_turn_kernel(LoraTurn p) {
     // (fewer than 2^31 blocks of 8 x 8 in all)
     const uint32_t r_blocks = p.R / 8, a_blocks = r_blocks * (uint32_t)(p.K / 8), b_blocks = r_blocks * (uint32_t)(p.ldn / 8);
     const uint32_t pools = (a_blocks + b_blocks) * p.adapters;
-    uint32_t at = blockIdx.x * 256 + threadIdx.x;
+    uint32_t at = blockIdx.x * 64 + threadIdx.x;
     if (at < pools) {
         const uint32_t of = at / (a_blocks + b_blocks);
         at -= of * (a_blocks + b_blocks);
@@ -839,16 +840,18 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
 }
 
 // Sums of an adapter's splits, in order (none: zeros): dA [R][K] as it lies, dB [R][N] turned to [N][R].  A thread takes
-// 8 rows of r of one column.
-__global__ __launch_bounds__(256) void lora_grad_sum_kernel(LoraGrad p) {
+// 8 rows of r of one column, of four splits at a time (20480 rows, 3072 -> 3072, rank 16, a training step: 191 us, 195
+// one after another and in workgroups of 256).
+__global__ __launch_bounds__(64) void lora_grad_sum_kernel(LoraGrad p) {
     const int64_t adapter = blockIdx.z;
     const bool second = (int)blockIdx.x >= p.sum_blocks_x;
     const LoraGradSide side = p.side[second];
-    const int64_t n = (int64_t)((int)blockIdx.x - (second ? p.sum_blocks_x : 0)) * 256 + threadIdx.x;
+    const int64_t n = (int64_t)((int)blockIdx.x - (second ? p.sum_blocks_x : 0)) * 64 + threadIdx.x;
     const int r = blockIdx.y * 8;
     if (n >= side.width) return;
     float v[8] = {0, 0, 0, 0, 0, 0, 0, 0};
     const int begin = p.first[adapter], end = p.first[adapter + 1];
+#pragma unroll 4
     for (int s = begin; s < end; ++s) {
         const float* const from = side.part + ((int64_t)s * p.R + r) * side.width + n;
 #pragma unroll
@@ -950,7 +953,7 @@ hipError_t launch_lora_rows(LoraRows p, int tiles, int tile_rows, bool f32, int 
 
 hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream) {
     const int64_t blocks = (int64_t)(p.R / 8) * ((p.K / 8 + p.ldn / 8) * p.adapters + 8 * p.count);
-    lora_turn_kernel<<<(unsigned)((blocks + 255) / 256), 256, 0, stream>>>(p);
+    lora_turn_kernel<<<(unsigned)((blocks + 63) / 64), 64, 0, stream>>>(p);
     return hipGetLastError();
 }
 
@@ -969,9 +972,9 @@ hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, bool together,
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || p.direct) return e;
     }
-    p.sum_blocks_x = (int)((p.side[0].width + 255) / 256);
-    const int sums = p.sum_blocks_x + (int)((p.side[1].width + 255) / 256);
-    lora_grad_sum_kernel<<<dim3(sums, p.R / 8, adapters), 256, 0, stream>>>(p);
+    p.sum_blocks_x = (int)((p.side[0].width + 63) / 64);
+    const int sums = p.sum_blocks_x + (int)((p.side[1].width + 63) / 64);
+    lora_grad_sum_kernel<<<dim3(sums, p.R / 8, adapters), 64, 0, stream>>>(p);
     return hipGetLastError();
 }
 
