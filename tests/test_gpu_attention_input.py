@@ -303,6 +303,25 @@ def test_weight_gradients_have_the_same_bits_every_time_and_at_many_rows():
         assert all(torch.equal(a, b) for a, b in zip(first, oq.qk_norm_rope_backward(plan, dq, dq, q, q, pos, w, w, eps=EPS)))
 
 
+@pytest.mark.parametrize("shape,stride", [((1, 70, 2, 64), (0, 2 ** 26 + 8, 64, 1)), ((2, 3, 2, 64), (64, 2 ** 31 + 8, 2 ** 30, 1))])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_offsets_beyond_32_bits(shape, stride, dtype):
+    plan, pos, _ = _plan_and_positions((16, 24, 16), shape[0], shape[1], 13, False)
+    q, dq = (_rows(shape, dtype, s) for s in (61, 62))
+    w = torch.linspace(0.5, 2.0, 64, device=DEV)
+    size = sum(n * (d - 1) for n, d in zip(stride, shape)) + 1
+
+    def apart(t):
+        return torch.empty(size, dtype=dtype, device=DEV).as_strided(shape, stride).copy_(t)
+
+    far, out = apart(q), apart(torch.zeros_like(q))
+    assert torch.equal(oq.axial_rope(plan, far, pos, out=out), oq.axial_rope(plan, q, pos))
+    assert torch.equal(oq.qk_norm_rope(plan, far, far, pos, w, w, eps=EPS, q_out=out)[0], oq.qk_norm_rope(plan, q, q, pos, w, w, eps=EPS)[0])
+    want = oq.qk_norm_rope_backward(plan, dq, dq, q, q, pos, w, w, eps=EPS)
+    got = oq.qk_norm_rope_backward(plan, apart(dq), dq, far, q, pos, w, w, eps=EPS, q_grad=out)
+    assert torch.equal(out, want[0]) and torch.equal(got[2], want[2])
+
+
 def test_streams_and_graph_replays():
     plan, pos, _ = _plan_and_positions((64, 64), 2, 50, 46, False)
     w = torch.linspace(0.5, 2.0, 128, device=DEV)

@@ -233,6 +233,22 @@ def test_many_adapters():
     b.check_backward(*b.backward())
 
 
+@pytest.mark.parametrize("M,stride", [(70, 2 ** 26 + 8), (3, 2 ** 31 + 1)])
+def test_offsets_beyond_32_bits(M, stride):
+    b = Batch(M, 136, 72, 16, [0, 1], [1, 0], [16, 9], [1.0, 0.5])
+    want = (b.forward(),) + tuple(b.backward())
+
+    def apart(t):
+        wide = torch.empty(stride * (M - 1) + t.shape[1], dtype=t.dtype, device=DEV).as_strided(t.shape, (stride, 1))
+        return wide.copy_(t)
+
+    b.x, b.dy, b.base = apart(b.x), apart(b.dy), apart(b.base)
+    assert torch.equal(b.forward(out=b.base), want[0]) and torch.equal(b.base, want[0])
+    base = apart(torch.zeros_like(want[1]))
+    dx, dA, dB = b.backward(base=base, out=base)
+    assert torch.equal(base, want[1]) and torch.equal(dx, want[1]) and torch.equal(dA, want[2]) and torch.equal(dB, want[3])
+
+
 def test_streams_and_graph_replays():
     b = Batch(300, 520, 264, 16, [0, 100], [0, 1], [16, 9], [1.0, 0.5])
 
