@@ -9,8 +9,9 @@
 //   expand  y (or dx): a narrow matrix times a narrow one, added to the wide base on its way through the registers
 //   grad    dA, dB: contraction over rows, of a wide matrix and a narrow one
 // The matrix cores multiply bf16.  x, dy, A and B are bf16 and their products exact; h and g are fp32 sums and go into
-// the next product as a sum of bf16 values: three where the result is fp32 (all 24 bits of their fraction), two where it
-// is rounded to bf16 (2^-17 of them is lost, below the rounding's 2^-9).  That costs MFMAs and no memory traffic.
+// the next product as a sum of three bf16 values, which have all 24 bits of their fraction.  That costs MFMAs and no
+// memory traffic.  (Two values lose 2^-17 of h: below a bf16 result's own rounding, but not where terms cancel.  They took
+// the same time to 1% up to rank 32, 2% less at rank 64, and 187 for 199 us at rank 128: 9216 rows in bf16, 3072 -> 9216.)
 //
 // A tile is up to 64 rows of one adapter; the plan lists them.  An MFMA operand is 8 values in a row of the contraction for
 // row (or column) lane % 16; loaded as such from rows 128 bytes or more apart, each lane's 16 bytes are a request of their
@@ -54,11 +55,12 @@ __device__ __forceinline__ f32x4 mfma(const u32x4& a, const u32x4& b, const f32x
 // v - hi, and 0 where hi holds v already: of an infinity too
 __device__ __forceinline__ float rest(float v, float hi) { return v == hi ? 0.f : v - hi; }
 
-// v as the sum of PARTS bf16 values, the largest first; v becomes what is left
-template <int PARTS>
+constexpr int kParts = 3;
+
+// v as the sum of kParts bf16 values, the largest first; v becomes what is left
 __device__ __forceinline__ void split8(float* v, u32x4* part) {
 #pragma unroll
-    for (int k = 0; k < PARTS; ++k)
+    for (int k = 0; k < kParts; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint32_t w = pack_bf16(v[2 * i], v[2 * i + 1]);
@@ -92,7 +94,7 @@ __device__ __forceinline__ int64_t lora_sum(int split, int64_t tiles, int64_t ti
 // Where value (row of a tile, r) of part k lies in what the gradients' kernel reads, in the order of its operands: per 32
 // rows, part and 16 r's, 64 lanes of 8 rows.
 __device__ __forceinline__ int64_t lora_operand(int64_t tile, int row, int k, int r, int R) {
-    const int64_t block = ((tile * 2 + row / 32) * 3 + k) * ((R + 15) / 16) + r / 16;
+    const int64_t block = ((tile * 2 + row / 32) * kParts + k) * ((R + 15) / 16) + r / 16;
     return (block * 64 + row % 32 / 8 * 16 + r % 16) * 8 + row % 8;
 }
 
@@ -229,7 +231,7 @@ struct Wide;
 
 template <>
 struct Wide<bf16_t> {
-    static constexpr int kParts = 2, kValues = 8;
+    static constexpr int kValues = 8;
     u32x4 w;
     __device__ __forceinline__ void load(const bf16_t* p) { w = load8((const uint16_t*)p); }
     __device__ __forceinline__ void load(const bf16_t* p, int64_t n) { w = load8_part((const uint16_t*)p, n); }
@@ -251,7 +253,7 @@ struct Wide<bf16_t> {
 
 template <>
 struct Wide<float> {
-    static constexpr int kParts = 3, kValues = 4;
+    static constexpr int kValues = 4;
     f32x4 w;
     __device__ __forceinline__ void load(const float* p) { w = *(const f32x4_any*)p; }
     __device__ __forceinline__ void load(const float* p, int64_t n) {
@@ -274,8 +276,8 @@ struct Wide<float> {
 constexpr int kTimes = 4;  // rows to a lane in a strip of 16 rows of 256 bytes
 
 // 16 rows of a tile of s h as operands of the expansion: the lane has row i and r = 32 c + 8 q .. + 7.
-template <int RC, int PARTS>
-__device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, int tile, int rows, int lane, u32x4 (&h)[RC][PARTS]) {
+template <int RC>
+__device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, int tile, int rows, int lane, u32x4 (&h)[RC][kParts]) {
 #pragma unroll
     for (int c = 0; c < RC; ++c) {
         f32x4 lo = {0, 0, 0, 0}, hi = {0, 0, 0, 0};
@@ -290,7 +292,7 @@ __device__ __forceinline__ void load_h(const LoraExpand& p, const LoraTile& t, i
         float v[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[j] = lo[j] * t.scale, v[j + 4] = hi[j] * t.scale;
-        split8<PARTS>(v, h[c]);
+        split8(v, h[c]);
     }
 }
 
@@ -318,13 +320,13 @@ __device__ __forceinline__ void copy_h(const LoraExpand& p, const LoraTile& t, i
         // lane: r = 16 (lane / 32) + lane % 16 of the 32, rows 8 (lane / 16 % 2) .. + 7 of the 16
         const int r = lane / 32 * 16 + i, first = lane / 16 % 2 * 8;
         float v[8];
-        u32x4 part[3];
+        u32x4 part[kParts];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = turn[(first + j) * stride + r];
-        split8<3>(v, part);
+        split8(v, part);
         if (c * 32 + r < p.R) {
 #pragma unroll
-            for (int k = 0; k < 3; ++k) *(u32x4*)(p.turned + lora_operand(tile, rows * 16 + first, k, c * 32 + r, p.R)) = part[k];
+            for (int k = 0; k < kParts; ++k) *(u32x4*)(p.turned + lora_operand(tile, rows * 16 + first, k, c * 32 + r, p.R)) = part[k];
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -340,7 +342,7 @@ __device__ __forceinline__ void copy_h(const LoraExpand& p, const LoraTile& t, i
 // values in fp32, rank 64, 666 us (5.5 TB/s); 9216 x 9216 in bf16, rank 32, 69 us (4.9 TB/s).
 template <typename T, int RC, bool BASE>
 __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) {
-    constexpr int kParts = Wide<T>::kParts, kValues = Wide<T>::kValues, kStrip = 16 * kValues;
+    constexpr int kValues = Wide<T>::kValues, kStrip = 16 * kValues;
     constexpr int kPieces = kStrip * RC * 4 / (64 * kWaves);  // of 16 bytes of the pool to a thread
     constexpr int kRow = kStrip + 4;
     constexpr int kZero = kStrip * (RC * 4 + 1);              // the last piece is zero
@@ -396,7 +398,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_expand_kernel(LoraExpand p) 
     if (last >= n0) load_wide(n0);
     if (t.rank > 0) load_pool(n0);
     u32x4 h[RC][kParts];
-    load_h<RC, kParts>(p, t, tile, wave, lane, h);
+    load_h<RC>(p, t, tile, wave, lane, h);
     if (block == 0 && (p.sum || p.turned)) copy_h(p, t, tile, wave, lane, turn + wave * 16 * kRow, kRow);
 
     // where the lane's operand pieces lie: those beyond R are the zero one
@@ -692,12 +694,12 @@ __global__ __launch_bounds__(64) void lora_turn_kernel(LoraTurn p) {
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        u32x4 part[3];
+        u32x4 part[kParts];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[e][j] = r + e < t.rank ? v[e][j] : 0.f;
-        split8<3>(v[e], part);
+        split8(v[e], part);
 #pragma unroll
-        for (int k = 0; k < 3; ++k) *(u32x4*)(p.turned + lora_operand(tile, first, k, r + e, p.R)) = part[k];
+        for (int k = 0; k < kParts; ++k) *(u32x4*)(p.turned + lora_operand(tile, first, k, r + e, p.R)) = part[k];
     }
 }
 
@@ -732,7 +734,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
         for (int j = 0; j < 8; ++j) acc[r][j] = (f32x4){0, 0, 0, 0};
     // two steps on their way; a load comes whether it is needed or not (the split's last step again), since after a branch
     // around one the compiler waits for all of them
-    u32x4 z[2][8], part[2][RF][3];
+    u32x4 z[2][8], part[2][RF][kParts];
     int mine[2], rows[2];  // the lane's first row of the step's tile, and the tile's rows
     auto load = [&](int d, int step, auto whole) __attribute__((always_inline)) {
         const LoraTile t = p.tiles[step / 2];
@@ -747,7 +749,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
         for (int r = 0; r < RF; ++r) {
             const int frag = min(r0 / 16 + r, (p.R - 1) / 16);
 #pragma unroll
-            for (int k = 0; k < 3; ++k) part[d][r][k] = *(const u32x4*)(side.narrow + lora_operand(step / 2, (step & 1) * 32, k, frag * 16, p.R) + lane * 8);
+            for (int k = 0; k < kParts; ++k) part[d][r][k] = *(const u32x4*)(side.narrow + lora_operand(step / 2, (step & 1) * 32, k, frag * 16, p.R) + lane * 8);
         }
     };
     auto multiply = [&](int d, int step) __attribute__((always_inline)) {
@@ -759,7 +761,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
 #pragma unroll
             for (int r = 0; r < RF; ++r)
 #pragma unroll
-                for (int k = 0; k < 3; ++k)
+                for (int k = 0; k < kParts; ++k)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         part[d][r][k][j] &= (mine[d] + 2 * j < rows[d] ? 0xFFFFu : 0u) | (mine[d] + 2 * j + 1 < rows[d] ? 0xFFFF0000u : 0u);
@@ -768,7 +770,7 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
 #pragma unroll
         for (int r = 0; r < RF; ++r)
 #pragma unroll
-            for (int k = 2; k >= 0; --k)
+            for (int k = kParts - 1; k >= 0; --k)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) acc[r][j] = mfma(part[d][r][k], z[d][j], acc[r][j]);
     };

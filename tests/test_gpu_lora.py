@@ -409,3 +409,56 @@ def test_ways_of_the_gradients(M, K, N, R, starts, adapters, ways):
         over = ((got.double() - ref).abs() - (bar * ref.abs() + (2.0 ** -16 + more) * size + 2 * U * ref.abs())).max()
         assert float(over) <= 0.0, f"{name}: {float(over)} beyond its bar"
     assert any(r.kernel == ways for r in launches(lambda: b.backward(out=dx)))
+
+
+# --- all bits of the narrow sums ------------------------------------------------------------------
+# 1 + 2^-10 + 2^-20 takes three bf16 values: what a result keeps of it once 1 + 2^-10 is taken off again is 2^-20, exactly,
+# in sums of any order (every partial sum has at most 22 bits), and nothing at all where only two values were multiplied
+WHOLE = 1 + 2.0 ** -10 + 2.0 ** -20
+ALL = slice(None)
+
+
+def _set(shape, *values):
+    t = torch.zeros(shape, dtype=BF16, device=DEV)
+    for at, v in values:
+        t[at] = v
+    return t
+
+
+@pytest.mark.parametrize("M", [3, 70, 200])
+@pytest.mark.parametrize("R,first,second", [(8, 0, 7), (32, 3, 20), (48, 1, 40), (64, 40, 50), (128, 2, 127), (128, 70, 71)])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_results_have_all_bits_of_h(M, R, first, second, dtype):
+    K, N = 264, 300
+    plan = oq.lora_plan(M, [0], [0], [R], [0.5])
+    x = _set((M, K), ((ALL, 0), 1.0), ((ALL, 130), 2.0 ** -10), ((ALL, 263), 2.0 ** -20))
+    A = _set((1, R, K), ((0, first), 1.0), ((0, second, 0), 1.0), ((0, second, 130), 1.0))
+    B = _set((1, N, R), ((0, ALL, first), 1.0), ((0, ALL, second), -1.0))
+    h = torch.empty((M, R), dtype=F32, device=DEV)
+    y = oq.lora_add(plan, x, A, B, torch.zeros((M, N), dtype=dtype, device=DEV), h=h)
+    assert (h[:, first] == WHOLE).all() and (h[:, second] == 1 + 2.0 ** -10).all()
+    assert (y == 0.5 * 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("M", [3, 70, 2000])
+@pytest.mark.parametrize("R,first,second", [(8, 0, 7), (32, 3, 20), (48, 1, 40), (64, 40, 50), (128, 2, 127), (128, 70, 71)])
+def test_gradients_have_all_bits_of_h_and_g(M, R, first, second):
+    K, N = 264, 300
+    plan = oq.lora_plan(M, [0], [0], [R], [0.5])
+    dy = _set((M, N), ((ALL, 0), 1.0), ((ALL, 130), 2.0 ** -10), ((ALL, 299), 2.0 ** -20))
+    B = _set((1, N, R), ((0, ALL, first), 1.0), ((0, 0, second), 1.0), ((0, 130, second), 1.0))
+    A = _set((1, R, K), ((0, first), 1.0), ((0, second), -1.0))
+    one, x = torch.zeros((M, R), dtype=F32, device=DEV), torch.zeros((M, K), dtype=BF16, device=DEV)
+    dx, _, _ = oq.lora_add_backward(plan, dy, x, A, B, one)
+    assert (dx == 0.5 * 2.0 ** -20).all()
+    # two rows whose contributions differ in the last bits alone
+    last = M - 1
+    dy[1:last], dy[last], x[0], x[last] = 0.0, -dy[0], 1.0, 1.0
+    dy[last, 299] = 0.0
+    _, dA, _ = oq.lora_add_backward(plan, dy, x, A, B, one)
+    assert (dA[0, first] == 0.5 * 2.0 ** -20).all()
+    one[0, first], one[last, first] = WHOLE, 1 + 2.0 ** -10
+    dy.zero_()
+    dy[0], dy[last] = 1.0, -1.0
+    _, _, dB = oq.lora_add_backward(plan, dy, x, A, B, one)
+    assert (dB[0, :, first] == 0.5 * 2.0 ** -20).all()
