@@ -791,6 +791,14 @@ __global__ __launch_bounds__(64 * kWaves) void lora_grad_kernel(LoraGrad p) {
         steps(std::true_type{});
     else
         steps(std::false_type{});
+    // a row of g or h beyond the rank is zero, and its sums are zero too where a value of x or dy is not finite
+    const int rank = split.begin < split.end ? p.tiles[split.begin].rank : 0;
+#pragma unroll
+    for (int r = 0; r < RF; ++r)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[r][j][k] = r0 + r * 16 + kg * 4 + k < rank ? acc[r][j][k] : 0.f;
     if (!TOGETHER) {
         // the lane has 8 columns in a row of rows q * 4 + k of each 16
 #pragma unroll

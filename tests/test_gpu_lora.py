@@ -462,3 +462,40 @@ def test_gradients_have_all_bits_of_h_and_g(M, R, first, second):
     dy[0], dy[last] = 1.0, -1.0
     _, _, dB = oq.lora_add_backward(plan, dy, x, A, B, one)
     assert (dB[0, :, first] == 0.5 * 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("M,K,N,R,ways", [(100, 128, 96, 8, "lora_grad_kernel<1,true>"), (1000, 256, 392, 16, "lora_grad_kernel<1,false>"),
+                                          (16384 + 40, 2048, 2056, 8, "lora_grad_kernel<1,true>"), (300, 520, 770, 128, "lora_grad_kernel<4,true>"),
+                                          (1500, 520, 770, 96, "lora_grad_kernel<4,false>")])
+def test_gradients_beyond_the_ranks_are_zeros_whatever_x_and_dy_hold(M, K, N, R, ways):
+    ranks, half = [R - 3, R], M // 2
+    b = Batch(M, K, N, R, [0, half], [0, 1], ranks, [0.5, -1.0])
+    b.forward()
+    want = b.backward()
+    b.x[3, 7], b.x[half - 1, K - 1] = float("nan"), float("inf")
+    b.dy[5, 2], b.dy[half - 2, N - 1] = float("-inf"), float("nan")
+    dx, dA, dB = b.backward()
+    hit = torch.zeros(M, dtype=torch.bool, device=DEV)
+    hit[5] = hit[half - 2] = True
+    # the rows that hold them, their columns of the adapter's own gradients (dA's all: g of those rows is not finite), and no more
+    assert torch.equal(dx[~hit], want[0][~hit]) and not torch.isfinite(dx[hit]).any()
+    assert not torch.isfinite(dA[0, :R - 3]).any() and (dA[0, R - 3:] == 0).all() and torch.equal(dA[1], want[1][1])
+    poisoned = torch.zeros(N, dtype=torch.bool, device=DEV)
+    poisoned[2] = poisoned[N - 1] = True
+    assert not torch.isfinite(dB[0, poisoned, :R - 3]).any() and torch.equal(dB[0, ~poisoned], want[2][0, ~poisoned])
+    assert (dB[0, :, R - 3:] == 0).all() and torch.equal(dB[1], want[2][1])
+    assert any(r.kernel == ways for r in launches(lambda: b.backward(out=dx)))
+
+
+def test_gradients_of_rows_that_are_not_finite_stay_with_them():
+    b = Batch(100, 128, 96, 8, [0, 40], [0, 1], [8, 5], [1.0, 1.0], F32)
+    b.forward()
+    want = b.backward()
+    b.dy[3, 2], b.dy[41, 2], b.dy[99, 1] = float("nan"), float("inf"), float("nan")
+    dx, dA, dB = b.backward()
+    clean = torch.ones(100, dtype=torch.bool, device=DEV)
+    clean[3] = clean[41] = clean[99] = False
+    assert torch.equal(dx[clean], want[0][clean]) and not torch.isfinite(dx[~clean]).any()
+    assert not torch.isfinite(dA[0]).any() and not torch.isfinite(dA[1, :5]).any() and (dA[1, 5:] == 0).all()
+    assert not torch.isfinite(dB[0, 2]).any() and not torch.isfinite(dB[1, 1:3, :5]).any() and (dB[1, :, 5:] == 0).all()
+    assert torch.equal(dB[0, 3:], want[2][0, 3:]) and torch.equal(dB[1, 3:], want[2][1, 3:])
