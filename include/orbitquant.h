@@ -513,7 +513,8 @@ orbit_status lora_add_workspace_size(orbit_lora p, int64_t K, int64_t N, int32_t
  * and Y[m] = base[m] for rows without one.  X A^T is a sum in fp32 of exact products and enters the
  * second product with all bits of its fraction; that product accumulates in fp32 again, and Y is rounded
  * once.  The order of a row's sums goes by the batch's largest tile of rows and by the sizes, so its last
- * bits may differ where it comes with other rows.
+ * bits may differ where it comes with other rows.  Values that depend on an infinity or a NaN are not
+ * finite; an infinity may come out as a NaN.
  *   X      device, bf16 [M][ldx]: the projection's input
  *   A, B   device, bf16 [n_adapters][R][K] and [n_adapters][N][R]; R a multiple of 8 up to 128 and at
  *          least every rank.  What lies beyond an adapter's rank does not matter

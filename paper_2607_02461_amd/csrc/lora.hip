@@ -57,13 +57,14 @@ __device__ __forceinline__ float rest(float v, float hi) { return v == hi ? 0.f 
 
 constexpr int kParts = 3;
 
-// v as the sum of kParts bf16 values, the largest first; v becomes what is left
+// v as the sum of kParts bf16 values, the largest first; v becomes what is left.  Each is cut off after its 8 bits and
+// not rounded: the next one has what follows, and a value above bf16's largest does not become an infinity.
 __device__ __forceinline__ void split8(float* v, u32x4* part) {
 #pragma unroll
     for (int k = 0; k < kParts; ++k)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t w = pack_bf16(v[2 * i], v[2 * i + 1]);
+            const uint32_t w = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302u);
             part[k][i] = w;
             v[2 * i] = rest(v[2 * i], bf16_low(w));
             v[2 * i + 1] = rest(v[2 * i + 1], bf16_high(w));

@@ -499,3 +499,34 @@ def test_gradients_of_rows_that_are_not_finite_stay_with_them():
     assert not torch.isfinite(dA[0]).any() and not torch.isfinite(dA[1, :5]).any() and (dA[1, 5:] == 0).all()
     assert not torch.isfinite(dB[0, 2]).any() and not torch.isfinite(dB[1, 1:3, :5]).any() and (dB[1, :, 5:] == 0).all()
     assert torch.equal(dB[0, 3:], want[2][0, 3:]) and torch.equal(dB[1, 3:], want[2][1, 3:])
+
+
+@pytest.mark.parametrize("M", [3, 70, 2000])
+@pytest.mark.parametrize("R", [8, 128])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_sums_above_the_largest_bf16_value(M, R, dtype):
+    # h and g of (2 - 2^-7) 2^127 + 2^119 + 2^118, which fp32 holds and whose nearest bf16 value is an infinity
+    K, N, large = 264, 300, (2 - 2.0 ** -7) * 2.0 ** 127 + 2.0 ** 119 + 2.0 ** 118
+    parts = ((ALL, 0), (2 - 2.0 ** -7) * 2.0 ** 127), ((ALL, 130), 2.0 ** 119), ((ALL, 263), 2.0 ** 118)
+    plan = oq.lora_plan(M, [0], [0], [R], [1.0])
+    x, dy = _set((M, K), *parts), _set((M, N), *parts)
+    wide_a, wide_b = _set((1, R, K), ((0, 1), 1.0)), _set((1, N, R), ((0, ALL, 1), 1.0))
+    thin_a, thin_b = _set((1, R, K), ((0, 1), 2.0 ** -100)), _set((1, N, R), ((0, ALL, 1), 2.0 ** -100))
+    h = torch.empty((M, R), dtype=F32, device=DEV)
+    y = oq.lora_add(plan, x, wide_a, thin_b, torch.zeros((M, N), dtype=dtype, device=DEV), h=h)
+    assert (h[:, 1] == large).all()
+    want = torch.tensor(large * 2.0 ** -100, dtype=F32, device=DEV)
+    assert (y == want.to(dtype)).all()
+    if dtype == F32:
+        return
+    dx, _, _ = oq.lora_add_backward(plan, dy, x, thin_a, wide_b, h)
+    assert (dx == want.to(BF16)).all()
+    # one row's g and h alone
+    x.zero_()
+    dy[1:] = 0.0
+    x[0] = 2.0 ** -100
+    _, dA, _ = oq.lora_add_backward(plan, dy, x, thin_a, wide_b, h)
+    assert (dA[0, 1] == want).all()
+    dy[0] = 2.0 ** -100
+    _, _, dB = oq.lora_add_backward(plan, dy, x, thin_a, wide_b, h)
+    assert (dB[0, :, 1] == want).all()
