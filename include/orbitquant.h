@@ -544,7 +544,8 @@ orbit_status lora_add(orbit_lora p, const uint16_t* X, int64_t ldx, const uint16
  *   dX     device, bf16 [M][lddx]; may be base with the same row stride
  *   dA, dB device, fp32 [n_adapters][R][K] and [n_adapters][N][R]: every element is written, zeros beyond
  *          the ranks and for adapters without rows
- * Other arguments, limits and errors as for lora_add.  M = 0 gives zeros in dA and dB.
+ * Other arguments, limits and errors as for lora_add; ORBIT_EUNSUPPORTED also where the adapters' gradients, or the tiles of
+ * 64 rows, are too many for one launch.  M = 0 gives zeros in dA and dB.
  */
 orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, const uint16_t* X, int64_t ldx,
                                const uint16_t* A, const uint16_t* B, const float* h, int64_t K, int64_t N, int32_t R,

@@ -935,6 +935,8 @@ hipError_t launch_lora_expand(LoraExpand p, int tiles, bool f32, int cus, hipStr
     // columns in fp32, rank 64: 761, 768, 845 and 788.
     p.columns = 512;
     while (p.columns > 128 && tiles * ((p.N + p.columns - 1) / p.columns) < 4 * (int64_t)cus) p.columns /= 2;
+    // a grid holds fewer than 2^32 threads: more columns to a workgroup where many short requests would pass that
+    while ((tiles + 7) / 8 * 8 * ((p.N + p.columns - 1) / p.columns) >= ((int64_t)1 << 32) / (64 * kWaves)) p.columns *= 2;
     // Non-temporal stores leave the caches to what is read next (a training step with 170 MB of y 232 -> 213 us, a call with
     // 1.8 GB 841 -> 818, small ones the same), where rows are whole lines: 144 MB of rows of 13424 bytes took 69 us, 48 with
     // plain stores.

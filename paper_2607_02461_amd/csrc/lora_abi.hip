@@ -15,7 +15,7 @@ using namespace orbit;
 namespace {
 
 constexpr int64_t kMaxRows = INT32_MAX;
-constexpr int64_t kMaxTiles = (int64_t)1 << 22;  // launch grids stay below 2^32 threads
+constexpr int64_t kMaxTiles = (int64_t)1 << 22;  // workgroups of up to 512 threads, one to a tile, stay below 2^32 threads
 constexpr int64_t kMaxWidth = (int64_t)1 << 21;
 constexpr int32_t kMaxAdapters = 65535;
 

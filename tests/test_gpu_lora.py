@@ -530,3 +530,22 @@ def test_sums_above_the_largest_bf16_value(M, R, dtype):
     dy[0] = 2.0 ** -100
     _, _, dB = oq.lora_add_backward(plan, dy, x, thin_a, wide_b, h)
     assert (dB[0, :, 1] == want).all()
+
+
+def test_many_short_requests_on_wide_rows():
+    # more tiles times columns than a grid of 512 columns to a workgroup holds; every request's row is one of B's columns
+    M, K, N = 467_000, 8, 18432
+    starts = list(range(M - 4))                                  # the last request has 5 rows
+    adapters = [i % 2 for i in range(M - 4)]
+    plan = oq.lora_plan(M, starts, adapters, [8, 8], [1.0, 1.0])
+    m = torch.arange(M, device=DEV)
+    x = torch.nn.functional.one_hot(m % 8, 8).to(BF16)
+    A = torch.eye(8, dtype=BF16, device=DEV).expand(2, 8, 8).contiguous()
+    n, r = torch.arange(N, device=DEV)[:, None], torch.arange(8, device=DEV)
+    B = torch.stack([((n + 3 * r + 5 * a) % 101).to(BF16) for a in range(2)])
+    y = torch.zeros((M, N), dtype=BF16, device=DEV)
+    oq.lora_add(plan, x, A, B, y, out=y)
+    rows = B.transpose(1, 2).reshape(16, N)
+    which = torch.tensor(adapters + adapters[-1:] * 4, device=DEV) * 8 + m % 8
+    for at in range(0, M, 8192):
+        assert torch.equal(y[at:at + 8192], rows[which[at:at + 8192]])
