@@ -35,6 +35,7 @@ constexpr int kRows = 6;       // head rows that a wave's lanes have in flight
 constexpr int kBackRows = 3;   // the same for the backward pass, which reads two tensors, where heads are few
 constexpr int kWaves = 4;      // waves to a workgroup
 constexpr int kBackGroups = 8; // most workgroups of the backward pass to a compute unit
+constexpr uint32_t kMostItems = 1u << 25;  // waves of one launch
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_add(float v) {
@@ -183,7 +184,7 @@ template <typename TI, typename TO, bool NORM, int LAY, bool NT>
 __global__ __launch_bounds__(64 * kWaves) void axial_rope_kernel(RopeParams p) {
     const RopeTensor& t = p.t[blockIdx.y];
     const int lane = threadIdx.x & 63;
-    const uint32_t item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint32_t item = p.first_item + blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= t.items) return;
     const Lane<LAY> me(p, lane);
     const Item it(p, t, item, lane);
@@ -401,14 +402,19 @@ hipError_t launch_axial_rope(RopeParams p, bool norm, bool in_f32, bool out_f32,
         divide(p, p.t[i], kRows, cus);
         items = std::max(items, p.t[i].items);
     }
-    const dim3 grid((items + kWaves - 1) / kWaves, p.tensors);
-    if (!norm)
-        in_f32 ? launch<float, float, false>(p, grid, stream) : launch<bf16_t, bf16_t, false>(p, grid, stream);
-    else if (in_f32)
-        out_f32 ? launch<float, float, true>(p, grid, stream) : launch<float, bf16_t, true>(p, grid, stream);
-    else
-        out_f32 ? launch<bf16_t, float, true>(p, grid, stream) : launch<bf16_t, bf16_t, true>(p, grid, stream);
-    return hipGetLastError();
+    // a grid holds fewer than 2^32 threads, which more than 2^26 items of a wave each pass
+    for (p.first_item = 0; p.first_item < items; p.first_item += kMostItems) {
+        const dim3 grid((std::min(items - p.first_item, kMostItems) + kWaves - 1) / kWaves, p.tensors);
+        if (!norm)
+            in_f32 ? launch<float, float, false>(p, grid, stream) : launch<bf16_t, bf16_t, false>(p, grid, stream);
+        else if (in_f32)
+            out_f32 ? launch<float, float, true>(p, grid, stream) : launch<float, bf16_t, true>(p, grid, stream);
+        else
+            out_f32 ? launch<bf16_t, float, true>(p, grid, stream) : launch<bf16_t, bf16_t, true>(p, grid, stream);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
 }
 
 int norm_rope_backward_groups(int cus) { return kBackGroups * cus; }

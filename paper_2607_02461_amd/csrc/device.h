@@ -185,9 +185,10 @@ struct RopeParams {
     int D, lanes;           // head size, and the lanes that share a head: a power of two, at least D / 8
     int halves;             // a pair is (p, p + pairs) and not (2p, 2p + 1)
     float sign, eps, inv_d;
+    uint32_t first_item;    // of a launch (set by the launcher)
 };
 
-// Grids hold one wave per item, items at most tokens * heads < 2^31.
+// One wave per item, items at most tokens * heads < 2^31, in as many launches as that takes.
 hipError_t launch_axial_rope(RopeParams p, bool norm, bool in_f32, bool out_f32, int cus, hipStream_t stream);
 // Rows of partial sums that the backward pass may write for each tensor.
 int norm_rope_backward_groups(int cus);

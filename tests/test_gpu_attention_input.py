@@ -447,3 +447,21 @@ def test_large_tensors(dtype, out, halves, D, dims):
     within(gq, r * (t * w64 - x64 * r * r * dot), r * (length + x64.abs() * r * r * (length * x64.abs()).mean(-1, keepdim=True)), dtype)
     terms = (_device_pair_length(t, P, halves) * x64.abs() * r).sum((0, 1, 2))
     assert ((dw.double() - (t * x64 * r).sum((0, 1, 2))).abs() <= (10 * (L * H) ** 0.5 + 32) * U * terms).all()
+
+
+def test_more_waves_than_a_launch_holds():
+    # heads of 264 values take a wave each: 2^26 of them and a few more, from one row of each of 40 positions
+    L, D = 2 ** 26 + 5, 264
+    plan = oq.rope_plan((264,), (40,))
+    x = _rows((1, 1, 1, D), BF16, 95)
+    pos = (torch.arange(L, device=DEV) % 40).to(torch.int32)[:, None]
+    w = torch.linspace(0.5, 2.0, D, device=DEV)
+    few = x.expand(1, 40, 1, D)
+    out = torch.empty((1, L, 1, D), dtype=BF16, device=DEV)
+    for call in (lambda x, p, y: oq.axial_rope(plan, x, p, out=y), lambda x, p, y: oq.qk_norm_rope(plan, x, None, p, w, eps=EPS, q_out=y)[0]):
+        want = call(few, pos[:40].contiguous(), None)[0]
+        out.zero_()
+        call(x.expand(1, L, 1, D), pos, out)
+        for at in range(0, L, 40 << 16):
+            got = out[0, at:at + (40 << 16)]
+            assert torch.equal(got, want.repeat((got.shape[0] + 39) // 40, 1, 1)[:got.shape[0]])
