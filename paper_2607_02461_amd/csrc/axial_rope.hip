@@ -326,24 +326,33 @@ void divide(const RopeParams& p, RopeTensor& t, int most, int cus) {
     t.items = (uint32_t)(token_groups * t.chunks);
 }
 
+// Whether what a tensor has in one place is whole lines of 128 bytes: a head's row, or a token's heads where they lie
+// together (with less than a row between them).
+bool whole_lines(const HeadRows& r, int heads, int D, int size) {
+    return D * size % 128 == 0 || (r.h < 2 * D && (int64_t)heads * D * size % 128 == 0);
+}
+
 // Non-temporal loads and stores where a call moves more than the memory-side cache keeps for the next kernel, in pieces
 // of whole lines.  Measured plain / non-temporal, us: 100 MB 18.4 / 20.8, 227 MB 51.7 / 46.2, 340 MB 62.6 / 58, 671 MB
-// 117 / 108; but in pieces of 64 bytes 66.8 / 75.
-bool streams(const RopeParams& p, int bytes_each, int smallest) {
+// 117 / 108; but in pieces of 64 bytes 66.8 / 75, and 24 heads of 80 that lie apart, [batch][head][token], 339 MB 77.5 / 92,
+// 699 MB 141 / 170.  Where a piece begins in a line does not matter (24 heads of 80 from 16 bytes behind one on, 699 MB
+// 130 / 131, their gradients 262 / 258), nor 16 bytes between heads (240 / 223).  size_g: of the gradients' values, or 0.
+bool streams(const RopeParams& p, int size_x, int size_y, int size_g) {
     int64_t heads = 0;
-    bool lines = !p.halves || p.pairs * smallest >= 128;
+    bool lines = !p.halves || p.pairs * std::min({size_x, size_y, size_g ? size_g : size_x}) >= 128;
     for (int i = 0; i < p.tensors; ++i) {
-        heads += p.t[i].heads;
-        // a token's heads, where they lie side by side, or a head
-        lines = lines && (p.D * smallest % 128 == 0 || (int64_t)p.t[i].heads * p.D * smallest % 128 == 0);
+        const RopeTensor& t = p.t[i];
+        heads += t.heads;
+        lines = lines && whole_lines(t.x, t.heads, p.D, size_x) && whole_lines(t.y, t.heads, p.D, size_y) &&
+                (!size_g || whole_lines(t.g, t.heads, p.D, size_g));
     }
-    return lines && (int64_t)p.tokens * heads * p.D * bytes_each > (int64_t)160 << 20;
+    return lines && (int64_t)p.tokens * heads * p.D * (size_x + size_y + size_g) > (int64_t)160 << 20;
 }
 
 template <typename TI, typename TO, bool NORM>
 void launch(const RopeParams& p, dim3 grid, hipStream_t stream) {
     constexpr int kPlain = sizeof(TI) + sizeof(TO) == 4 ? kRow : kApart;
-    const bool nt = streams(p, sizeof(TI) + sizeof(TO), std::min(sizeof(TI), sizeof(TO)));
+    const bool nt = streams(p, sizeof(TI), sizeof(TO), 0);
     if (p.halves)
         nt ? axial_rope_kernel<TI, TO, NORM, kHalves, true><<<grid, 64 * kWaves, 0, stream>>>(p)
            : axial_rope_kernel<TI, TO, NORM, kHalves, false><<<grid, 64 * kWaves, 0, stream>>>(p);
@@ -389,7 +398,7 @@ hipError_t launch_backward(RopeParams p, int cus, hipStream_t stream) {
 template <typename TX, typename TG>
 hipError_t launch_backward(const RopeParams& p, int cus, hipStream_t stream) {
     constexpr int kPlain = sizeof(TX) + sizeof(TG) == 4 ? kRow : kApart;
-    const bool nt = streams(p, 2 * sizeof(TX) + sizeof(TG), std::min(sizeof(TX), sizeof(TG)));
+    const bool nt = streams(p, sizeof(TX), sizeof(TX), sizeof(TG));
     if (p.halves) return nt ? launch_backward<TX, TG, kHalves, true>(p, cus, stream) : launch_backward<TX, TG, kHalves, false>(p, cus, stream);
     return nt ? launch_backward<TX, TG, kPlain, true>(p, cus, stream) : launch_backward<TX, TG, kPlain, false>(p, cus, stream);
 }

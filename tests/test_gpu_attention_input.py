@@ -9,12 +9,15 @@ five products.  Weight gradients are sums of n terms: 10 sqrt(n) u sum|terms| (H
 2019, lambda = 10) + 32 u sum|terms|.
 """
 
+import re
+
 import numpy as np
 import pytest
 import torch
 
 import oracle
 import paper_2607_02461_amd as oq
+from paper_2607_02461_amd import launches as launches_module
 
 pytestmark = pytest.mark.gpu
 
@@ -465,3 +468,36 @@ def test_more_waves_than_a_launch_holds():
         for at in range(0, L, 40 << 16):
             got = out[0, at:at + (40 << 16)]
             assert torch.equal(got, want.repeat((got.shape[0] + 39) // 40, 1, 1)[:got.shape[0]])
+
+
+def _instances(call):
+    """(kernel, layout, non-temporal, rows in flight or None, grid) of each rotation that the call launches, off its mangled name."""
+    with pytest.MonkeyPatch.context() as patch:
+        patch.setattr(launches_module, "short_name", str)
+        found = [(re.search(r"\d\d((?:axial|qk)_\w*?kernel)I.*?Li(\d)ELb([01])E(?:Li(\d)E)?EEvNS", r.kernel), r.grid) for r in launches_module.launches(call)]
+    return [(m[1], int(m[2]), m[3] == "1", m[4] and int(m[4]), grid) for m, grid in found if m]
+
+
+@pytest.mark.parametrize("D,dims,layout,streams", [(80, (40, 40), "dense", True), (80, (40, 40), "padded", True), (80, (40, 40), "heads", False),
+                                                   (128, (64, 64), "heads", True), (160, (64, 64), "dense", False)])
+def test_non_temporal_accesses_go_by_what_lies_together(D, dims, layout, streams):
+    # above 160 MiB in and out; heads of 80 values are no whole lines, 24 of a token are; nor are 9 heads of 160
+    H = 9 if D == 160 else 24
+    L = (170 << 20) // (H * D * 4) + 1
+    plan, pos, _ = _plan_and_positions(dims, 1, L, 96, False)
+    q, dq = _rows((1, L, H, D), BF16, 97), _rows((1, L, H, D), BF16, 98)
+    want = oq.qk_norm_rope(plan, q, None, pos)[0], oq.qk_norm_rope_backward(plan, dq, None, q, None, pos)[0]
+
+    def lay(t):
+        if layout == "heads":
+            return t.transpose(1, 2).contiguous().transpose(1, 2)
+        return torch.nn.functional.pad(t, (8, 0))[..., 8:] if layout == "padded" else t
+
+    q, dq, y = lay(q), lay(dq), lay(torch.zeros_like(q))
+    forward = lambda: oq.qk_norm_rope(plan, q, None, pos, q_out=y)  # noqa: E731
+    backward = lambda: oq.qk_norm_rope_backward(plan, dq, None, q, None, pos, q_grad=y)  # noqa: E731
+    for call, ref, name in ((forward, want[0], "axial_rope_kernel"), (backward, want[1], "qk_norm_rope_backward_kernel")):
+        call()
+        assert torch.equal(y, ref)
+        (kernel, _, non_temporal, _, _), = _instances(call)
+        assert kernel == name and non_temporal == streams
