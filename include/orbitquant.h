@@ -385,7 +385,9 @@ typedef struct orbit_rope_s* orbit_rope;
  * strides in elements, ORBIT_OUT_F32 or ORBIT_OUT_BF16 values.  A view of a fused projection's
  * output (queries, keys and values side by side) or of an attention layout ([batch][head][token])
  * is such rows.  The data and the strides (of dimensions with more than one entry) are multiples of
- * 16 bytes.  Strides of inputs may be 0 (broadcast); rows of an output must not overlap.
+ * 16 bytes.  Strides of inputs may be 0 (broadcast); rows of an output must not overlap.  An output may
+ * replace its own input (same data, strides and type, as stated at each call) and overlaps no other
+ * operand; one that begins where another input or output does is refused.
  */
 typedef struct {
     void* data;
@@ -520,7 +522,7 @@ orbit_status lora_add_workspace_size(orbit_lora p, int64_t K, int64_t N, int32_t
  *          least every rank.  What lies beyond an adapter's rank does not matter
  *   base   device, [M][ldb] of `dtype` (orbit_qlinear's output, bias included), or NULL (zeros)
  *   Y      device, [M][ldy] of `dtype` (ORBIT_OUT_F32 or ORBIT_OUT_BF16); may be base with the same row
- *          stride, else they do not overlap
+ *          stride (another one is refused), else it overlaps no input (one that begins where X does is refused)
  *   h      device, fp32 [M][R], or NULL: receives X A^T (zeros beyond the rank and in rows without an
  *          adapter), which the backward call takes
  *   workspace   lora_add_workspace_size bytes, aligned to 16; contents and ownership as for orbit_qlinear_ws
@@ -541,7 +543,8 @@ orbit_status lora_add(orbit_lora p, const uint16_t* X, int64_t ldx, const uint16
  *   dY     device, bf16 [M][ldd]
  *   X, A, B, h   lora_add's inputs and its h
  *   base   device, bf16 [M][ldb], the gradient that X has from elsewhere (the projection), or NULL
- *   dX     device, bf16 [M][lddx]; may be base with the same row stride
+ *   dX     device, bf16 [M][lddx]; may be base with the same row stride, else it overlaps no input (one that
+ *          begins where base, X or dY do is refused)
  *   dA, dB device, fp32 [n_adapters][R][K] and [n_adapters][N][R]: every element is written, zeros beyond
  *          the ranks and for adapters without rows
  * Other arguments, limits and errors as for lora_add; ORBIT_EUNSUPPORTED also where the adapters' gradients, or the tiles of

@@ -106,6 +106,25 @@ orbit_status check_heads(const char* who, const char* name, const orbit_heads* t
     return ORBIT_OK;
 }
 
+// An output at an input's place has to be that input: its type and strides.  `from` may be another tensor's input, which an
+// output never replaces.
+orbit_status check_in_place(const char* who, const char* name, const HeadRows& y, const HeadRows& from, bool own) {
+    if (!y.p || y.p != from.p || (own && y.b == from.b && y.l == from.l && y.h == from.h)) return ORBIT_OK;
+    return fail(ORBIT_EINVAL, "%s: %s lies on an input that it does not replace row by row", who, name);
+}
+
+// The outputs against all inputs and each other.  Types: of x and y, and of g and y, equal or not.
+orbit_status check_places(const char* who, const char* const* names, const RopeParams& p, bool x_type, bool g_type) {
+    for (int i = 0; i < p.tensors; ++i)
+        for (int j = 0; j < p.tensors; ++j) {
+            orbit_status st = check_in_place(who, names[i], p.t[i].y, p.t[j].x, i == j && x_type);
+            if (st == ORBIT_OK) st = check_in_place(who, names[i], p.t[i].y, p.t[j].g, i == j && g_type);
+            if (st == ORBIT_OK && i != j) st = check_in_place(who, names[i], p.t[i].y, p.t[j].y, false);
+            if (st != ORBIT_OK) return st;
+        }
+    return ORBIT_OK;
+}
+
 // Sizes, positions and the plan's tables, checked and written into p.  done: there is nothing to launch.
 orbit_status common(const char* who, orbit_rope plan, int64_t B, int64_t L, int64_t D, const int32_t* pos, int64_t pos_batch, int heads,
                     RopeParams* p, DeviceInfo* info, bool* done) {
@@ -212,10 +231,12 @@ orbit_status axial_rope(orbit_rope plan, const orbit_heads* x, const orbit_heads
     bool done;
     orbit_status st = check_heads(who, "x", x, B, L, x->heads, x->dtype, &p.t[0].x);
     if (st == ORBIT_OK) st = check_heads(who, "y", y, B, L, x->heads, x->dtype, &p.t[0].y);
-    if (st == ORBIT_OK) st = common(who, plan, B, L, D, positions, pos_batch, x->heads, &p, &info, &done);
-    if (st != ORBIT_OK || done) return st;
     p.tensors = 1;
     p.t[0].heads = x->heads;
+    const char* const names[] = {"y"};
+    if (st == ORBIT_OK) st = check_places(who, names, p, true, true);
+    if (st == ORBIT_OK) st = common(who, plan, B, L, D, positions, pos_batch, x->heads, &p, &info, &done);
+    if (st != ORBIT_OK || done) return st;
     p.sign = inverse ? -1.f : 1.f;
     const bool f32 = x->dtype == ORBIT_OUT_F32;
     const hipError_t e = launch_axial_rope(p, false, f32, f32, info.cus, (hipStream_t)stream);
@@ -247,7 +268,9 @@ orbit_status qk_norm_rope(orbit_rope plan, const orbit_heads* q, const orbit_hea
         t.heads = in[i]->heads;
         most = t.heads > most ? t.heads : most;
     }
-    const orbit_status st = common(who, plan, B, L, D, positions, pos_batch, most, &p, &info, &done);
+    const char* const names[] = {"q_out", "k_out"};
+    orbit_status st = check_places(who, names, p, q->dtype == q_out->dtype, true);
+    if (st == ORBIT_OK) st = common(who, plan, B, L, D, positions, pos_batch, most, &p, &info, &done);
     if (st != ORBIT_OK || done) return st;
     p.eps = eps;
     const hipError_t e = launch_axial_rope(p, true, q->dtype == ORBIT_OUT_F32, q_out->dtype == ORBIT_OUT_F32, info.cus, (hipStream_t)stream);
@@ -301,7 +324,9 @@ orbit_status qk_norm_rope_backward(orbit_rope plan, const orbit_heads* dq, const
         t.dw = dw[i];
         most = t.heads > most ? t.heads : most;
     }
-    orbit_status st = common(who, plan, B, L, D, positions, pos_batch, most, &p, &info, &done);
+    const char* const names[] = {"q_grad", "k_grad"};
+    orbit_status st = check_places(who, names, p, true, q->dtype == dq->dtype);
+    if (st == ORBIT_OK) st = common(who, plan, B, L, D, positions, pos_batch, most, &p, &info, &done);
     if (st != ORBIT_OK) return st;
     const size_t part = (size_t)norm_rope_backward_groups(info.cus) * (size_t)D;
     if ((q_weight_grad || k_weight_grad) && (!workspace || !aligned(workspace, 16) || workspace_bytes < 2 * part * sizeof(float)))

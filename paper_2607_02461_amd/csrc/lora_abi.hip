@@ -147,6 +147,15 @@ orbit_status check_sizes(const char* who, orbit_lora p, int64_t K, int64_t N, in
     return ORBIT_OK;
 }
 
+// An output at base's place has base's rows; the other wide inputs are read after an output's first values are written.
+orbit_status check_places(const char* who, const char* name, const void* y, int64_t ldy, const void* base, int64_t ldb, int64_t rows,
+                          const void* x, const void* dy) {
+    if (!y) return ORBIT_OK;
+    if (y == base && rows > 1 && ldy != ldb) return fail(ORBIT_EINVAL, "%s: %s lies on base with another row stride", who, name);
+    if (y == x || y == dy) return fail(ORBIT_EINVAL, "%s: %s lies on an input other than base", who, name);
+    return ORBIT_OK;
+}
+
 orbit_status lists_on(const char* who, orbit_lora p, int dev, const unsigned char** out) {
     std::lock_guard<std::mutex> lk(p->mu);
     if (!p->dev_lists[dev])
@@ -254,6 +263,8 @@ orbit_status lora_add(orbit_lora p, const uint16_t* X, int64_t ldx, const uint16
     if (!X || !A || !B || !Y) return fail(ORBIT_EINVAL, "%s: null device pointer", who);
     if (!aligned(X, 2) || !aligned(A, 16) || !aligned(B, 16) || !aligned(base, size) || !aligned(Y, size) || !aligned(h, 16))
         return fail(ORBIT_EINVAL, "%s: misaligned pointer (A, B and h need 16 bytes)", who);
+    st = check_places(who, "Y", Y, ldy, base, ldb, p->rows, X, nullptr);
+    if (st != ORBIT_OK) return st;
     int dev;
     DeviceInfo info;
     st = current_device(&dev, &info);
@@ -321,6 +332,8 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
     if (!aligned(dY, 2) || !aligned(X, 2) || !aligned(base, 2) || !aligned(dX, 2) || !aligned(A, 16) || !aligned(B, 16) || !aligned(h, 16) ||
         !aligned(dA, 16) || !aligned(dB, 16))
         return fail(ORBIT_EINVAL, "%s: misaligned pointer (A, B, h, dA and dB need 16 bytes)", who);
+    st = check_places(who, "dX", dX, lddx, base, ldb, p->rows, X, dY);
+    if (st != ORBIT_OK) return st;
     int dev;
     DeviceInfo info;
     st = current_device(&dev, &info);

@@ -68,3 +68,29 @@ def test_device_calls_validate_before_launch():
     assert st == 1 and "without the weight" in lib.orbit_last_error().decode()
     assert lib.rope_plan_upload(None) == 1
     lib.rope_plan_destroy(None)
+
+
+def test_outputs_on_inputs_that_they_do_not_replace_are_refused():
+    lib, here, there = oq.lib(), 1 << 20, 1 << 24   # never dereferenced: without a device no call gets further than its checks
+    plan = oq.rope_plan((16, 16), (4, 4))
+
+    def heads(data, strides=(0, 64, 32), n=2, dtype=1):
+        return ctypes.byref(Heads(data, *strides, n, dtype))
+
+    def refused(status):
+        return status == 1 and "lies on an input" in lib.orbit_last_error().decode()
+
+    other = (0, 128, 32)
+    rope = lambda x, y, L=3: lib.axial_rope(plan.handle, x, y, 1, L, 32, here, 0, 0, None)  # noqa: E731
+    assert refused(rope(heads(here), heads(here, other)))
+    none = ctypes.c_void_p(0)
+    norm = lambda q, k, qo, ko: lib.qk_norm_rope(plan.handle, q, k, qo, ko, 1, 3, 32, here, 0, None, None, 0, 1e-6, None)  # noqa: E731
+    assert refused(norm(heads(here, dtype=0), none, heads(here), none))                         # another type
+    assert refused(norm(heads(here), heads(there), heads(there), heads(here)))                  # q and k change places
+    assert refused(norm(heads(here), heads(here), heads(here), heads(there)))                   # q replaced, read as k
+    assert refused(norm(heads(here), heads(here), heads(there), heads(there)))                  # one output for both
+    back = lambda dq, q, qg, dk=none, k=none, kg=none: lib.qk_norm_rope_backward(  # noqa: E731
+        plan.handle, dq, dk, q, k, qg, kg, 1, 3, 32, here, 0, None, None, 0, 1e-6, None, None, None, 0, None)
+    assert refused(back(heads(here, dtype=0), heads(there), heads(here)))
+    assert refused(back(heads(here), heads(there), heads(here, other)))
+    assert refused(back(heads(here), heads(there), heads(2 * there), heads(3 * there), heads(4 * there), heads(here)))

@@ -55,3 +55,24 @@ def test_device_calls_validate_before_launch():
     assert lib.lora_add_workspace_size(None, 64, 32, 8, 0, ctypes.byref(n)) == 1 and n.value == 0
     assert lib.lora_plan_upload(None) == 1
     lib.lora_plan_destroy(None)
+
+
+def test_outputs_on_inputs_that_they_do_not_replace_are_refused():
+    lib, at = oq.lib(), [1 << 20 + i for i in range(8)]   # never dereferenced: every case fails its checks
+    plan = _plan()
+
+    def refused(status, word):
+        return status == 1 and word in lib.orbit_last_error().decode()
+
+    def add(x, base, ldb, y, ldy):
+        return lib.lora_add(plan.handle, x, 64, at[6], at[7], 64, 64, 8, base, ldb, 1, y, ldy, None, at[5], 1 << 30, None)
+
+    assert refused(add(at[0], at[1], 64, at[1], 72), "another row stride")
+    assert refused(add(at[0], at[1], 64, at[0], 64), "other than base")
+
+    def back(dy, x, base, ldb, dx, lddx):
+        return lib.lora_add_backward(plan.handle, dy, 64, x, 64, at[6], at[7], at[5], 64, 64, 8, base, ldb, dx, lddx, at[4], at[4], at[4], 1 << 30, None)
+
+    assert refused(back(at[0], at[1], at[2], 64, at[2], 72), "another row stride")
+    assert refused(back(at[0], at[1], None, 0, at[0], 64), "other than base")
+    assert refused(back(at[0], at[1], at[2], 64, at[1], 64), "other than base")
