@@ -501,3 +501,45 @@ def test_non_temporal_accesses_go_by_what_lies_together(D, dims, layout, streams
         assert torch.equal(y, ref)
         (kernel, _, non_temporal, _, _), = _instances(call)
         assert kernel == name and non_temporal == streams
+
+
+# --- several rows to a wave and several waves to a token -------------------------------------------
+@pytest.mark.parametrize("Hq,Hk,chunks,rows", [(24, 8, 1, 6), (40, 24, 2, 6), (43, 13, 2, 6), (16, 5, 1, 3)])
+@pytest.mark.parametrize("large", [False, True])
+@pytest.mark.parametrize("halves", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_many_heads_of_many_tokens(Hq, Hk, chunks, rows, large, halves, dtype):
+    # heads of 128 are four to a wave side by side: 43 are two waves of 6 and 5 rows, whose last one has 3 heads
+    D, dims = 128, (16, 56, 40)
+    L = (161 << 20) // ((Hq + Hk) * D * 4) if large else 1103    # above 160 MiB the accesses are non-temporal
+    plan, pos, angles = _plan_and_positions(dims, 1, L, 100, halves)
+    angles, P = torch.tensor(angles[0], device=DEV), sum(dims) // 2
+    g = torch.Generator(device=DEV).manual_seed(101)
+    q, k, dq, dk = (torch.randn((1, L, h, D), generator=g, device=DEV).to(t) for h, t in ((Hq, dtype), (Hk, dtype), (Hq, BF16), (Hk, BF16)))
+    wq, wk = torch.linspace(0.5, 2.0, D, device=DEV), torch.linspace(2.0, 0.5, D, device=DEV)
+    forward = lambda: oq.qk_norm_rope(plan, q, k, pos, wq, wk, eps=EPS, out_dtype=BF16)  # noqa: E731
+    backward = lambda: oq.qk_norm_rope_backward(plan, dq, dk, q, k, pos, wq, wk, eps=EPS)  # noqa: E731
+    (_, _, non_temporal, _, grid), = _instances(forward)
+    # (a half of the turned part, 56 values of bf16, is no whole line)
+    assert non_temporal == (large and not halves) and grid == ((L * chunks + 3) // 4, 2, 1)
+    (_, _, non_temporal, in_flight, _), = _instances(backward)
+    assert non_temporal == (L * (Hq + Hk) * D * (2 * q.element_size() + 2) > 160 << 20 and not halves) and in_flight == rows
+
+    def within(name, got, ref, size, kind):
+        over = float(((got.double() - ref).abs() - (HALF_ULP[kind] * ref.abs() + 32 * U * size)).max())
+        assert over <= 0.0, f"{name}: {over} beyond its bar"
+
+    got, grads = forward(), backward()
+    for i, (name, x, dy, w) in enumerate((("q", q, dq, wq), ("k", k, dk, wk))):
+        x, w = x.double(), w.double()
+        r = torch.rsqrt(x.square().mean(-1, keepdim=True) + EPS)
+        n = x * r * w
+        within(name, got[i], _turned(n, angles, halves), _device_pair_length(n, P, halves), BF16)
+        t = _turned(dy.double(), angles, halves, -1.0)
+        length = _device_pair_length(t, P, halves)
+        ref = r * (t * w - x * r * r * (t * w * x).mean(-1, keepdim=True))
+        size = r * (length * w + x.abs() * r * r * (length * w * x.abs()).mean(-1, keepdim=True))
+        within(f"{name} grad", grads[i], ref, size, dtype)
+        terms = (length * x.abs() * r).sum((0, 1, 2))
+        bar = (10 * (L * x.shape[2]) ** 0.5 + 32) * U * terms
+        assert ((grads[2 + i].double() - (t * x * r).sum((0, 1, 2))).abs() <= bar).all(), f"{name} weight grad"
