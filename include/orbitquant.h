@@ -434,7 +434,7 @@ void rope_plan_destroy(orbit_rope p);
  *              all share one).  They are not checked before the launch: a position outside its axis's
  *              lengths gives NaN in the values of that axis
  * Errors: ORBIT_EINVAL (null pointers, types, strides, alignment, a plan without tables on the device);
- * ORBIT_EUNSUPPORTED (D, more than 2^31 - 1 head rows); ORBIT_EHIP.  B = 0 or L = 0 returns at once.
+ * ORBIT_EUNSUPPORTED (D, more than 2^31 - 1 head rows or 2^30 heads); ORBIT_EHIP.  B = 0 or L = 0 returns at once.
  */
 orbit_status axial_rope(orbit_rope plan, const orbit_heads* x, const orbit_heads* y, int64_t B, int64_t L, int64_t D,
                         const int32_t* positions, int64_t pos_batch, int32_t inverse, void* stream);

@@ -12,6 +12,8 @@ using namespace orbit;
 
 namespace {
 
+constexpr int32_t kMaxHeads = 1 << 30;        // indices of the heads that a wave's last step has beyond them fit 32 bits too
+constexpr int64_t kMaxReach = (int64_t)1 << 50;  // elements from a dimension's first entry to its last: offsets fit 64 bits
 constexpr int64_t kMaxTable = (int64_t)1 << 27;  // (cos, sin) pairs of a plan: their byte offsets and indices fit 32 bits
 
 orbit_status rope_upload_dev(orbit_rope p, int dev) {
@@ -81,6 +83,8 @@ orbit_status make_plan(int32_t axes, const int32_t* dims, const int32_t* lengths
     return ORBIT_OK;
 }
 
+bool too_far(int64_t entries, int64_t stride) { return entries > 1 && (stride < 0 || stride > kMaxReach / (entries - 1)); }
+
 bool is_type(int32_t t) { return t == ORBIT_OUT_F32 || t == ORBIT_OUT_BF16; }
 
 // Rows of 16-byte groups: pointer and strides (of dimensions with more than one entry) multiples of 16 bytes.
@@ -90,14 +94,13 @@ orbit_status check_heads(const char* who, const char* name, const orbit_heads* t
     if (t->heads != heads) return fail(ORBIT_EINVAL, "%s: %s has %d heads, %d expected", who, name, t->heads, heads);
     if (t->dtype != dtype) return fail(ORBIT_EINVAL, "%s: %s has type %d, %d expected", who, name, t->dtype, dtype);
     if (heads < 1) return fail(ORBIT_EINVAL, "%s: %s has %d heads", who, name, heads);
-    if (B == 0 || L == 0) return ORBIT_OK;
+    if (heads > kMaxHeads) return fail(ORBIT_EUNSUPPORTED, "%s: %s has more than %d heads", who, name, kMaxHeads);
+    if (B <= 0 || L <= 0) return ORBIT_OK;
     if (!t->data) return fail(ORBIT_EINVAL, "%s: %s is a null device pointer", who, name);
     const int unit = dtype == ORBIT_OUT_F32 ? 4 : 8;
-    const int64_t limit = (int64_t)1 << 40;  // the products below stay far from 2^63
     if (!aligned(t->data, 16) || (B > 1 && t->batch % unit) || (L > 1 && t->token % unit) || (heads > 1 && t->head % unit))
         return fail(ORBIT_EINVAL, "%s: %s must be aligned to 16 bytes, its strides too", who, name);
-    if ((B > 1 && (t->batch < 0 || t->batch > limit)) || (L > 1 && (t->token < 0 || t->token > limit)) ||
-        (heads > 1 && (t->head < 0 || t->head > limit)))
+    if (too_far(B, t->batch) || too_far(L, t->token) || too_far(heads, t->head))
         return fail(ORBIT_EINVAL, "%s: %s has a stride out of range", who, name);
     out->p = t->data;
     out->b = B > 1 ? t->batch : 0;
@@ -134,7 +137,7 @@ orbit_status common(const char* who, orbit_rope plan, int64_t B, int64_t L, int6
         return fail(ORBIT_EUNSUPPORTED, "%s: head size %lld, a multiple of 8 up to %d is implemented", who, (long long)D, kMaxHeadDim);
     if (plan && 2 * plan->pairs > D)
         return fail(ORBIT_EINVAL, "%s: the plan rotates %d values, a head has %lld", who, 2 * plan->pairs, (long long)D);
-    if (pos_batch < 0 || pos_batch > (int64_t)1 << 40) return fail(ORBIT_EINVAL, "%s: positions' batch stride out of range", who);
+    if (pos_batch < 0 || too_far(B, pos_batch)) return fail(ORBIT_EINVAL, "%s: positions' batch stride out of range", who);
     if (B > INT32_MAX || L > INT32_MAX || B * L > INT32_MAX / heads)
         return fail(ORBIT_EUNSUPPORTED, "%s: more than 2^31 - 1 head rows", who);
     *done = B == 0 || L == 0;

@@ -94,3 +94,12 @@ def test_outputs_on_inputs_that_they_do_not_replace_are_refused():
     assert refused(back(heads(here, dtype=0), heads(there), heads(here)))
     assert refused(back(heads(here), heads(there), heads(here, other)))
     assert refused(back(heads(here), heads(there), heads(2 * there), heads(3 * there), heads(4 * there), heads(here)))
+
+
+@pytest.mark.parametrize("n,strides,B,status,word", [((1 << 31) - 1, (0, 1 << 34, 8), 1, 2, "heads"), ((1 << 30) + 1, (0, 1 << 34, 8), 1, 2, "heads"),
+                                                     (2, (1 << 40, 64, 32), 1 << 20, 1, "stride"), (1 << 20, (0, 64, 1 << 40), 1, 1, "stride")])
+def test_offsets_that_pass_their_numbers_are_refused(n, strides, B, status, word):
+    # a token's last head and the rows behind it have 32-bit indices, an element's offset has 64 bits
+    lib, plan = oq.lib(), oq.rope_plan((8,), (4,))
+    x = ctypes.byref(Heads(1 << 20, *strides, n, 1))
+    assert lib.axial_rope(plan.handle, x, x, B, 1, 8, 1 << 20, 0, 0, None) == status and word in lib.orbit_last_error().decode()
