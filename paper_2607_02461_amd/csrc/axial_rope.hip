@@ -12,13 +12,16 @@
 // All of it is bound by HBM: a value is read and written once and takes 3 to 16 operations.  So a head's row stays
 // in registers, eight values (16 bytes of bf16) to a lane and D / 8 lanes to a head, a wave holds the same token's
 // heads side by side and has the loads of up to kRows rows in flight before the first is used, and the cosines and
-// sines of a lane's four pairs are fetched once per token for all of its heads.  Heads of 128, bytes read and written:
-//   rotation, 32760 tokens of 40 heads in bf16                         109 us, 6.2 TB/s (a part stays in the last cache)
+// sines of a lane's four pairs are fetched once for all of these rows.  (A token of more heads takes further waves, queries
+// and keys take waves of their own, and each of them fetches them again, from a cache.)  Heads of 128, bytes read and written:
+//   rotation, 32760 tokens of 40 heads in bf16                         108 us, 6.2 TB/s (a part stays in the last cache),
+//     107 us where a pair's values are a half of the head apart
 //   norms and rotation, 9216 tokens of 24 + 24 heads in bf16            47 us, 4.8 TB/s
-//   the same, 32760 tokens of 40 + 40 heads, fp32 to bf16              378 us, 5.3 TB/s
-//   its gradients, 8858 tokens of 24 + 24 heads in bf16            68 + 5 us, 4.8 TB/s
-// One token takes 4 to 6 us.  Heads of 80 or 96 leave lanes idle (a power of two of them share a head) and take 1.6 to
-// 1.8 times as long a byte.
+//   the same, 32760 tokens of 40 + 40 heads, fp32 to bf16              372 us, 5.4 TB/s; fp32 to fp32 487, bf16 to fp32 361
+//   its gradients, 8858 tokens of 24 + 24 heads in bf16            67 + 5 us, 4.9 TB/s; in fp32 122
+// One token takes 4 to 6 us.  Heads of 80 or 96 leave 6 or 4 of 16 lanes idle: 9216 tokens of 24 + 24 of them take the
+// norm's 18 million vector instructions of heads of 128, and 42 us for 142 and 170 MB where those take 47 for 226.
+// The rotation alone (27 and 32 us; 40) keeps to the copy's rate, and so does the norm of 700 MB of heads of 80 (141 us).
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 

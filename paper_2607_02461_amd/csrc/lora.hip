@@ -4,7 +4,8 @@
 //     h = x A_a^T,  y = base + s h B_a^T                                    (A_a [R][K], B_a [N][R], bf16)
 // and with g = dy B_a
 //     dx = s g A_a,  dA_a = s sum over its rows of g^T x,  dB_a = s sum over its rows of dy^T h.
-// At ranks up to 128 all of it is bound by the wide matrices x, base, y, dy and dx, each of which a kernel streams once:
+// At ranks up to 128 all of it is bound by the wide matrices x, base, y, dy and dx, which each kernel streams once (x and dy
+// are read by two: by the shrink, and by the gradients):
 //   shrink  h (or g): a wide matrix times a narrow one, contraction over the wide side
 //   expand  y (or dx): a narrow matrix times a narrow one, added to the wide base on its way through the registers
 //   grad    dA, dB: contraction over rows, of a wide matrix and a narrow one

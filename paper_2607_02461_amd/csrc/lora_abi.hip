@@ -373,7 +373,7 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
         s.tiles = t.tiles;
         s.x = dY;
         s.ldx = ldd;
-            s.K = N;
+        s.K = N;
         s.pool = t.bt;
         s.ldp = l.ldn;
         s.R = R;
@@ -386,7 +386,7 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
         x.turned = (uint16_t*)(ws + l.g_turned);
         x.splits = l.splits;
         x.R = R;
-            x.N = K;
+        x.N = K;
         x.pool = t.at;
         x.base = base;
         x.ldb = ldb;
