@@ -555,6 +555,105 @@ orbit_status lora_add_backward(orbit_lora p, const uint16_t* dY, int64_t ldd, co
                                const uint16_t* base, int64_t ldb, uint16_t* dX, int64_t lddx, float* dA, float* dB,
                                void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------- layer norms in front of a projection */
+
+/*
+ * Rows of N values, [batch][row][N] on the device with the values of a row contiguous: strides in elements,
+ * ORBIT_OUT_F32 or ORBIT_OUT_BF16 values, aligned to their type.  Strides of inputs may be 0 (broadcast); rows of an
+ * output must not overlap.  An output may replace an input row by row (same data, strides and type) and overlaps no
+ * other operand; one that begins where an input does is refused otherwise.
+ */
+typedef struct {
+    void* data;
+    int64_t batch, row;
+    int32_t dtype;
+} orbit_rows;
+
+/*
+ * layer_norm -- the norm of each row, with a weight and a bias or modulated by its batch's scale and shift (the
+ * adaptive norms of a diffusion transformer, whose scale and shift the AdaLN projection makes):
+ *     y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * g + bias,     g = weight, or 1 + weight with `modulate`.
+ * Computed in fp32 and rounded once; the sum of squares is one of deviations from means, also where the mean is large.
+ * A row whose variance passes fp32's range gives its bias.
+ *   x, y       [B][L][N]; y may be x
+ *   weight, bias   device, rows [N] of w_dtype, or NULL (g = 1; 0); weight_batch, bias_batch: elements from one batch's row
+ *              to the next's, 0 where the batches share one.  A view of the modulation projection's output is such rows
+ *   eps        finite, >= 0
+ * N is 1..12288.  Errors: ORBIT_EINVAL (null pointers, types, strides, alignment, eps); ORBIT_EUNSUPPORTED (N, more than
+ * 2^31 - 1 rows); ORBIT_EHIP.  B = 0 or L = 0 returns at once.
+ */
+orbit_status layer_norm(const orbit_rows* x, const orbit_rows* y, int64_t B, int64_t L, int64_t N, const void* weight,
+                        int64_t weight_batch, const void* bias, int64_t bias_batch, int32_t w_dtype, int32_t modulate,
+                        float eps, void* stream);
+
+/* Bytes of device workspace that layer_norm_backward takes on the current device for gradients of weight or bias. */
+orbit_status layer_norm_backward_workspace_size(int64_t B, int64_t L, int64_t N, int32_t per_batch, size_t* bytes);
+
+/*
+ * layer_norm_backward -- gradients of layer_norm's inputs from that of its output: dx in x's type (x is the forward call's
+ * input, not its output, if that replaced it), the weight's (or scale's) and the bias's (or shift's) in fp32.  These are
+ * sums over rows in a fixed order (the same bits on the same device): over each batch's rows, [B][N], with per_batch, else
+ * over all rows, [N]; NULL where they are not needed.
+ *   dx         may be dy where the types are equal, or x
+ *   weight     as for layer_norm; weights that differ between batches have gradients per batch
+ *   workspace  layer_norm_backward_workspace_size bytes, aligned to 16, where dweight or dbias is asked for; contents and
+ *              ownership as for orbit_qlinear_ws
+ * Limits and errors as for layer_norm; ORBIT_EUNSUPPORTED also where the batches' gradients are too many for one launch.
+ * Without rows the gradients are zeros.
+ */
+orbit_status layer_norm_backward(const orbit_rows* dy, const orbit_rows* x, const orbit_rows* dx, int64_t B, int64_t L,
+                                 int64_t N, const void* weight, int64_t weight_batch, int32_t w_dtype, int32_t modulate,
+                                 float eps, float* dweight, float* dbias, int32_t per_batch, void* workspace,
+                                 size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------- attention */
+
+typedef struct orbit_attention_s* orbit_attention;
+
+/*
+ * attention_plan -- which queries attend to which keys: n sequences, each of consecutive query tokens and consecutive key
+ * tokens, with `heads` query heads over kv_heads key heads (query head h reads key head h / (heads / kv_heads)).  Lengths
+ * may differ and may be 0; starts may leave tokens out (padded batches) and come in any order; sequences may share keys, not
+ * queries.  With `causal`, query i of a sequence of n_q queries sees its first i + 1 + n_k - n_q keys (the last query sees
+ * them all: a chunk of new tokens over the keys so far), none where that is below 1.  One plan serves every layer of a
+ * batch.  Its lists are kept on the device as for rpbh_plan.
+ *   q_starts, q_lens, k_starts, k_lens   host, [n], in tokens
+ * Errors: ORBIT_EINVAL; ORBIT_EUNSUPPORTED (a sequence beyond 2^31 rows, more than 65535 heads, or more tiles of 128 rows
+ * (queries times heads of a group, or keys) times kv_heads than some 2^24); ORBIT_ENOMEM; ORBIT_EHIP.
+ */
+orbit_status attention_plan(int64_t n, const int64_t* q_starts, const int64_t* q_lens, const int64_t* k_starts,
+                            const int64_t* k_lens, int32_t heads, int32_t kv_heads, int32_t causal, orbit_attention* out);
+
+/* Copy the plan's lists to the current device, as rpbh_plan_upload. */
+orbit_status attention_plan_upload(orbit_attention p);
+
+/* Free a plan.  NULL is ignored. */
+void attention_plan_destroy(orbit_attention p);
+
+/* Bytes of device workspace that attention takes for heads of D; 0 where it takes none (the workspace may then be NULL). */
+orbit_status attention_workspace_size(orbit_attention p, int64_t D, size_t* bytes);
+
+/*
+ * attention -- out = softmax(scale q k^T) v for each query head over the keys that the plan lets it see:
+ *   q, k, v    rows of bf16 heads, [token][head][D], the plan's tokens and heads (orbit_heads.batch is not read): queries,
+ *              keys and values may be views of one fused projection's output
+ *   out        [token][head][D], bf16 or fp32; it does not overlap the inputs (one that begins where an input does is
+ *              refused).  A query that sees no key gets zeros; tokens of no sequence are left as they were
+ *   D          a multiple of 8 up to 128
+ *   scale      finite, above 0
+ *   lse        device, fp32 [token][heads], or NULL: the logarithm of each row's sum of exponentials, -inf where it sees no key
+ *   workspace  attention_workspace_size bytes, aligned to 16; contents and ownership as for orbit_qlinear_ws
+ * Scores, maxima and sums are fp32; probabilities enter the product with v in bf16, whose sum is fp32 and is rounded once.
+ * The same plan and inputs give the same bits.  A value that is not finite in a key or value may show, as a NaN, in every
+ * query of its sequence that shares a tile of 128 rows with one that sees it; rows of other sequences do not depend on it.
+ * Data and strides are multiples of 16 bytes, a token's stride at most 2^24 values.  Errors: ORBIT_EINVAL (null pointers,
+ * types, strides, alignment, scale, a plan without tables on the device); ORBIT_EUNSUPPORTED (D); ORBIT_EHIP.  A plan
+ * without queries returns at once.
+ */
+orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_heads* k, const orbit_heads* v,
+                       const orbit_heads* out, int64_t D, float scale, float* lse, void* workspace, size_t workspace_bytes,
+                       void* stream);
+
 #ifdef __cplusplus
 }
 #endif

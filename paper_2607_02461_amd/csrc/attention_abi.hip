@@ -1,0 +1,304 @@
+// Entry points of attention: plans, argument checks, workspaces, launches.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <utility>
+
+#include "abi.h"
+#include "device.h"
+#include "internal.h"
+
+using namespace orbit;
+
+namespace {
+
+constexpr int64_t kMaxTokens = INT32_MAX;
+constexpr int32_t kMaxHeads = 65535;
+constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 8;   // workgroups of 256 threads to a launch
+constexpr int64_t kMaxStride = (int64_t)1 << 24;         // elements from a token to the next: a tile's rows lie within 2^32 bytes
+
+struct Sequence {
+    int64_t q_start, q_len, k_start, k_len;
+};
+
+// A list's tiles, with what each costs in units of the other side's tiles.
+struct Work {
+    AttnTile tile;
+    int64_t cost;
+};
+
+// Tiles that would leave the card partly idle are divided along the other side into parts of at least `least` units of `step` keys
+// (or queries) each, so that there are about `most` workgroups in all.  Parts leave their sums in slots, which a join adds up.
+// The longest come first: workgroups start in the list's order, and the last to start are the shortest.
+void divide(std::vector<Work>& work, int64_t kv_heads, int64_t step, int64_t least, int64_t most, int64_t* slots, std::vector<AttnJoin>* joins,
+            std::vector<AttnTile>* out) {
+    int64_t total = 0;
+    for (const Work& w : work) total += w.cost;
+    const int64_t part = (int64_t)work.size() * kv_heads >= most ? INT64_MAX : std::max(least, (total * kv_heads + most - 1) / most);
+    std::vector<Work> all;
+    for (const Work& w : work) {
+        const int64_t n = std::max<int64_t>(1, (w.cost + part / 2) / part);
+        if (n == 1) {
+            all.push_back(w);
+            continue;
+        }
+        const AttnTile& t = w.tile;
+        joins->push_back({t.q_start, t.q_len, t.k_start, t.k_len, t.first, (int32_t)*slots, (int32_t)n, 0});
+        for (int64_t i = 0; i < n; ++i) {
+            Work piece = w;
+            const int64_t from = w.cost * i / n, to = w.cost * (i + 1) / n;
+            piece.cost = to - from;
+            piece.tile.begin = (int32_t)(t.begin + from * step);
+            piece.tile.end = (int32_t)std::min<int64_t>(t.end, t.begin + to * step);
+            piece.tile.slot = (int32_t)(*slots)++;
+            all.push_back(piece);
+        }
+    }
+    std::stable_sort(all.begin(), all.end(), [](const Work& a, const Work& b) { return a.cost > b.cost; });
+    for (const Work& w : all) out->push_back(w.tile);
+}
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Lists of checked sequences.
+void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
+    const int64_t group = p->heads / p->kv_heads;
+    std::vector<Work> whole, few;
+    for (const Sequence& s : sequences) {
+        const int64_t rows = s.q_len * group, most = rows <= kAttnFewRows ? kAttnFewRows : kAttnRows;
+        for (int64_t first = 0; first < rows; first += most) {
+            const int64_t last = (std::min(first + most, rows) - 1) / group;   // the tile's last query
+            const int64_t end = p->causal ? std::min(s.k_len, std::max<int64_t>(0, last + 1 + s.k_len - s.q_len)) : s.k_len;
+            const AttnTile t{(int32_t)s.q_start, (int32_t)s.q_len, (int32_t)s.k_start, (int32_t)s.k_len, (int32_t)first, 0, (int32_t)end, -1};
+            if (most == kAttnFewRows)
+                few.push_back({t, ceil_div(end, 128)});
+            else
+                whole.push_back({t, ceil_div(end, 64)});
+        }
+    }
+    std::vector<AttnTile> list[kAttnLists];
+    std::vector<AttnJoin> joins;
+    // 512 workgroups of whole tiles are resident on 256 compute units, 256 of few rows
+    divide(whole, p->kv_heads, 64, 8, 1024, &p->slots, &joins, &list[kAttnForward]);
+    divide(few, p->kv_heads, 128, 2, 768, &p->slots, &joins, &list[kAttnFew]);
+
+    std::vector<unsigned char>& blob = p->lists;
+    auto append = [&](int which, const void* data, size_t count, size_t size) {
+        p->at[which] = (blob.size() + 15) / 16 * 16;
+        p->count[which] = (int64_t)count;
+        blob.resize(std::max<size_t>(p->at[which] + count * size, 16));
+        if (count) std::memcpy(blob.data() + p->at[which], data, count * size);
+    };
+    for (int i : {kAttnForward, kAttnFew}) append(i, list[i].data(), list[i].size(), sizeof(AttnTile));
+    append(kAttnJoins, joins.data(), joins.size(), sizeof(AttnJoin));
+}
+
+orbit_status upload_dev(orbit_attention p, int dev) {
+    std::lock_guard<std::mutex> lk(p->mu);
+    if (p->dev_lists[dev]) return ORBIT_OK;
+    void* d = nullptr;
+    const orbit_status st = upload_copy("attention_plan upload", p->lists.data(), p->lists.size(), &d);
+    p->dev_lists[dev] = (unsigned char*)d;
+    return st;
+}
+
+orbit_status lists_on(const char* who, orbit_attention p, int dev, const unsigned char** out) {
+    std::lock_guard<std::mutex> lk(p->mu);
+    if (!p->dev_lists[dev])
+        return fail(ORBIT_EINVAL, "%s: the plan has no tables on device %d: create it with that device current, or call "
+                                  "attention_plan_upload there first", who, dev);
+    *out = p->dev_lists[dev];
+    return ORBIT_OK;
+}
+
+// Whether two of the intervals (start, length) have a token in common
+bool overlap(std::vector<std::pair<int64_t, int64_t>> v) {
+    std::sort(v.begin(), v.end());
+    int64_t end = 0;
+    for (const auto& [start, length] : v) {
+        if (length == 0) continue;
+        if (start < end) return true;
+        end = start + length;
+    }
+    return false;
+}
+
+orbit_status check_dim(const char* who, orbit_attention p, int64_t D) {
+    if (!p) return fail(ORBIT_EINVAL, "%s: plan is NULL", who);
+    if (D < 8 || D % 8 || D > kAttnMaxDim)
+        return fail(ORBIT_EUNSUPPORTED, "%s: head size %lld, a multiple of 8 up to %d is implemented", who, (long long)D, kAttnMaxDim);
+    return ORBIT_OK;
+}
+
+orbit_status check_heads(const char* who, const char* name, const orbit_heads* t, int64_t tokens, int32_t heads, int64_t D, bool f32,
+                         bool output, AttnHeads* out) {
+    if (!t) return fail(ORBIT_EINVAL, "%s: %s is NULL", who, name);
+    if (t->heads != heads) return fail(ORBIT_EINVAL, "%s: %s has %d heads, the plan %d", who, name, t->heads, heads);
+    if (t->dtype != ORBIT_OUT_BF16 && !(f32 && t->dtype == ORBIT_OUT_F32)) return fail(ORBIT_EINVAL, "%s: %s has type %d", who, name, t->dtype);
+    const int unit = t->dtype == ORBIT_OUT_F32 ? 4 : 8;
+    if (tokens == 0) return ORBIT_OK;
+    if (!t->data) return fail(ORBIT_EINVAL, "%s: %s is a null device pointer", who, name);
+    if (!aligned(t->data, 16) || (tokens > 1 && t->token % unit) || (heads > 1 && t->head % unit))
+        return fail(ORBIT_EINVAL, "%s: %s must be aligned to 16 bytes, its strides too", who, name);
+    if ((tokens > 1 && (t->token < 0 || t->token > kMaxStride)) || (heads > 1 && (t->head < 0 || t->head > ((int64_t)1 << 50) / heads)))
+        return fail(ORBIT_EINVAL, "%s: %s has a stride out of range", who, name);
+    out->p = t->data;
+    out->token = tokens > 1 ? t->token : 0;
+    out->head = heads > 1 ? t->head : 0;
+    if (!output) return ORBIT_OK;
+    // a token's heads lie together, or a head's tokens do
+    const bool heads_apart = heads == 1 || out->head >= D, tokens_apart = tokens == 1 || out->token >= D;
+    const bool nested = heads == 1 || tokens == 1 || out->token >= (heads - 1) * out->head + D || out->head >= (tokens - 1) * out->token + D;
+    if (!heads_apart || !tokens_apart || !nested) return fail(ORBIT_EINVAL, "%s: %s's rows overlap", who, name);
+    return ORBIT_OK;
+}
+
+size_t slot_floats(int64_t D) { return (size_t)(attention_part((int)D) + 2 * kAttnRows); }
+
+size_t forward_bytes(orbit_attention p, int64_t D) { return (size_t)p->slots * p->kv_heads * slot_floats(D) * sizeof(float); }
+
+}  // namespace
+
+extern "C" {
+
+orbit_status attention_plan(int64_t n, const int64_t* q_starts, const int64_t* q_lens, const int64_t* k_starts, const int64_t* k_lens, int32_t heads,
+                            int32_t kv_heads, int32_t causal, orbit_attention* out) {
+    const char* who = "attention_plan";
+    clear_error();
+    if (!out) return fail(ORBIT_EINVAL, "%s: out is NULL", who);
+    *out = nullptr;
+    if (n < 0) return fail(ORBIT_EINVAL, "%s: negative number of sequences", who);
+    if (n && (!q_starts || !q_lens || !k_starts || !k_lens)) return fail(ORBIT_EINVAL, "%s: a list is NULL", who);
+    if (heads < 1 || kv_heads < 1 || heads % kv_heads) return fail(ORBIT_EINVAL, "%s: %d heads over %d key heads", who, heads, kv_heads);
+    if (heads > kMaxHeads) return fail(ORBIT_EUNSUPPORTED, "%s: more than %d heads", who, kMaxHeads);
+    const int64_t group = heads / kv_heads;
+    int64_t tiles = 0, q_tokens = 0, k_tokens = 0;
+    for (int64_t i = 0; i < n; ++i) {
+        if (q_starts[i] < 0 || q_lens[i] < 0 || k_starts[i] < 0 || k_lens[i] < 0)
+            return fail(ORBIT_EINVAL, "%s: sequence %lld has a negative start or length", who, (long long)i);
+        if (q_starts[i] > kMaxTokens || q_lens[i] > kMaxTokens - q_starts[i] || k_starts[i] > kMaxTokens || k_lens[i] > kMaxTokens - k_starts[i] ||
+            q_lens[i] > (kMaxTokens - kAttnRows) / group || k_lens[i] > kMaxTokens - kAttnRows)
+            return fail(ORBIT_EUNSUPPORTED, "%s: sequence %lld passes 2^31 rows", who, (long long)i);
+        // keys' tiles too, those of the backward pass; a list divides further only where it has fewer than some 1000 tiles
+        tiles += ceil_div(q_lens[i] * group, kAttnRows) + ceil_div(k_lens[i], kAttnRows);
+        if (tiles > (kMaxGroups - 8192) / kv_heads) return fail(ORBIT_EUNSUPPORTED, "%s: more tiles of rows than a launch takes", who);
+        if (q_lens[i]) q_tokens = std::max(q_tokens, q_starts[i] + q_lens[i]);
+        if (k_lens[i]) k_tokens = std::max(k_tokens, k_starts[i] + k_lens[i]);
+    }
+    orbit_attention p = new (std::nothrow) orbit_attention_s;
+    if (!p) return fail(ORBIT_ENOMEM, "%s: out of host memory", who);
+    p->heads = heads;
+    p->kv_heads = kv_heads;
+    p->causal = causal != 0;
+    p->q_tokens = q_tokens;
+    p->k_tokens = k_tokens;
+    bool twice = false;
+    try {
+        std::vector<Sequence> s;
+        std::vector<std::pair<int64_t, int64_t>> q, k;
+        for (int64_t i = 0; i < n; ++i) {
+            s.push_back({q_starts[i], q_lens[i], k_starts[i], k_lens[i]});
+            q.push_back({q_starts[i], q_lens[i]});
+            k.push_back({k_starts[i], k_lens[i]});
+        }
+        twice = overlap(q);
+        p->shared_keys = overlap(k);
+        if (!twice) fill(p, s);
+    } catch (...) {
+        delete p;
+        return fail(ORBIT_ENOMEM, "%s: out of host memory", who);
+    }
+    if (twice) {
+        delete p;
+        return fail(ORBIT_EINVAL, "%s: two sequences have a query in common", who);
+    }
+    int dev;
+    orbit_status st = device_for_upload(&dev);
+    if (st == ORBIT_OK && dev >= 0) st = upload_dev(p, dev);
+    if (st != ORBIT_OK) {
+        delete p;
+        return st;
+    }
+    *out = p;
+    return ORBIT_OK;
+}
+
+orbit_status attention_plan_upload(orbit_attention p) {
+    clear_error();
+    if (!p) return fail(ORBIT_EINVAL, "attention_plan_upload: plan is NULL");
+    int dev;
+    DeviceInfo info;
+    const orbit_status st = current_device(&dev, &info);
+    return st != ORBIT_OK ? st : upload_dev(p, dev);
+}
+
+void attention_plan_destroy(orbit_attention p) {
+    if (!p) return;
+    free_per_device(p->dev_lists);
+    delete p;
+}
+
+orbit_status attention_workspace_size(orbit_attention p, int64_t D, size_t* bytes) {
+    const char* who = "attention_workspace_size";
+    clear_error();
+    if (!bytes) return fail(ORBIT_EINVAL, "%s: null output pointer", who);
+    *bytes = 0;
+    const orbit_status st = check_dim(who, p, D);
+    if (st == ORBIT_OK) *bytes = forward_bytes(p, D);
+    return st;
+}
+
+orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_heads* k, const orbit_heads* v, const orbit_heads* out, int64_t D,
+                       float scale, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "attention";
+    clear_error();
+    orbit_status st = check_dim(who, p, D);
+    if (st != ORBIT_OK) return st;
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ORBIT_EINVAL, "%s: scale must be finite and above 0", who);
+    if (p->q_tokens == 0) return ORBIT_OK;
+    AttnParams a{};
+    st = check_heads(who, "q", q, p->q_tokens, p->heads, D, false, false, &a.q);
+    if (st == ORBIT_OK) st = check_heads(who, "k", k, p->k_tokens, p->kv_heads, D, false, false, &a.k);
+    if (st == ORBIT_OK) st = check_heads(who, "v", v, p->k_tokens, p->kv_heads, D, false, false, &a.v);
+    if (st == ORBIT_OK) st = check_heads(who, "out", out, p->q_tokens, p->heads, D, true, true, &a.o);
+    if (st != ORBIT_OK) return st;
+    if (a.o.p == a.q.p || a.o.p == a.k.p || a.o.p == a.v.p) return fail(ORBIT_EINVAL, "%s: out lies on an input", who);
+    if (!aligned(lse, 4)) return fail(ORBIT_EINVAL, "%s: misaligned lse", who);
+    const size_t bytes = forward_bytes(p, D);
+    if (bytes && (!workspace || !aligned(workspace, 16) || workspace_bytes < bytes))
+        return fail(ORBIT_EINVAL, "%s: takes a workspace of %zu bytes, aligned to 16", who, bytes);
+    int dev;
+    DeviceInfo info;
+    st = current_device(&dev, &info);
+    if (st != ORBIT_OK) return st;
+    const unsigned char* lists = nullptr;
+    st = lists_on(who, p, dev, &lists);
+    if (st != ORBIT_OK) return st;
+    a.heads = p->heads;
+    a.kv_heads = p->kv_heads;
+    a.group = p->heads / p->kv_heads;
+    a.D = (int)D;
+    a.causal = p->causal;
+    a.scale = (float)(scale * 1.4426950408889634);
+    a.out_f32 = out->dtype == ORBIT_OUT_F32;
+    a.lse = lse;
+    a.part = (float*)workspace;
+    a.stat = a.part + p->slots * p->kv_heads * attention_part((int)D);
+    for (int which : {kAttnForward, kAttnFew}) {
+        a.tiles = (const AttnTile*)(lists + p->at[which]);
+        a.count = (int)p->count[which];
+        if (!a.count) continue;
+        const hipError_t e = launch_attention(a, which == kAttnFew, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, who);
+    }
+    a.joins = (const AttnJoin*)(lists + p->at[kAttnJoins]);
+    a.count = (int)p->count[kAttnJoins];
+    if (!a.count) return ORBIT_OK;
+    const hipError_t e = launch_attention_join(a, (hipStream_t)stream);
+    return e == hipSuccess ? ORBIT_OK : hip_fail(e, who);
+}
+
+}  // extern "C"

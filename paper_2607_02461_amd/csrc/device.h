@@ -295,4 +295,76 @@ hipError_t launch_lora_turn(const LoraTurn& p, hipStream_t stream);
 // together: a workgroup's waves share columns (direct: always), else they share rows.
 hipError_t launch_lora_grad(LoraGrad p, int splits, int adapters, bool together, hipStream_t stream);
 
+// Layer norm of rows, modulated or with weights.
+constexpr int kNormMaxWidth = 12288;
+
+struct NormRows {     // [B][L][N] values, rows contiguous; strides in elements
+    void* p;
+    int64_t batch, row;
+};
+
+struct NormParams {
+    NormRows x, y, g;      // input; output, or x's gradient; the output's gradient
+    const void *w, *b;     // weight (or scale) and bias (or shift) [group][N], bf16 or fp32, or null
+    int64_t w_batch, b_batch;
+    int w_f32, modulate;   // modulate: the gain is 1 + w
+    int N;
+    int joined;            // the batches' rows are one group (they share weights and their gradients)
+    int64_t rows, L;       // rows of a group; rows of a batch
+    float eps;
+    int stream;            // rows are loaded and stored non-temporally
+    float *dw, *db;        // fp32 [group][N] or null
+    float* part;           // [group][parts][2][N], the workgroups' sums
+    int parts;
+};
+
+hipError_t launch_layer_norm(const NormParams& p, int groups, bool x_f32, bool y_f32, int cus, hipStream_t stream);
+// Workgroups to a group of the backward pass, each with a row of sums.
+int layer_norm_parts(int64_t rows, int groups, int cus);
+// rows = 0 gives zeros in dw and db.
+hipError_t launch_layer_norm_backward(const NormParams& p, int groups, bool x_f32, bool g_f32, int cus, hipStream_t stream);
+
+// Attention of packed sequences, grouped heads.
+constexpr int kAttnRows = 128;     // rows of a workgroup's tile: queries x heads of a group, or keys
+constexpr int kAttnFewRows = 32;   // of a sequence, up to which a workgroup's waves share the rows and divide the keys
+constexpr int kAttnMaxDim = 128;
+
+struct AttnTile {             // what one workgroup computes for each key head
+    int32_t q_start, q_len;   // its sequence's queries and keys, in tokens
+    int32_t k_start, k_len;
+    int32_t first;            // of the tile's rows (token * group + head of the group), or of its keys
+    int32_t begin, end;       // of the keys that it goes over, or of the queries
+    int32_t slot;             // where its partial sums lie, or -1: it has them all
+};
+
+struct AttnJoin {             // partial sums of one tile
+    int32_t q_start, q_len, k_start, k_len, first;
+    int32_t slot, count;
+    int32_t pad;
+};
+
+struct AttnHeads {            // [token][head][D] bf16 values (or fp32, results), strides in elements
+    void* p;
+    int64_t token, head;
+};
+
+struct AttnParams {
+    const AttnTile* tiles;
+    const AttnJoin* joins;
+    int count;                // of the tiles, or of the joins
+    int heads, kv_heads, group, D;
+    int causal;
+    float scale;              // of the scores, times log2(e)
+    AttnHeads q, k, v, o;
+    int out_f32;
+    float* lse;               // [token][heads] or null
+    float* part;              // [slot][key head][row][padded D] of tiles that share their rows' keys
+    float* stat;              // [slot][key head][row][2]: largest scaled score, sum
+};
+
+// Floats of a slot's sums.
+constexpr int64_t attention_part(int D) { return (int64_t)kAttnRows * (D > 64 ? 128 : 64); }
+hipError_t launch_attention(const AttnParams& p, bool few, hipStream_t stream);
+hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream);
+
 }  // namespace orbit
