@@ -618,7 +618,7 @@ typedef struct orbit_attention_s* orbit_attention;
  * them all: a chunk of new tokens over the keys so far), none where that is below 1.  One plan serves every layer of a
  * batch.  Its lists are kept on the device as for rpbh_plan.
  *   q_starts, q_lens, k_starts, k_lens   host, [n], in tokens
- * Errors: ORBIT_EINVAL; ORBIT_EUNSUPPORTED (a sequence beyond 2^31 rows, more than 65535 heads, or more tiles of 128 rows
+ * Errors: ORBIT_EINVAL; ORBIT_EUNSUPPORTED (a sequence beyond 2^31 rows, more than 32767 heads, or more tiles of 128 rows
  * (queries times heads of a group, or keys) times kv_heads than some 2^24); ORBIT_ENOMEM; ORBIT_EHIP.
  */
 orbit_status attention_plan(int64_t n, const int64_t* q_starts, const int64_t* q_lens, const int64_t* k_starts,
@@ -630,8 +630,9 @@ orbit_status attention_plan_upload(orbit_attention p);
 /* Free a plan.  NULL is ignored. */
 void attention_plan_destroy(orbit_attention p);
 
-/* Bytes of device workspace that attention takes for heads of D; 0 where it takes none (the workspace may then be NULL). */
-orbit_status attention_workspace_size(orbit_attention p, int64_t D, size_t* bytes);
+/* Bytes of device workspace that attention (or, where `backward` is not 0, attention_backward) takes for heads of D; 0 where
+ * it takes none (the workspace may then be NULL). */
+orbit_status attention_workspace_size(orbit_attention p, int64_t D, int32_t backward, size_t* bytes);
 
 /*
  * attention -- out = softmax(scale q k^T) v for each query head over the keys that the plan lets it see:
@@ -653,6 +654,25 @@ orbit_status attention_workspace_size(orbit_attention p, int64_t D, size_t* byte
 orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_heads* k, const orbit_heads* v,
                        const orbit_heads* out, int64_t D, float scale, float* lse, void* workspace, size_t workspace_bytes,
                        void* stream);
+
+/*
+ * attention_backward -- gradients of attention's q, k and v from dout, that of its output, all in bf16:
+ *     dv = p^T dout,  ds = p (dout v^T - sum(dout out)),  dq = scale ds k,  dk = scale ds^T q,
+ * summed over the heads of a group in dk and dv, with the probabilities p computed again from lse.
+ *   q, k, v, out, lse   attention's inputs, its output (bf16 or fp32) and its lse
+ *   dq, dk, dv          as q, k and v; they overlap no input and not each other (one that begins where another does is
+ *                       refused).  Queries that see no key and keys that no query sees get zeros; tokens of no sequence are
+ *                       left as they were
+ *   workspace           attention_workspace_size bytes with `backward`
+ * Sums are fp32, in a fixed order (the same bits each time); p and ds enter their products in bf16.  Refused
+ * (ORBIT_EINVAL) for a plan whose sequences share keys.  Values that are not finite spread as with attention, over keys that
+ * share a tile of 128 too.  Other limits and errors as for attention; ORBIT_EUNSUPPORTED also where the heads of a group in
+ * q or dout lie more than 2^29 values apart.
+ */
+orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, const orbit_heads* q, const orbit_heads* k,
+                                const orbit_heads* v, const orbit_heads* out, const float* lse, const orbit_heads* dq,
+                                const orbit_heads* dk, const orbit_heads* dv, int64_t D, float scale, void* workspace,
+                                size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -82,7 +82,9 @@ SIGNATURES = {
     "attention_plan": (ctypes.c_int, [_i64, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i32, _i32, _i32, ctypes.POINTER(_c_void_p)]),
     "attention_plan_upload": (ctypes.c_int, [_c_void_p]),
     "attention_plan_destroy": (None, [_c_void_p]),
-    "attention_workspace_size": (ctypes.c_int, [_c_void_p, _i64, ctypes.POINTER(ctypes.c_size_t)]),
+    "attention_workspace_size": (ctypes.c_int, [_c_void_p, _i64, _i32, ctypes.POINTER(ctypes.c_size_t)]),
+    "attention_backward": (ctypes.c_int, [_c_void_p] * 6 + [_c_void_p] + [_c_void_p] * 3 + [_i64, ctypes.c_float, _c_void_p, ctypes.c_size_t,
+                                          _c_void_p]),
     "attention": (ctypes.c_int, [_c_void_p, _c_void_p, _c_void_p, _c_void_p, _c_void_p, _i64, ctypes.c_float, _c_void_p, _c_void_p,
                                  ctypes.c_size_t, _c_void_p]),
     "layer_norm": (ctypes.c_int, [_c_void_p, _c_void_p, _i64, _i64, _i64, _c_void_p, _i64, _c_void_p, _i64, _i32, _i32,
@@ -456,10 +458,10 @@ def adaln_int4_linear(X: torch.Tensor, q: torch.Tensor, scales: torch.Tensor, bi
 from .adapters import LoraPlan, lora_add, lora_add_backward, lora_plan  # noqa: E402
 from .attention_input import (RopePlan, axial_rope, qk_norm_rope, qk_norm_rope_backward, rope_plan,  # noqa: E402
                               rope_plan_from_angles)
-from .attention import AttentionPlan, attention, attention_plan  # noqa: E402
+from .attention import AttentionPlan, attention, attention_backward, attention_plan  # noqa: E402
 from .norms import layer_norm, layer_norm_backward, layer_norm_modulate, layer_norm_modulate_backward  # noqa: E402
 
-__all__ = ["AttentionPlan", "attention_plan", "attention", "layer_norm", "layer_norm_backward", "layer_norm_modulate", "layer_norm_modulate_backward", "LoraPlan", "lora_plan", "lora_add", "lora_add_backward", "RopePlan", "rope_plan", "rope_plan_from_angles", "axial_rope", "qk_norm_rope", "qk_norm_rope_backward", "adaln_int4_quantize_weights", "adaln_int4_linear", "rpbh_plan", "rpbh_plan_from_arrays", "lloydmax_codebook", "quantize_weights_offline",
+__all__ = ["AttentionPlan", "attention_plan", "attention", "attention_backward", "layer_norm", "layer_norm_backward", "layer_norm_modulate", "layer_norm_modulate_backward", "LoraPlan", "lora_plan", "lora_add", "lora_add_backward", "RopePlan", "rope_plan", "rope_plan_from_angles", "axial_rope", "qk_norm_rope", "qk_norm_rope_backward", "adaln_int4_quantize_weights", "adaln_int4_linear", "rpbh_plan", "rpbh_plan_from_arrays", "lloydmax_codebook", "quantize_weights_offline",
            "rpbh_quantize_act", "orbit_qlinear", "orbit_qlinear_ex",
            "orbit_qlinear_workspace_size", "orbit_qlinear_ws", "Plan", "Codebook", "OrbitError", "lib", "LIB_PATH",
            "SIGNATURES", "code_bytes"]

@@ -37,13 +37,13 @@ class AttentionPlan:
             _check("attention_plan_upload", lib().attention_plan_upload(self._h))
         return self
 
-    def _workspace(self, D, dev):
+    def _workspace(self, D, backward, dev):
         """(a new workspace or None, its bytes); the plan and the head size alone decide them."""
-        if D not in self._bytes:
+        if (D, backward) not in self._bytes:
             n = ctypes.c_size_t(0)
-            _check("attention_workspace_size", lib().attention_workspace_size(self._h, D, ctypes.byref(n)))
-            self._bytes[D] = n.value
-        n = self._bytes[D]
+            _check("attention_workspace_size", lib().attention_workspace_size(self._h, D, backward, ctypes.byref(n)))
+            self._bytes[D, backward] = n.value
+        n = self._bytes[D, backward]
         return torch.empty((n,), dtype=torch.uint8, device=dev) if n else None, n
 
     def __del__(self):
@@ -152,6 +152,26 @@ def attention(plan: AttentionPlan, q: torch.Tensor, k: torch.Tensor, v: torch.Te
     out, ho = _output(out, q, "out", plan._queries, out_dtype)
     if lse is not None:
         _expect(lse, "lse", torch.float32, (q.shape[0], plan.heads), q.device)
-    ws, ws_bytes = plan._workspace(D, q.device)
+    ws, ws_bytes = plan._workspace(D, 0, q.device)
     _call("attention", q.device, plan._h, hq, hk, hv, ho, D, 1 / math.sqrt(D) if scale is None else scale, _ptr(lse), _ptr(ws), ws_bytes)
     return out
+
+
+def attention_backward(plan: AttentionPlan, dout: torch.Tensor, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor,
+                       lse: torch.Tensor, scale: float = None, q_grad: torch.Tensor = None, k_grad: torch.Tensor = None,
+                       v_grad: torch.Tensor = None):
+    """(q_grad, k_grad, v_grad), bf16 in the shapes of q, k and v, from dout, the gradient of attention's output in bf16, its
+    inputs, its output and its lse.  Tokens of no sequence are left as they were in gradients that are given (views of a
+    fused projection's gradient, for example), zeros in new ones.  The plan's sequences share no keys."""
+    D, hq, hk, hv = _inputs(plan, q, k, v)
+    dev = q.device
+    hg = _heads(dout, "dout", plan.heads, plan._queries[0], D, dev)
+    ho = _heads(out, "out", plan.heads, plan._queries[0], D, dev, (torch.bfloat16, torch.float32))
+    _expect(lse, "lse", torch.float32, (q.shape[0], plan.heads), dev)
+    q_grad, hdq = _output(q_grad, q, "q_grad", plan._queries, torch.bfloat16)
+    k_grad, hdk = _output(k_grad, k, "k_grad", plan._keys, torch.bfloat16)
+    v_grad, hdv = _output(v_grad, v, "v_grad", plan._keys, torch.bfloat16)
+    ws, ws_bytes = plan._workspace(D, 1, dev)
+    _call("attention_backward", dev, plan._h, hg, hq, hk, hv, ho, lse.data_ptr(), hdq, hdk, hdv, D,
+          1 / math.sqrt(D) if scale is None else scale, _ptr(ws), ws_bytes)
+    return q_grad, k_grad, v_grad

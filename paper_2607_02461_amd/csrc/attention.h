@@ -26,6 +26,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 #define ORBIT_LDS __attribute__((address_space(3)))
 
+__device__ __forceinline__ uint32_t lds_address(const char* p) { return (uint32_t)(uintptr_t)(const ORBIT_LDS char*)p; }
+
 constexpr float kLowest = -3.0e38f;   // stands for the largest of no scores
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kLog2e = 1.4426950408889634f;
@@ -76,7 +78,7 @@ struct TileLoads {
     }
     // rows first .. into the tile; those behind the last one are the last one
     __device__ __forceinline__ void load(int first, char* tile, int D, int lane) const {
-        const uint32_t lds = (uint32_t)(uintptr_t)(ORBIT_LDS char*)tile + to;
+        const uint32_t lds = lds_address(tile) + to;
         const char* const base = rows + first * stride;
         if (first + ROWS <= last + 1) {
 #pragma unroll
@@ -101,33 +103,28 @@ __device__ __forceinline__ void loads_done() {
     asm volatile("" ::: "memory");
 }
 
-// Where a lane reads operands of a tile: rows of it (row l % 32 of 32, chunk l / 32 of each pair), and columns of it.
+// Where a lane reads operands of a tile: rows of it (row l % 32 of 32, chunk l / 32 of each pair), and columns of it.  A chunk's
+// place is an exclusive or of its number and the row's, so the other places are one such operation from the first.
 template <int DP>
 struct Operands {
-    int row[DP / 16];        // bytes of the lane's chunk of k-step s
-    int column[DP / 32][2];  // of the lane's 4 values in 32 columns, for rows 8 a + 4 (l / 32) ..
+    int row, column;   // bytes: of chunk l / 32 of the lane's row, and of the lane's 4 values in columns 0 .. 31 of rows 4 (l / 32) ..
     __device__ __forceinline__ explicit Operands(int lane) {
-        const int r = lane & 31, half = lane >> 5;
-#pragma unroll
-        for (int s = 0; s < DP / 16; ++s) row[s] = r * (2 * DP) + 16 * swizzled<DP>(r, 2 * s + half);
-        const int i = lane & 15, of16 = lane >> 4 & 1;
-#pragma unroll
-        for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-            for (int a = 0; a < 2; ++a) {
-                const int key = 8 * a + 4 * half + (i >> 2), d = 32 * b + 16 * of16 + 4 * (i & 3);
-                column[b][a] = key * (2 * DP) + 16 * swizzled<DP>(key, d / 8) + 2 * (d & 7);
-            }
+        const int r = lane & 31, half = lane >> 5, i = lane & 15, key = 4 * half + (i >> 2), d = 16 * (lane >> 4 & 1) + 4 * (i & 3);
+        row = r * (2 * DP) + 16 * swizzled<DP>(r, half);
+        column = key * (2 * DP) + 16 * swizzled<DP>(key, d / 8) + 2 * (d & 7);
     }
     // rows 32 block .. of the tile, k-step s
     __device__ __forceinline__ u32x4 rows_of(const char* tile, int block, int s) const {
-        return *(const ORBIT_LDS u32x4*)(tile + block * 64 * DP + row[s]);
+        return *(const ORBIT_LDS u32x4*)(uintptr_t)(lds_address(tile) + block * 64 * DP + (row ^ 32 * s));
     }
-    // columns 32 b .., rows 16 step .. of the tile
+    // columns 32 b .., rows 16 step .. of the tile, 8 a + 4 (l / 32) .. of them
     __device__ __forceinline__ u32x4 columns_of(const char* tile, int step, int b) const {
-        const char* at = tile + step * 32 * DP;
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ORBIT_LDS s16x4*)(at + column[b][0])));
-        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((ORBIT_LDS s16x4*)(at + column[b][1])));
+        const uint32_t at = lds_address(tile) + step * 32 * DP;
+        auto four = [&](int a) {
+            return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                                                 (ORBIT_LDS s16x4*)(uintptr_t)(at + 16 * DP * a + (column ^ (64 * b | 32 * a)))));
+        };
+        const u32x2 lo = four(0), hi = four(1);
         return (u32x4){lo.x, lo.y, hi.x, hi.y};
     }
 };
@@ -174,6 +171,11 @@ __device__ __forceinline__ void store_column_f32(const f32x16 (&v)[DP / 32], flo
             if (live && d < D)
                 *(f32x4*)(row + d) = (f32x4){v[b][4 * a] * factor, v[b][4 * a + 1] * factor, v[b][4 * a + 2] * factor, v[b][4 * a + 3] * factor};
         }
+}
+
+// Keys of the sequence that a query sees
+__device__ __forceinline__ int seen_keys(int causal, int q_len, int k_len, int token) {
+    return causal ? max(0, min(k_len, token + 1 + k_len - q_len)) : k_len;
 }
 
 // Workgroups go round the 8 dies.  Those of one key head go to as few as they can, so that its keys and values stay in their

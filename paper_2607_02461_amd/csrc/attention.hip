@@ -120,11 +120,6 @@ __device__ __forceinline__ void finish(const AttnParams& p, const AttnTile& t, i
         p.lse[(int64_t)(t.q_start + token) * p.heads + head] = l == 0.f ? -__builtin_inff() : (mine.m + __builtin_log2f(l)) * kLn2;
 }
 
-// Keys of the sequence that a query sees
-__device__ __forceinline__ int seen_keys(const AttnParams& p, int q_len, int k_len, int token) {
-    return p.causal ? max(0, min(k_len, token + 1 + k_len - q_len)) : k_len;
-}
-
 // 128 rows to a workgroup, 32 to each wave; 64 keys at a time, shared, in two buffers.
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p) {
@@ -146,9 +141,9 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p) {
     const int r = min(t.first + row, rows - 1), token = r / p.group;
     load_operand<DP>(at(p.q, t.q_start + token, kv * p.group + r % p.group), p.D, lane, mine.q);
     mine.clear();
-    const int seen = seen_keys(p, t.q_len, t.k_len, token);
+    const int seen = seen_keys(p.causal, t.q_len, t.k_len, token);
     // keys that all of the tile's rows see
-    const int all = seen_keys(p, t.q_len, t.k_len, t.first / p.group);
+    const int all = seen_keys(p.causal, t.q_len, t.k_len, t.first / p.group);
     loads_done();
     __syncthreads();
     // in pairs, so that a buffer's place is part of the reads' instructions
@@ -192,8 +187,8 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     const int r = min(t.first + row, rows - 1), token = r / p.group;
     load_operand<DP>(at(p.q, t.q_start + token, kv * p.group + r % p.group), p.D, lane, mine.q);
     mine.clear();
-    const int seen = seen_keys(p, t.q_len, t.k_len, token);
-    const int all = seen_keys(p, t.q_len, t.k_len, t.first / p.group);
+    const int seen = seen_keys(p.causal, t.q_len, t.k_len, token);
+    const int all = seen_keys(p.causal, t.q_len, t.k_len, t.first / p.group);
     for (int buffer = 0; key < t.end; key += 128, buffer ^= 1) {
         if (key + 128 < t.end) {
             load(key + 128, buffer ^ 1);

@@ -16,7 +16,7 @@ using namespace orbit;
 namespace {
 
 constexpr int64_t kMaxTokens = INT32_MAX;
-constexpr int32_t kMaxHeads = 65535;
+constexpr int32_t kMaxHeads = 32767;
 constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 8;   // workgroups of 256 threads to a launch
 constexpr int64_t kMaxStride = (int64_t)1 << 24;         // elements from a token to the next: a tile's rows lie within 2^32 bytes
 
@@ -65,8 +65,8 @@ int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Lists of checked sequences.
 void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
-    const int64_t group = p->heads / p->kv_heads;
-    std::vector<Work> whole, few;
+    const int64_t group = p->heads / p->kv_heads, queries = std::max<int64_t>(1, 64 / group);   // of 64 rows
+    std::vector<Work> whole, few, every, keys;
     for (const Sequence& s : sequences) {
         const int64_t rows = s.q_len * group, most = rows <= kAttnFewRows ? kAttnFewRows : kAttnRows;
         for (int64_t first = 0; first < rows; first += most) {
@@ -77,13 +77,22 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
                 few.push_back({t, ceil_div(end, 128)});
             else
                 whole.push_back({t, ceil_div(end, 64)});
+            every.push_back({t, ceil_div(end, 64)});   // few rows are one tile here as well
+        }
+        for (int64_t first = 0; first < s.k_len; first += kAttnRows) {
+            // the first query that sees the tile's first key
+            const int64_t begin = p->causal ? std::min(s.q_len, std::max<int64_t>(0, first - (s.k_len - s.q_len))) : 0;
+            const AttnTile t{(int32_t)s.q_start, (int32_t)s.q_len, (int32_t)s.k_start, (int32_t)s.k_len, (int32_t)first, (int32_t)begin, (int32_t)s.q_len, -1};
+            keys.push_back({t, ceil_div(s.q_len - begin, queries)});
         }
     }
     std::vector<AttnTile> list[kAttnLists];
-    std::vector<AttnJoin> joins;
+    std::vector<AttnJoin> joins, row_joins, key_joins;
     // 512 workgroups of whole tiles are resident on 256 compute units, 256 of few rows
     divide(whole, p->kv_heads, 64, 8, 1024, &p->slots, &joins, &list[kAttnForward]);
     divide(few, p->kv_heads, 128, 2, 768, &p->slots, &joins, &list[kAttnFew]);
+    divide(every, p->kv_heads, 64, 8, 1024, &p->row_slots, &row_joins, &list[kAttnRowGrads]);
+    divide(keys, p->kv_heads, queries, 8, 1024, &p->key_slots, &key_joins, &list[kAttnKeyGrads]);
 
     std::vector<unsigned char>& blob = p->lists;
     auto append = [&](int which, const void* data, size_t count, size_t size) {
@@ -92,8 +101,10 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
         blob.resize(std::max<size_t>(p->at[which] + count * size, 16));
         if (count) std::memcpy(blob.data() + p->at[which], data, count * size);
     };
-    for (int i : {kAttnForward, kAttnFew}) append(i, list[i].data(), list[i].size(), sizeof(AttnTile));
+    for (int i : {kAttnForward, kAttnFew, kAttnRowGrads, kAttnKeyGrads}) append(i, list[i].data(), list[i].size(), sizeof(AttnTile));
     append(kAttnJoins, joins.data(), joins.size(), sizeof(AttnJoin));
+    append(kAttnRowJoins, row_joins.data(), row_joins.size(), sizeof(AttnJoin));
+    append(kAttnKeyJoins, key_joins.data(), key_joins.size(), sizeof(AttnJoin));
 }
 
 orbit_status upload_dev(orbit_attention p, int dev) {
@@ -159,6 +170,19 @@ orbit_status check_heads(const char* who, const char* name, const orbit_heads* t
 size_t slot_floats(int64_t D) { return (size_t)(attention_part((int)D) + 2 * kAttnRows); }
 
 size_t forward_bytes(orbit_attention p, int64_t D) { return (size_t)p->slots * p->kv_heads * slot_floats(D) * sizeof(float); }
+
+// Of the backward pass: lse and delta of each row, then the parts of dq, whose place those of dk and dv take afterwards.
+size_t stat_floats(orbit_attention p) { return ((size_t)p->heads * p->q_tokens + 63) / 64 * 64; }
+
+size_t backward_bytes(orbit_attention p, int64_t D) {
+    return (2 * stat_floats(p) + (size_t)std::max(p->row_slots, 2 * p->key_slots) * p->kv_heads * attention_part((int)D)) * sizeof(float);
+}
+
+// The backward pass finds a tile's heads by 32-bit offsets
+orbit_status check_group(const char* who, const char* name, const AttnHeads& t, int group) {
+    if (group > 1 && t.head > ((int64_t)1 << 29) / group) return fail(ORBIT_EUNSUPPORTED, "%s: %s's heads lie more than 2^29 values apart", who, name);
+    return ORBIT_OK;
+}
 
 }  // namespace
 
@@ -241,13 +265,13 @@ void attention_plan_destroy(orbit_attention p) {
     delete p;
 }
 
-orbit_status attention_workspace_size(orbit_attention p, int64_t D, size_t* bytes) {
+orbit_status attention_workspace_size(orbit_attention p, int64_t D, int32_t backward, size_t* bytes) {
     const char* who = "attention_workspace_size";
     clear_error();
     if (!bytes) return fail(ORBIT_EINVAL, "%s: null output pointer", who);
     *bytes = 0;
     const orbit_status st = check_dim(who, p, D);
-    if (st == ORBIT_OK) *bytes = forward_bytes(p, D);
+    if (st == ORBIT_OK) *bytes = backward ? backward_bytes(p, D) : forward_bytes(p, D);
     return st;
 }
 
@@ -299,6 +323,78 @@ orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_head
     if (!a.count) return ORBIT_OK;
     const hipError_t e = launch_attention_join(a, (hipStream_t)stream);
     return e == hipSuccess ? ORBIT_OK : hip_fail(e, who);
+}
+
+orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, const orbit_heads* q, const orbit_heads* k, const orbit_heads* v,
+                                const orbit_heads* out, const float* lse, const orbit_heads* dq, const orbit_heads* dk, const orbit_heads* dv, int64_t D,
+                                float scale, void* workspace, size_t workspace_bytes, void* stream) {
+    const char* who = "attention_backward";
+    clear_error();
+    orbit_status st = check_dim(who, p, D);
+    if (st != ORBIT_OK) return st;
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ORBIT_EINVAL, "%s: scale must be finite and above 0", who);
+    if (p->shared_keys) return fail(ORBIT_EINVAL, "%s: two of the plan's sequences have a key in common", who);
+    AttnGradParams a{};
+    st = check_heads(who, "dout", dout, p->q_tokens, p->heads, D, false, false, &a.g);
+    if (st == ORBIT_OK) st = check_heads(who, "q", q, p->q_tokens, p->heads, D, false, false, &a.q);
+    if (st == ORBIT_OK) st = check_heads(who, "k", k, p->k_tokens, p->kv_heads, D, false, false, &a.k);
+    if (st == ORBIT_OK) st = check_heads(who, "v", v, p->k_tokens, p->kv_heads, D, false, false, &a.v);
+    if (st == ORBIT_OK) st = check_heads(who, "out", out, p->q_tokens, p->heads, D, true, false, &a.o);
+    if (st == ORBIT_OK) st = check_heads(who, "dq", dq, p->q_tokens, p->heads, D, false, true, &a.dq);
+    if (st == ORBIT_OK) st = check_heads(who, "dk", dk, p->k_tokens, p->kv_heads, D, false, true, &a.dk);
+    if (st == ORBIT_OK) st = check_heads(who, "dv", dv, p->k_tokens, p->kv_heads, D, false, true, &a.dv);
+    if (st != ORBIT_OK) return st;
+    a.group = p->heads / p->kv_heads;
+    st = check_group(who, "q", a.q, a.group);
+    if (st == ORBIT_OK) st = check_group(who, "dout", a.g, a.group);
+    if (st != ORBIT_OK) return st;
+    const void* const inputs[] = {a.g.p, a.q.p, a.k.p, a.v.p, a.o.p};
+    const void* const outputs[] = {a.dq.p, a.dk.p, a.dv.p};
+    for (int i = 0; i < 3; ++i) {
+        for (const void* other : inputs)
+            if (outputs[i] && outputs[i] == other) return fail(ORBIT_EINVAL, "%s: a gradient lies on an input", who);
+        if (outputs[i] && outputs[i] == outputs[(i + 1) % 3]) return fail(ORBIT_EINVAL, "%s: two gradients lie in one place", who);
+    }
+    if (p->q_tokens == 0 && p->k_tokens == 0) return ORBIT_OK;
+    if (p->q_tokens && (!lse || !aligned(lse, 4))) return fail(ORBIT_EINVAL, "%s: lse is a null or misaligned device pointer", who);
+    const size_t bytes = backward_bytes(p, D);
+    if (bytes && (!workspace || !aligned(workspace, 16) || workspace_bytes < bytes))
+        return fail(ORBIT_EINVAL, "%s: takes a workspace of %zu bytes, aligned to 16", who, bytes);
+    int dev;
+    DeviceInfo info;
+    st = current_device(&dev, &info);
+    if (st != ORBIT_OK) return st;
+    const unsigned char* lists = nullptr;
+    st = lists_on(who, p, dev, &lists);
+    if (st != ORBIT_OK) return st;
+    a.heads = p->heads;
+    a.kv_heads = p->kv_heads;
+    a.D = (int)D;
+    a.causal = p->causal;
+    a.o_f32 = out && out->dtype == ORBIT_OUT_F32;
+    a.q_tokens = p->q_tokens;
+    a.scale = (float)(scale * 1.4426950408889634);
+    a.out_scale = scale;
+    a.lse = lse;
+    a.lse2 = (float*)workspace;
+    a.delta = a.lse2 + stat_floats(p);
+    a.part = a.delta + stat_floats(p);
+    a.part2 = a.part + p->key_slots * p->kv_heads * attention_part((int)D);
+    const struct {
+        AttnGradStep step;
+        int list;
+    } steps[] = {{kAttnDelta, -1}, {kAttnRowGrad, kAttnRowGrads}, {kAttnRowJoin, kAttnRowJoins}, {kAttnKeyGrad, kAttnKeyGrads}, {kAttnKeyJoin, kAttnKeyJoins}};
+    for (const auto& s : steps) {
+        if (s.list >= 0) {
+            a.count = (int)p->count[s.list];
+            a.tiles = (const AttnTile*)(lists + p->at[s.list]);
+            a.joins = (const AttnJoin*)(lists + p->at[s.list]);
+        }
+        if (s.list >= 0 ? a.count == 0 : p->q_tokens == 0) continue;
+        const hipError_t e = launch_attention_grad(a, s.step, (hipStream_t)stream);
+        if (e != hipSuccess) return hip_fail(e, who);
+    }
+    return ORBIT_OK;
 }
 
 }  // extern "C"

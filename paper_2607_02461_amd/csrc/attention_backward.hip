@@ -1,0 +1,362 @@
+// Gradients of attention over packed sequences for gfx950.
+//
+// With p = softmax(scale q k^T), dp = do v^T and delta = sum(do o) for each query, ds = p (dp - delta):
+//     dq = scale ds k,   dk = scale ds^T q,   dv = p^T do.
+// p comes from the scores and the forward pass's lse again.  Two kernels go over the pairs: one has 128 rows and all of their
+// keys, for dq; the other 128 keys and all of their rows, for dk and dv.  So every sum is one workgroup's, in a fixed order, and no
+// result is added up in memory; that costs 7 products of 2 D operations for each pair instead of the 5 that there are.
+//
+// Both are bound by the matrix cores: 3 and 4 products for each pair beside one exponential.  p and ds enter their products in
+// bf16, half a step of 2^-8 relative, as q, k, v and do have it; sums are fp32.
+//
+// Rows are those of the forward pass: row = token * group + head of the group; dk and dv sum over a group's heads as over
+// tokens.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "attention.h"
+#include "device.h"
+#include "vec.h"
+
+namespace orbit {
+
+namespace {
+
+__device__ __forceinline__ const uint16_t* at(const AttnHeads& t, int64_t token, int head) {
+    return (const uint16_t*)t.p + token * t.token + head * t.head;
+}
+
+// For each row its sum of do o, and lse in units of log2 (infinite where the row sees no key: its probabilities are zeros then),
+// [key head][token * group + head of the group]: DP / 8 lanes to a row.
+template <int DP>
+__global__ __launch_bounds__(256) void attention_delta_kernel(AttnGradParams p) {
+    constexpr int kLanes = DP / 8;
+    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
+    if (id >= p.q_tokens * p.heads) return;
+    const int64_t token = id / p.heads;
+    const int head = (int)(id - token * p.heads), d = threadIdx.x % kLanes * 8;
+    float sum = 0.f;
+    if (d < p.D) {
+        float a[8], b[8];
+        const u32x4 g = *(const u32x4*)(at(p.g, token, head) + d);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[2 * i] = bf16_low(g[i]), a[2 * i + 1] = bf16_high(g[i]);
+        const int64_t from = token * p.o.token + head * p.o.head + d;
+        if (p.o_f32) {
+            const f32x4 lo = *(const f32x4*)((const float*)p.o.p + from), hi = *(const f32x4*)((const float*)p.o.p + from + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[i] = lo[i], b[4 + i] = hi[i];
+        } else {
+            const u32x4 o = *(const u32x4*)((const uint16_t*)p.o.p + from);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[2 * i] = bf16_low(o[i]), b[2 * i + 1] = bf16_high(o[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += a[i] * b[i];
+    }
+#pragma unroll
+    for (int apart = 1; apart < kLanes; apart *= 2) sum += __shfl_xor(sum, apart);
+    if (d) return;
+    const int kv = head / p.group;
+    const int64_t to = (kv * p.q_tokens + token) * p.group + (head - kv * p.group);
+    const float lse = p.lse[token * p.heads + head];
+    p.delta[to] = -sum;
+    p.lse2[to] = lse == -__builtin_inff() ? lse : -lse * kLog2e / p.scale;
+}
+
+// dq of 128 rows, 32 to each wave, over their keys, 64 at a time in two buffers.  Transposed as in the forward pass: a lane has
+// one query.
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradParams p) {
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * 2 * DP];
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
+    if (place.tile >= p.count) return;
+    const AttnTile t = p.tiles[place.tile];
+    const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const TileLoads<DP, 64, 4> k(at(p.k, t.k_start, kv), p.k.token, t.k_len - 1, p.D, wave, lane);
+    const TileLoads<DP, 64, 4> v(at(p.v, t.k_start, kv), p.v.token, t.k_len - 1, p.D, wave, lane);
+    auto load = [&](int key, int buffer) {
+        k.load(key, lds[buffer][0], p.D, lane);
+        v.load(key, lds[buffer][1], p.D, lane);
+    };
+    if (t.begin < t.end) load(t.begin, 0);
+    const Operands<DP> where(lane);
+    const int row = 32 * wave + (lane & 31), rows = t.q_len * p.group;
+    const int r = min(t.first + row, rows - 1), token = r / p.group, head = kv * p.group + r % p.group;
+    u32x4 q[DP / 16], g[DP / 16];
+    load_operand<DP>(at(p.q, t.q_start + token, head), p.D, lane, q);
+    load_operand<DP>(at(p.g, t.q_start + token, head), p.D, lane, g);
+    const int64_t stat = ((int64_t)kv * p.q_tokens + t.q_start) * p.group + r;
+    const float lse2 = p.lse2[stat] * p.scale, delta = p.delta[stat];
+    f32x16 dq[DP / 32];
+#pragma unroll
+    for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dq[b][i] = 0.f;
+    const int seen = seen_keys(p.causal, t.q_len, t.k_len, token), all = seen_keys(p.causal, t.q_len, t.k_len, t.first / p.group);
+    loads_done();
+    __syncthreads();
+    for (int key = t.begin; key < t.end;) {
+#pragma unroll
+        for (int buffer = 0; buffer < 2; ++buffer) {
+            if (key >= t.end) break;
+            if (key + 64 < t.end) load(key + 64, buffer ^ 1);
+            const char *const kt = lds[buffer][0], *const vt = lds[buffer][1];
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                f32x16 s, dp;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+#pragma unroll
+                for (int step = 0; step < DP / 16; ++step) {
+                    s = mfma32(where.rows_of(kt, n, step), q[step], s);
+                    dp = mfma32(where.rows_of(vt, n, step), g[step], dp);
+                }
+                if (key + 64 > all) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const bool hidden = 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= seen - key;
+                        s[i] = hidden ? -__builtin_inff() : s[i];
+                        dp[i] = hidden ? -delta : dp[i];
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 16; ++i) dp[i] = exp2_fast(__builtin_fmaf(s[i], p.scale, lse2)) * (dp[i] + delta);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const u32x4 ds = as_operand(dp, u);
+#pragma unroll
+                    for (int b = 0; b < DP / 32; ++b) dq[b] = mfma32(where.columns_of(kt, 2 * n + u, b), ds, dq[b]);
+                }
+            }
+            loads_done();
+            __syncthreads();
+            key += 64;
+        }
+    }
+    const bool live = t.first + row < rows;
+    if (t.slot >= 0)
+        store_column_f32<DP>(dq, 1.f, p.part + (((int64_t)t.slot * p.kv_heads + kv) * kAttnRows + row) * DP, DP, lane, live);
+    else
+        store_column<DP>(dq, p.out_scale, (uint16_t*)at(p.dq, t.q_start + token, head), p.D, lane, live);
+}
+
+// Loads of 64 rows (token * group + head of the group) of one key head's queries, as TileLoads.
+template <int DP, int WAVES>
+struct RowLoads {
+    static constexpr int kChunks = DP / 8, kEach = 64 / kChunks, kLoads = 64 / kEach / WAVES;
+    const char* rows;
+    int64_t token;    // bytes
+    uint32_t head;    // bytes
+    int group, last;  // last: row
+    uint32_t inverse; // 2^32 / group, rounded up: n * inverse >> 32 is n / group for n < 2^16
+    __device__ __forceinline__ RowLoads(const uint16_t* t, int64_t token, int64_t head, int group, int last)
+        : rows((const char*)t), token(2 * token), head((uint32_t)(2 * head)), group(group), last(last), inverse((uint32_t)(0xFFFFFFFFull / (uint32_t)group) + 1) {}
+    __device__ __forceinline__ void load(int first, char* tile, int D, int wave, int lane) const {
+        const uint32_t lds = lds_address(tile) + wave * kLoads * 1024;
+        const int from = first / group, rest = first - from * group;   // scalar
+        const char* const base = rows + from * token;
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) {
+            const int row = (wave * kLoads + i) * kEach + lane / kChunks;
+            const int c = swizzled<DP>(row, lane % kChunks);
+            const uint32_t r = (uint32_t)(rest + min(row, last - first));
+            const uint32_t ahead = group == 1 ? r : __umulhi(r, inverse);
+            const uint32_t offset = ahead * (uint32_t)token + (r - ahead * group) * head + (8 * c >= D ? 0 : 16 * c);
+            TileLoads<DP, 64, WAVES>::one(base, offset, lds + 1024 * i);
+        }
+    }
+};
+
+// dk and dv of 128 keys, 32 NK to each wave, over the rows that see them, 64 at a time in two buffers: q, do, lse2 and delta.  A lane
+// has one key of each 32.  At D = 128 a wave's keys, values and sums take 192 registers for 32 keys; 64 take all 512 of a wave
+// alone on its SIMD, and each operand that is read from LDS serves twice.
+template <int DP, int NK>
+__global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_kernel(AttnGradParams p) {
+    constexpr int kTile = 64 * 2 * DP, kBuffer = 2 * kTile + 1024, kWaves = 4 / NK;
+    extern __shared__ __attribute__((aligned(1024))) char key_lds[];
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
+    if (place.tile >= p.count) return;
+    const AttnTile t = p.tiles[place.tile];
+    const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int rows = t.q_len * p.group, begin = t.begin * p.group, end = t.end * p.group;
+    const RowLoads<DP, kWaves> q(at(p.q, t.q_start, kv * p.group), p.q.token, p.q.head, p.group, rows - 1);
+    const RowLoads<DP, kWaves> g(at(p.g, t.q_start, kv * p.group), p.g.token, p.g.head, p.group, rows - 1);
+    const int64_t stat = ((int64_t)kv * p.q_tokens + t.q_start) * p.group;
+    const char* const stats = (const char*)((wave & 1 ? p.delta : p.lse2) + stat);
+    auto load = [&](int row, int buffer) {
+        char* const to = key_lds + buffer * kBuffer;
+        int lane = threadIdx.x & 63;
+        asm volatile("" : "+v"(lane));   // what is made of it is made again for each tile: the registers are taken
+        q.load(row, to, p.D, wave, lane);
+        g.load(row, to + kTile, p.D, wave, lane);
+        if (wave < 2)
+            asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(lds_address(to) + 2 * kTile + 256 * wave),
+                         "v"((uint32_t)(4 * min(lane, rows - 1 - row))), "s"(stats + 4 * (int64_t)row)
+                         : "memory");
+    };
+    if (begin < end) load(begin, 0);
+    Operands<DP> where(lane);
+    int key[NK];
+    u32x4 k[NK][DP / 16], v[NK][DP / 16];
+    f32x16 dk[NK][DP / 32], dv[NK][DP / 32];
+#pragma unroll
+    for (int m = 0; m < NK; ++m) {
+        key[m] = t.first + 32 * (NK * wave + m) + (lane & 31);
+        load_operand<DP>(at(p.k, t.k_start + min(key[m], t.k_len - 1), kv), p.D, lane, k[m]);
+        load_operand<DP>(at(p.v, t.k_start + min(key[m], t.k_len - 1), kv), p.D, lane, v[m]);
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dk[m][b][i] = dv[m][b][i] = 0.f;
+    }
+    // the first row that sees all of the tile's keys
+    const int shift = t.k_len - t.q_len;
+    const int all = p.causal ? max(0, min(t.first + kAttnRows, t.k_len) - 1 - shift) * p.group : 0;
+    loads_done();
+    __syncthreads();
+    for (int row = begin; row < end;) {
+#pragma unroll
+        for (int buffer = 0; buffer < 2; ++buffer) {
+            if (row >= end) break;
+            if (row + 64 < end) load(row + 64, buffer ^ 1);
+            const char *const qt = key_lds + buffer * kBuffer, *const gt = qt + kTile;
+#pragma unroll
+            for (int n = 0; n < 2; ++n) {
+                f32x16 s[NK], dp[NK];
+                asm volatile("" : "+v"(where.row), "+v"(where.column));
+#pragma unroll
+                for (int m = 0; m < NK; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const char* const from = gt + kTile + 4 * (32 * n + 8 * (i / 4) + 4 * (lane >> 5));
+                        s[m][i] = (*(const ORBIT_LDS f32x4*)from)[i % 4];
+                        dp[m][i] = (*(const ORBIT_LDS f32x4*)(from + 256))[i % 4];
+                    }
+#pragma unroll
+                for (int step = 0; step < DP / 16; ++step) {
+                    const u32x4 a = where.rows_of(qt, n, step), b = where.rows_of(gt, n, step);
+#pragma unroll
+                    for (int m = 0; m < NK; ++m) {
+                        s[m] = mfma32(a, k[m][step], s[m]);
+                        dp[m] = mfma32(b, v[m][step], dp[m]);
+                    }
+                }
+                const bool masked = row < all || row + 64 > end;
+#pragma unroll
+                for (int m = 0; m < NK; ++m)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        s[m][i] = exp2_fast(s[m][i] * p.scale);
+                        dp[m][i] *= s[m][i];
+                    }
+                if (masked) {
+#pragma unroll
+                    for (int m = 0; m < NK; ++m) {
+                        const int first = p.causal ? max(0, key[m] - shift) * p.group : 0;   // that sees the lane's key
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            const int r = row + 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+                            const bool live = r >= first && r < end;
+                            s[m][i] = live ? s[m][i] : 0.f;
+                            dp[m][i] = live ? dp[m][i] : 0.f;
+                        }
+                    }
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    u32x4 pb[NK], ds[NK];
+#pragma unroll
+                    for (int m = 0; m < NK; ++m) pb[m] = as_operand(s[m], u), ds[m] = as_operand(dp[m], u);
+#pragma unroll
+                    for (int b = 0; b < DP / 32; ++b) {
+                        const u32x4 gc = where.columns_of(gt, 2 * n + u, b), qc = where.columns_of(qt, 2 * n + u, b);
+#pragma unroll
+                        for (int m = 0; m < NK; ++m) {
+                            dv[m][b] = mfma32(gc, pb[m], dv[m][b]);
+                            dk[m][b] = mfma32(qc, ds[m], dk[m][b]);
+                        }
+                    }
+                }
+            }
+            loads_done();
+            __syncthreads();
+            row += 64;
+        }
+    }
+#pragma unroll
+    for (int m = 0; m < NK; ++m) {
+        const bool live = key[m] < t.k_len;
+        if (t.slot >= 0) {
+            const int64_t to = (((int64_t)t.slot * p.kv_heads + kv) * kAttnRows + 32 * (NK * wave + m) + (lane & 31)) * DP;
+            store_column_f32<DP>(dk[m], 1.f, p.part + to, DP, lane, live);
+            store_column_f32<DP>(dv[m], 1.f, p.part2 + to, DP, lane, live);
+        } else {
+            const int64_t token = t.k_start + min(key[m], t.k_len - 1);
+            store_column<DP>(dk[m], p.out_scale, (uint16_t*)at(p.dk, token, kv), p.D, lane, live);
+            store_column<DP>(dv[m], 1.f, (uint16_t*)at(p.dv, token, kv), p.D, lane, live);
+        }
+    }
+}
+
+// Sums of the parts of tiles that several workgroups shared, in the order of their slots: DP / 8 lanes to a row or key.
+template <int DP>
+__global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams p, bool keys) {
+    constexpr int kLanes = DP / 8;
+    const uint32_t id = (blockIdx.x * 256 + threadIdx.x) / kLanes;
+    const int row = id % kAttnRows, kv = id / kAttnRows % (uint32_t)p.kv_heads, d = threadIdx.x % kLanes * 8;
+    const AttnJoin j = p.joins[id / kAttnRows / (uint32_t)p.kv_heads];
+    const int r = j.first + row;
+    if (r >= (keys ? j.k_len : j.q_len * p.group) || d >= p.D) return;
+    for (int which = 0; which < (keys ? 2 : 1); ++which) {
+        const float* const part = which ? p.part2 : p.part;
+        float sum[8] = {};
+        for (int i = 0; i < j.count; ++i) {
+            const float* const from = part + (((int64_t)(j.slot + i) * p.kv_heads + kv) * kAttnRows + row) * DP + d;
+            const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) sum[c] += lo[c], sum[4 + c] += hi[c];
+        }
+        const float factor = which ? 1.f : p.out_scale;
+        u32x4 w;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) w[c] = pack_bf16(sum[2 * c] * factor, sum[2 * c + 1] * factor);
+        const uint16_t* const to = keys ? at(which ? p.dv : p.dk, j.k_start + r, kv) : at(p.dq, j.q_start + r / p.group, kv * p.group + r % p.group);
+        *(u32x4*)(to + d) = w;
+    }
+}
+
+template <int DP>
+hipError_t launch(const AttnGradParams& p, AttnGradStep step, hipStream_t stream) {
+    const unsigned grid = step == kAttnDelta ? 0 : (unsigned)places(p.count, p.kv_heads);
+    switch (step) {
+        case kAttnDelta:
+            attention_delta_kernel<DP><<<(unsigned)((p.q_tokens * p.heads * (DP / 8) + 255) / 256), 256, 0, stream>>>(p);
+            break;
+        case kAttnRowGrad:
+            attention_row_grad_kernel<DP><<<grid, 256, 0, stream>>>(p);
+            break;
+        case kAttnKeyGrad: {
+            constexpr int kKeys = 1, kBytes = 2 * (2 * 64 * 2 * DP + 1024);
+            static std::atomic<uint64_t> raised{0};
+            const hipError_t e = raise_lds_limit((const void*)attention_key_grad_kernel<DP, kKeys>, kBytes, raised);
+            if (e != hipSuccess) return e;
+            attention_key_grad_kernel<DP, kKeys><<<grid, 256 / kKeys, kBytes, stream>>>(p);
+            break;
+        }
+        default:
+            attention_grad_join_kernel<DP><<<(unsigned)((int64_t)p.count * p.kv_heads * kAttnRows * (DP / 8) / 256), 256, 0, stream>>>(p, step == kAttnKeyJoin);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_attention_grad(const AttnGradParams& p, AttnGradStep step, hipStream_t stream) {
+    return p.D > 64 ? launch<128>(p, step, stream) : launch<64>(p, step, stream);
+}
+
+}  // namespace orbit

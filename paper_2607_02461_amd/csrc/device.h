@@ -367,4 +367,21 @@ constexpr int64_t attention_part(int D) { return (int64_t)kAttnRows * (D > 64 ? 
 hipError_t launch_attention(const AttnParams& p, bool few, hipStream_t stream);
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream);
 
+struct AttnGradParams {
+    const AttnTile* tiles;
+    const AttnJoin* joins;
+    int count;                // of the tiles, or of the joins
+    int heads, kv_heads, group, D;
+    int causal, o_f32;
+    int64_t q_tokens;
+    float scale, out_scale;   // of the scores times log2(e), and of dq and dk
+    AttnHeads q, k, v, o, g, dq, dk, dv;   // g: the output's gradient
+    const float* lse;         // [token][heads]
+    float *lse2, *delta;      // [key head][token * group + head of the group]
+    float *part, *part2;      // [slot][key head][row or key][padded D]: of dq; of dk and of dv
+};
+
+enum AttnGradStep { kAttnDelta, kAttnRowGrad, kAttnKeyGrad, kAttnRowJoin, kAttnKeyJoin };
+hipError_t launch_attention_grad(const AttnGradParams& p, AttnGradStep step, hipStream_t stream);
+
 }  // namespace orbit
