@@ -38,6 +38,8 @@ from .qlinear import layer_epilogue, qlinear, qlinear_dense_reference
 from .adaln_rtn import rtn_int4_quantize, rtn_int4_dequantize, pack_rtn_int4, unpack_rtn_int4, rtn_int4_linear
 from .attention_input import rope_angles, rope_turn, qk_norm_rope, qk_norm_rope_backward
 from .lora import lora_add, lora_add_backward
+from .layer_norm import layer_norm, layer_norm_backward
+from .attention import attention, attention_backward, probabilities as attention_probabilities
 
 EPS_DEFAULT = 1e-10  # Sec. 4.3: the clamp guarding zero-norm (padding) tokens
 
@@ -51,4 +53,5 @@ __all__ = [
     "rtn_int4_quantize", "rtn_int4_dequantize", "pack_rtn_int4", "unpack_rtn_int4", "rtn_int4_linear",
     "rope_angles", "rope_turn", "qk_norm_rope", "qk_norm_rope_backward",
     "lora_add", "lora_add_backward",
+    "layer_norm", "layer_norm_backward", "attention", "attention_backward", "attention_probabilities",
 ]

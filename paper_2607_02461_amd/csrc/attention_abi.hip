@@ -89,10 +89,10 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
     std::vector<AttnTile> list[kAttnLists];
     std::vector<AttnJoin> joins, row_joins, key_joins;
     // 512 workgroups of whole tiles are resident on 256 compute units, 256 of few rows
-    divide(whole, p->kv_heads, 64, 8, 1024, &p->slots, &joins, &list[kAttnForward]);
+    divide(whole, p->kv_heads, 64, 4, 1024, &p->slots, &joins, &list[kAttnForward]);
     divide(few, p->kv_heads, 128, 2, 768, &p->slots, &joins, &list[kAttnFew]);
-    divide(every, p->kv_heads, 64, 8, 1024, &p->row_slots, &row_joins, &list[kAttnRowGrads]);
-    divide(keys, p->kv_heads, queries, 8, 1024, &p->key_slots, &key_joins, &list[kAttnKeyGrads]);
+    divide(every, p->kv_heads, 64, 4, 1024, &p->row_slots, &row_joins, &list[kAttnRowGrads]);
+    divide(keys, p->kv_heads, queries, 4, 1024, &p->key_slots, &key_joins, &list[kAttnKeyGrads]);
 
     std::vector<unsigned char>& blob = p->lists;
     auto append = [&](int which, const void* data, size_t count, size_t size) {

@@ -29,42 +29,44 @@ __device__ __forceinline__ const uint16_t* at(const AttnHeads& t, int64_t token,
     return (const uint16_t*)t.p + token * t.token + head * t.head;
 }
 
-// For each row its sum of do o, and lse in units of log2 (infinite where the row sees no key: its probabilities are zeros then),
-// [key head][token * group + head of the group]: DP / 8 lanes to a row.
+// For each row -sum(do o), and -lse in units of the scores (-infinite where the row sees no key: its probabilities are zeros then),
+// [key head][token * group + head of the group]: what the products of the next kernels begin from.  DP / 8 lanes to a row.
 template <int DP>
 __global__ __launch_bounds__(256) void attention_delta_kernel(AttnGradParams p) {
     constexpr int kLanes = DP / 8;
-    const int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes;
-    if (id >= p.q_tokens * p.heads) return;
-    const int64_t token = id / p.heads;
-    const int head = (int)(id - token * p.heads), d = threadIdx.x % kLanes * 8;
-    float sum = 0.f;
-    if (d < p.D) {
-        float a[8], b[8];
-        const u32x4 g = *(const u32x4*)(at(p.g, token, head) + d);
+    const int d = threadIdx.x % kLanes * 8;
+    const int64_t rows = p.q_tokens * p.heads;
+    for (int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes; id < rows; id += (int64_t)gridDim.x * (256 / kLanes)) {
+        const int64_t token = id / p.heads;
+        const int head = (int)(id - token * p.heads);
+        float sum = 0.f;
+        if (d < p.D) {
+            float a[8], b[8];
+            const u32x4 g = *(const u32x4*)(at(p.g, token, head) + d);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) a[2 * i] = bf16_low(g[i]), a[2 * i + 1] = bf16_high(g[i]);
-        const int64_t from = token * p.o.token + head * p.o.head + d;
-        if (p.o_f32) {
-            const f32x4 lo = *(const f32x4*)((const float*)p.o.p + from), hi = *(const f32x4*)((const float*)p.o.p + from + 4);
+            for (int i = 0; i < 4; ++i) a[2 * i] = bf16_low(g[i]), a[2 * i + 1] = bf16_high(g[i]);
+            const int64_t from = token * p.o.token + head * p.o.head + d;
+            if (p.o_f32) {
+                const f32x4 lo = *(const f32x4*)((const float*)p.o.p + from), hi = *(const f32x4*)((const float*)p.o.p + from + 4);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) b[i] = lo[i], b[4 + i] = hi[i];
-        } else {
-            const u32x4 o = *(const u32x4*)((const uint16_t*)p.o.p + from);
+                for (int i = 0; i < 4; ++i) b[i] = lo[i], b[4 + i] = hi[i];
+            } else {
+                const u32x4 o = *(const u32x4*)((const uint16_t*)p.o.p + from);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) b[2 * i] = bf16_low(o[i]), b[2 * i + 1] = bf16_high(o[i]);
+                for (int i = 0; i < 4; ++i) b[2 * i] = bf16_low(o[i]), b[2 * i + 1] = bf16_high(o[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += a[i] * b[i];
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += a[i] * b[i];
+        for (int apart = 1; apart < kLanes; apart *= 2) sum += __shfl_xor(sum, apart);
+        if (d) continue;
+        const int kv = head / p.group;
+        const int64_t to = (kv * p.q_tokens + token) * p.group + (head - kv * p.group);
+        const float lse = p.lse[token * p.heads + head];
+        p.delta[to] = -sum;
+        p.lse2[to] = lse == -__builtin_inff() ? lse : -lse * kLog2e / p.scale;
     }
-#pragma unroll
-    for (int apart = 1; apart < kLanes; apart *= 2) sum += __shfl_xor(sum, apart);
-    if (d) return;
-    const int kv = head / p.group;
-    const int64_t to = (kv * p.q_tokens + token) * p.group + (head - kv * p.group);
-    const float lse = p.lse[token * p.heads + head];
-    p.delta[to] = -sum;
-    p.lse2[to] = lse == -__builtin_inff() ? lse : -lse * kLog2e / p.scale;
 }
 
 // dq of 128 rows, 32 to each wave, over their keys, 64 at a time in two buffers.  Transposed as in the forward pass: a lane has
@@ -334,7 +336,7 @@ hipError_t launch(const AttnGradParams& p, AttnGradStep step, hipStream_t stream
     const unsigned grid = step == kAttnDelta ? 0 : (unsigned)places(p.count, p.kv_heads);
     switch (step) {
         case kAttnDelta:
-            attention_delta_kernel<DP><<<(unsigned)((p.q_tokens * p.heads * (DP / 8) + 255) / 256), 256, 0, stream>>>(p);
+            attention_delta_kernel<DP><<<(unsigned)std::min<int64_t>((p.q_tokens * p.heads * (DP / 8) + 255) / 256, 1 << 20), 256, 0, stream>>>(p);
             break;
         case kAttnRowGrad:
             attention_row_grad_kernel<DP><<<grid, 256, 0, stream>>>(p);

@@ -185,13 +185,13 @@ __device__ __forceinline__ int wave_values(int w, int N) {
 
 // A wave's mean, the deviations from it in v's place (zeros for what the row does not have) and their sum of squares
 template <int V, int C>
-__device__ __forceinline__ void wave_statistics(float (&v)[C][V], const Columns<V, C>& k, float inv_n, float* mean, float* squares) {
+__device__ __forceinline__ void wave_statistics(float (&v)[C][V], const Columns<V, C>& k, float n, float* mean, float* squares) {
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int i = 0; i < V; ++i) sum += v[c][i];
-    *mean = wave_sum(sum) * inv_n;
+    *mean = n ? wave_sum(sum) / n : 0.f;   // a quotient: a row of equal values has that value for a mean
     float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
@@ -210,10 +210,10 @@ struct Joined {
 
 // What the waves found of a row, joined.  part[w]: n_w times its mean, squares, and backward sum h and sum h (x - m_w).
 template <int Q>
-__device__ __forceinline__ Joined join(const float (*part)[Q], const float* count, int waves, int wave, float inv_N) {
+__device__ __forceinline__ Joined join(const float (*part)[Q], const float* count, int waves, int wave, float N) {
     float total = 0.f;
     for (int w = 0; w < waves; ++w) total += part[w][0] * count[w];
-    const float mean = total * inv_N;
+    const float mean = total / N;
     Joined j{part[wave][0] - mean, 0.f, 0.f, 0.f};
     for (int w = 0; w < waves; ++w) {
         const float d = part[w][0] - mean;
@@ -240,7 +240,7 @@ __global__ __launch_bounds__((C * values_of<TX, TY>() > 8 ? 512 : 1024)) void la
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const Columns<V, C> k(p.N);
     const int n = wave_values<V, C>(wave, p.N);
-    const float inv_n = n ? 1.f / n : 0.f, inv_N = 1.f / p.N;
+    const float inv_N = 1.f / p.N;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
     const int64_t g = blockIdx.x / (uint32_t)p.parts;
     int64_t row = blockIdx.x % (uint32_t)p.parts, b = g, l = row;
@@ -264,10 +264,10 @@ __global__ __launch_bounds__((C * values_of<TX, TY>() > 8 ? 512 : 1024)) void la
             next.load(row_of<const TX>(p.x, b, l), k);
         }
         float mean, squares;
-        wave_statistics<V, C>(v, k, inv_n, &mean, &squares);
+        wave_statistics<V, C>(v, k, n, &mean, &squares);
         if ((threadIdx.x & 63) == 0) part[turn][wave][0] = mean, part[turn][wave][1] = squares;
         __syncthreads();
-        const Joined j = join<2>(part[turn], count, waves, wave, inv_N);
+        const Joined j = join<2>(part[turn], count, waves, wave, p.N);
         const float r = rsqrtf(j.squares * inv_N + p.eps);
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -285,7 +285,7 @@ __global__ __launch_bounds__((C * values_of<TX, TG>() > 8 ? 512 : 1024)) void la
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const Columns<V, C> k(p.N);
     const int n = wave_values<V, C>(wave, p.N);
-    const float inv_n = n ? 1.f / n : 0.f, inv_N = 1.f / p.N;
+    const float inv_N = 1.f / p.N;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
     const int64_t g = blockIdx.x / (uint32_t)p.parts;
     int64_t row = blockIdx.x % (uint32_t)p.parts, b = g, l = row;
@@ -318,7 +318,7 @@ __global__ __launch_bounds__((C * values_of<TX, TG>() > 8 ? 512 : 1024)) void la
             next_g.load(row_of<const TG>(p.g, b, l), k);
         }
         float mean, squares, sum = 0.f, dot = 0.f;
-        wave_statistics<V, C>(v, k, inv_n, &mean, &squares);
+        wave_statistics<V, C>(v, k, n, &mean, &squares);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -334,7 +334,7 @@ __global__ __launch_bounds__((C * values_of<TX, TG>() > 8 ? 512 : 1024)) void la
             part[turn][wave][2] = sum, part[turn][wave][3] = dot;
         }
         __syncthreads();
-        const Joined j = join<4>(part[turn], count, waves, wave, inv_N);
+        const Joined j = join<4>(part[turn], count, waves, wave, p.N);
         const float r = rsqrtf(j.squares * inv_N + p.eps);
         const float mean_h = j.sum * inv_N, mean_hn = r * (j.dot * inv_N);
 #pragma unroll
