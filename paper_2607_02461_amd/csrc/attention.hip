@@ -48,10 +48,29 @@ struct Queries {
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int i = 0; i < 16; ++i) s[n][i] = 0.f;
+        // operands are read kAhead k-steps before their products: LDS takes longer than a pair of those
+        constexpr int kSteps = DP / 16, kAhead = kSteps < 4 ? kSteps : 4;
+        u32x4 a[kSteps][NB];
 #pragma unroll
-        for (int step = 0; step < DP / 16; ++step)
+        for (int step = 0; step < kAhead; ++step)
 #pragma unroll
-            for (int n = 0; n < NB; ++n) s[n] = mfma32(at.rows_of(k, n, step), q[step], s[n]);
+            for (int n = 0; n < NB; ++n) a[step][n] = at.rows_of(k, n, step);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int step = 0; step < kSteps; ++step) {
+#pragma unroll
+            for (int n = 0; n < NB; ++n) s[n] = mfma32(a[step][n], q[step], s[n]);
+            if (step + kAhead < kSteps) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n) a[step + kAhead][n] = at.rows_of(k, n, step + kAhead);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        constexpr int kParts = 2 * NB * (DP / 32), kFirst = kParts < 8 ? kParts : 8;
+        u32x4 c[kParts];
+#pragma unroll
+        for (int i = 0; i < kFirst; ++i) c[i] = at.columns_of(v, i / (DP / 32), i % (DP / 32));
+        __builtin_amdgcn_sched_barrier(0);
         if (masked) {
 #pragma unroll
             for (int n = 0; n < NB; ++n)
@@ -85,11 +104,13 @@ struct Queries {
                 sum[i % 4] += s[n][i];
             }
         l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+        u32x4 p;
 #pragma unroll
-        for (int u = 0; u < 2 * NB; ++u) {
-            const u32x4 p = as_operand(s[u / 2], u % 2);
-#pragma unroll
-            for (int b = 0; b < DP / 32; ++b) o[b] = mfma32(at.columns_of(v, u, b), p, o[b]);
+        for (int i = 0; i < kParts; ++i) {
+            const int u = i / (DP / 32), b = i % (DP / 32);
+            if (b == 0) p = as_operand(s[u / 2], u % 2);
+            o[b] = mfma32(c[i], p, o[b]);
+            if (i + kFirst < kParts) c[i + kFirst] = at.columns_of(v, (i + kFirst) / (DP / 32), (i + kFirst) % (DP / 32));
         }
     }
 };
@@ -99,12 +120,12 @@ __device__ __forceinline__ const uint16_t* at(const AttnHeads& t, int64_t token,
 }
 
 // The end of a row: its result and lse, or its part of them.  row: of the tile.
-template <int DP>
+template <int DP, int ROWS>
 __device__ __forceinline__ void finish(const AttnParams& p, const AttnTile& t, int kv, int row, Queries<DP>& mine, float l, int lane) {
     const int r = t.first + row;
     const bool live = r < t.q_len * p.group;
     if (t.slot >= 0) {
-        const int64_t at = ((int64_t)t.slot * p.kv_heads + kv) * kAttnRows + row;
+        const int64_t at = (int64_t)t.slot * p.kv_heads + kv * ROWS + row;
         store_column_f32<DP>(mine.o, 1.f, p.part + at * DP, DP, lane, live);
         if (live && lane < 32) *(f32x2*)(p.stat + 2 * at) = (f32x2){mine.m, l};
         return;
@@ -120,16 +141,16 @@ __device__ __forceinline__ void finish(const AttnParams& p, const AttnTile& t, i
         p.lse[(int64_t)(t.q_start + token) * p.heads + head] = l == 0.f ? -__builtin_inff() : (mine.m + __builtin_log2f(l)) * kLn2;
 }
 
-// 128 rows to a workgroup, 32 to each wave; 64 keys at a time, shared, in two buffers.
-template <int DP>
-__global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p) {
+// 32 rows to each wave; 64 keys at a time, shared, in two buffers.
+template <int DP, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void attention_kernel(AttnParams p) {
     __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * 2 * DP];
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const TileLoads<DP, 64, 4> k(at(p.k, t.k_start, kv), p.k.token, t.k_len - 1, p.D, wave, lane);
-    const TileLoads<DP, 64, 4> v(at(p.v, t.k_start, kv), p.v.token, t.k_len - 1, p.D, wave, lane);
+    const TileLoads<DP, 64, WAVES> k(at(p.k, t.k_start, kv), p.k.token, t.k_len - 1, p.D, wave, lane);
+    const TileLoads<DP, 64, WAVES> v(at(p.v, t.k_start, kv), p.v.token, t.k_len - 1, p.D, wave, lane);
     auto load = [&](int key, int buffer) {
         k.load(key, lds[buffer][0], p.D, lane);
         v.load(key, lds[buffer][1], p.D, lane);
@@ -158,7 +179,7 @@ __global__ __launch_bounds__(256, 2) void attention_kernel(AttnParams p) {
             key += 64;
         }
     }
-    finish<DP>(p, t, kv, row, mine, mine.l + other_half(mine.l), lane);
+    finish<DP, 32 * WAVES>(p, t, kv, row, mine, mine.l + other_half(mine.l), lane);
 }
 
 // Up to 32 rows: the workgroup's four waves have the same ones and 32 keys each at a time, in buffers of their own, so they wait
@@ -167,7 +188,7 @@ template <int DP>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     extern __shared__ __attribute__((aligned(1024))) char few_lds[];
     constexpr int kTile = 32 * 2 * DP;
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -228,7 +249,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
             for (int w = 0; w < 4; ++w) sum += factor[w] * sums[(w * (DP / 2) + 16 * b + i) * 64 + lane];
             mine.o[b][i] = sum;
         }
-    finish<DP>(p, t, kv, row, mine, l, lane);
+    finish<DP, kAttnFewRows>(p, t, kv, row, mine, l, lane);
 }
 
 // Rows whose keys several workgroups shared: a wave to a row, in the order of the slots.
@@ -236,12 +257,12 @@ template <int DP>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
     const int lane = threadIdx.x & 63;
     const uint32_t id = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int row = id % kAttnRows, kv = id / kAttnRows % (uint32_t)p.kv_heads;
-    const AttnJoin j = p.joins[id / kAttnRows / (uint32_t)p.kv_heads];
+    const int row = id % kAttnWideRows, kv = id / kAttnWideRows % (uint32_t)p.kv_heads;
+    const AttnJoin j = p.joins[id / kAttnWideRows / (uint32_t)p.kv_heads];
     const int r = j.first + row;
-    if (r >= j.q_len * p.group) return;
+    if (row >= j.rows || r >= j.q_len * p.group) return;
     float m = kLowest, l = 0.f, o[DP / 64] = {};
-    auto place = [&](int i) { return ((int64_t)(j.slot + i) * p.kv_heads + kv) * kAttnRows + row; };
+    auto place = [&](int i) { return (int64_t)(j.slot + i * j.rows) * p.kv_heads + kv * j.rows + row; };
     for (int i = 0; i < j.count; ++i) m = fmaxf(m, p.stat[2 * place(i)]);
     for (int i = 0; i < j.count; ++i) {
         const float factor = exp2_fast(p.stat[2 * place(i)] - m);
@@ -265,13 +286,16 @@ __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
 }
 
 template <int DP>
-hipError_t launch(const AttnParams& p, bool few, hipStream_t stream) {
-    const unsigned grid = (unsigned)places(p.count, p.kv_heads);
-    if (!few) {
-        attention_kernel<DP><<<grid, 256, 0, stream>>>(p);
+hipError_t launch(const AttnParams& p, AttnWay way, hipStream_t stream) {
+    const unsigned grid = (unsigned)places(p.lead, p.count, p.kv_heads);
+    if (way != kAttnShared) {
+        if (way == kAttnWide)
+            attention_kernel<DP, 8><<<grid, 512, 0, stream>>>(p);
+        else
+            attention_kernel<DP, 4><<<grid, 256, 0, stream>>>(p);
         return hipGetLastError();
     }
-    constexpr int kBytes = 4 * 4 * 32 * 2 * DP + 2048;   // the waves' buffers; their sums take as much, and their states the rest
+    constexpr int kBytes = 4 * 4 * 32 * 2 * DP;   // the waves' buffers; their sums and states take less
     static std::atomic<uint64_t> raised{0};
     const hipError_t e = raise_lds_limit((const void*)attention_few_kernel<DP>, kBytes, raised);
     if (e != hipSuccess) return e;
@@ -281,12 +305,12 @@ hipError_t launch(const AttnParams& p, bool few, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_attention(const AttnParams& p, bool few, hipStream_t stream) {
-    return p.D > 64 ? launch<128>(p, few, stream) : launch<64>(p, few, stream);
+hipError_t launch_attention(const AttnParams& p, AttnWay way, hipStream_t stream) {
+    return p.D > 64 ? launch<128>(p, way, stream) : launch<64>(p, way, stream);
 }
 
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream) {
-    const unsigned grid = (unsigned)((int64_t)p.count * p.kv_heads * (kAttnRows / 4));
+    const unsigned grid = (unsigned)((int64_t)p.count * p.kv_heads * (kAttnWideRows / 4));
     if (p.D > 64)
         attention_join_kernel<128><<<grid, 256, 0, stream>>>(p);
     else

@@ -30,55 +30,107 @@ struct Work {
     int64_t cost;
 };
 
-// Tiles that would leave the card partly idle are divided along the other side into parts of at least `least` units of `step` keys
-// (or queries) each, so that there are about `most` workgroups in all.  Parts leave their sums in slots, which a join adds up.
-// The longest come first: workgroups start in the list's order, and the last to start are the shortest.
-void divide(std::vector<Work>& work, int64_t kv_heads, int64_t step, int64_t least, int64_t most, int64_t* slots, std::vector<AttnJoin>* joins,
-            std::vector<AttnTile>* out) {
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// What a list's tiles are divided for.
+struct Card {
+    int64_t slots;   // workgroups that are resident
+    int64_t rows;    // of a tile
+    int64_t step;    // keys (or queries) in a unit of cost
+    int64_t least;   // units that a part has at least
+};
+
+// Divides tiles along the other side where whole ones would leave the card partly idle; parts leave their sums in rows of their own,
+// which a join adds up.
+//   Slots that have less than two of the longest tiles each: parts of about half of what a slot has on average.
+//   A few rounds of tiles of one size: those of the last, partial round are divided so that all slots share them (or those of the last
+//   two).  With 1728 equal tiles on 512 slots the last round is 0.4 long instead of 1, of 3.4.
+// The longest tiles come first, then the parts: workgroups start in the list's order.
+void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t* slot_rows, std::vector<AttnJoin>* joins, std::vector<AttnTile>* out,
+            int64_t* lead) {
+    std::stable_sort(work.begin(), work.end(), [](const Work& a, const Work& b) { return a.cost > b.cost; });
+    const int64_t n = (int64_t)work.size(), all = n * kv_heads;
     int64_t total = 0;
     for (const Work& w : work) total += w.cost;
-    const int64_t part = (int64_t)work.size() * kv_heads >= most ? INT64_MAX : std::max(least, (total * kv_heads + most - 1) / most);
-    std::vector<Work> all;
-    for (const Work& w : work) {
-        const int64_t n = std::max<int64_t>(1, (w.cost + part / 2) / part);
-        if (n == 1) {
-            all.push_back(w);
+    int64_t whole = n, part = 1;   // tiles that stay whole, and the size of the others' parts
+    if (n && total * kv_heads < 2 * work[0].cost * card.slots) {
+        part = std::max(card.least, ceil_div(total * kv_heads, 2 * card.slots));
+        whole = 0;
+    } else if (n && all < 12 * card.slots && 2 * work[n - 1].cost > work[0].cost) {
+        const int64_t rounds = all / card.slots, rest = all % card.slots;
+        const double cost = (double)total / n;
+        double best = rest ? 1.0 - 0.06 * (rounds + 1) : 0.0;   // of a round; a gain below 6% is none
+        for (int64_t more = 0; more <= 1 && more < rounds; ++more)
+            for (int64_t k = 2; k <= 6 && rest && cost >= k * card.least; ++k) {
+                const int64_t parts = (more * card.slots + rest) * k;
+                const double time = (double)ceil_div(parts, card.slots) * (1.0 / k + 1.5 / cost) - more;   // a part's begin and end: 1.5 units
+                if (time < best) {
+                    best = time;
+                    whole = n - ceil_div(more * card.slots + rest, kv_heads);
+                    part = ceil_div(work[0].cost, k);
+                }
+            }
+    }
+    *lead = whole;
+    std::vector<Work> parts;
+    for (int64_t i = 0; i < n; ++i) {
+        const Work& w = work[i];
+        const AttnTile& t = w.tile;
+        const int64_t k = i < whole ? 1 : std::max<int64_t>(1, (w.cost + part / 2) / part);
+        if (k == 1) {
+            if (i < whole)
+                out->push_back(t);
+            else
+                parts.push_back(w);
             continue;
         }
-        const AttnTile& t = w.tile;
-        joins->push_back({t.q_start, t.q_len, t.k_start, t.k_len, t.first, (int32_t)*slots, (int32_t)n, 0});
-        for (int64_t i = 0; i < n; ++i) {
+        joins->push_back({t.q_start, t.q_len, t.k_start, t.k_len, t.first, (int32_t)*slot_rows, (int32_t)k, (int32_t)card.rows});
+        for (int64_t j = 0; j < k; ++j) {
             Work piece = w;
-            const int64_t from = w.cost * i / n, to = w.cost * (i + 1) / n;
+            const int64_t from = w.cost * j / k, to = w.cost * (j + 1) / k;
             piece.cost = to - from;
-            piece.tile.begin = (int32_t)(t.begin + from * step);
-            piece.tile.end = (int32_t)std::min<int64_t>(t.end, t.begin + to * step);
-            piece.tile.slot = (int32_t)(*slots)++;
-            all.push_back(piece);
+            piece.tile.begin = (int32_t)(t.begin + from * card.step);
+            piece.tile.end = (int32_t)std::min<int64_t>(t.end, t.begin + to * card.step);
+            piece.tile.slot = (int32_t)*slot_rows;
+            *slot_rows += card.rows;
+            parts.push_back(piece);
         }
     }
-    std::stable_sort(all.begin(), all.end(), [](const Work& a, const Work& b) { return a.cost > b.cost; });
-    for (const Work& w : all) out->push_back(w.tile);
+    std::stable_sort(parts.begin(), parts.end(), [](const Work& a, const Work& b) { return a.cost > b.cost; });
+    for (const Work& w : parts) out->push_back(w.tile);
 }
-
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // Lists of checked sequences.
 void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
     const int64_t group = p->heads / p->kv_heads, queries = std::max<int64_t>(1, 64 / group);   // of 64 rows
-    std::vector<Work> whole, few, every, keys;
+    std::vector<Work> whole, wide, few, every, keys;
+    // Wide tiles load keys and values half as often, but a compute unit has one workgroup of them, whose begin and end nothing
+    // else covers: 32760 tokens in 40 heads of 128 19.0 ms instead of 20.0, 4608 tokens 512 us instead of 502, over 512 keys
+    // 442 us instead of 418.
+    int64_t wide_tiles = 0, wide_cost = 0;
     for (const Sequence& s : sequences) {
-        const int64_t rows = s.q_len * group, most = rows <= kAttnFewRows ? kAttnFewRows : kAttnRows;
-        for (int64_t first = 0; first < rows; first += most) {
-            const int64_t last = (std::min(first + most, rows) - 1) / group;   // the tile's last query
-            const int64_t end = p->causal ? std::min(s.k_len, std::max<int64_t>(0, last + 1 + s.k_len - s.q_len)) : s.k_len;
-            const AttnTile t{(int32_t)s.q_start, (int32_t)s.q_len, (int32_t)s.k_start, (int32_t)s.k_len, (int32_t)first, 0, (int32_t)end, -1};
-            if (most == kAttnFewRows)
-                few.push_back({t, ceil_div(end, 128)});
-            else
-                whole.push_back({t, ceil_div(end, 64)});
-            every.push_back({t, ceil_div(end, 64)});   // few rows are one tile here as well
-        }
+        const int64_t tiles = s.q_len * group > kAttnFewRows ? ceil_div(s.q_len * group, kAttnWideRows) : 0;
+        wide_tiles += tiles;
+        wide_cost += tiles * (p->causal ? (s.k_len + 1) / 2 : s.k_len);
+    }
+    const bool widely = wide_tiles * p->kv_heads >= 2 * 256 && wide_cost >= 8192 * wide_tiles;
+    for (const Sequence& s : sequences) {
+        const int64_t rows = s.q_len * group;
+        auto tiles = [&](std::vector<Work>& to, int64_t most, int64_t unit) {
+            for (int64_t first = 0; first < rows; first += most) {
+                const int64_t last = (std::min(first + most, rows) - 1) / group;   // the tile's last query
+                const int64_t end = p->causal ? std::min(s.k_len, std::max<int64_t>(0, last + 1 + s.k_len - s.q_len)) : s.k_len;
+                to.push_back({{(int32_t)s.q_start, (int32_t)s.q_len, (int32_t)s.k_start, (int32_t)s.k_len, (int32_t)first, 0, (int32_t)end, -1},
+                              ceil_div(end, unit)});
+            }
+        };
+        if (rows <= kAttnFewRows)
+            tiles(few, kAttnFewRows, 128);
+        else if (widely)
+            tiles(wide, kAttnWideRows, 64);
+        else
+            tiles(whole, kAttnRows, 64);
+        tiles(every, kAttnRows, 64);
         for (int64_t first = 0; first < s.k_len; first += kAttnRows) {
             // the first query that sees the tile's first key
             const int64_t begin = p->causal ? std::min(s.q_len, std::max<int64_t>(0, first - (s.k_len - s.q_len))) : 0;
@@ -88,11 +140,12 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
     }
     std::vector<AttnTile> list[kAttnLists];
     std::vector<AttnJoin> joins, row_joins, key_joins;
-    // 512 workgroups of whole tiles are resident on 256 compute units, 256 of few rows
-    divide(whole, p->kv_heads, 64, 4, 1024, &p->slots, &joins, &list[kAttnForward]);
-    divide(few, p->kv_heads, 128, 2, 768, &p->slots, &joins, &list[kAttnFew]);
-    divide(every, p->kv_heads, 64, 4, 1024, &p->row_slots, &row_joins, &list[kAttnRowGrads]);
-    divide(keys, p->kv_heads, queries, 4, 1024, &p->key_slots, &key_joins, &list[kAttnKeyGrads]);
+    // resident on 256 compute units: two workgroups of four waves, one of eight, or one whose buffers take the LDS
+    divide(whole, p->kv_heads, {512, kAttnRows, 64, 4}, &p->slots, &joins, &list[kAttnForward], &p->lead[kAttnForward]);
+    divide(wide, p->kv_heads, {256, kAttnWideRows, 64, 4}, &p->slots, &joins, &list[kAttnForwardWide], &p->lead[kAttnForwardWide]);
+    divide(few, p->kv_heads, {256, kAttnFewRows, 128, 2}, &p->slots, &joins, &list[kAttnFew], &p->lead[kAttnFew]);
+    divide(every, p->kv_heads, {512, kAttnRows, 64, 4}, &p->row_slots, &row_joins, &list[kAttnRowGrads], &p->lead[kAttnRowGrads]);
+    divide(keys, p->kv_heads, {512, kAttnRows, queries, 4}, &p->key_slots, &key_joins, &list[kAttnKeyGrads], &p->lead[kAttnKeyGrads]);
 
     std::vector<unsigned char>& blob = p->lists;
     auto append = [&](int which, const void* data, size_t count, size_t size) {
@@ -101,7 +154,7 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
         blob.resize(std::max<size_t>(p->at[which] + count * size, 16));
         if (count) std::memcpy(blob.data() + p->at[which], data, count * size);
     };
-    for (int i : {kAttnForward, kAttnFew, kAttnRowGrads, kAttnKeyGrads}) append(i, list[i].data(), list[i].size(), sizeof(AttnTile));
+    for (int i : {kAttnForward, kAttnForwardWide, kAttnFew, kAttnRowGrads, kAttnKeyGrads}) append(i, list[i].data(), list[i].size(), sizeof(AttnTile));
     append(kAttnJoins, joins.data(), joins.size(), sizeof(AttnJoin));
     append(kAttnRowJoins, row_joins.data(), row_joins.size(), sizeof(AttnJoin));
     append(kAttnKeyJoins, key_joins.data(), key_joins.size(), sizeof(AttnJoin));
@@ -167,9 +220,7 @@ orbit_status check_heads(const char* who, const char* name, const orbit_heads* t
     return ORBIT_OK;
 }
 
-size_t slot_floats(int64_t D) { return (size_t)(attention_part((int)D) + 2 * kAttnRows); }
-
-size_t forward_bytes(orbit_attention p, int64_t D) { return (size_t)p->slots * p->kv_heads * slot_floats(D) * sizeof(float); }
+size_t forward_bytes(orbit_attention p, int64_t D) { return (size_t)p->slots * p->kv_heads * (attention_part((int)D) + 2) * sizeof(float); }
 
 // Of the backward pass: lse and delta of each row, then the parts of dq, whose place those of dk and dv take afterwards.
 size_t stat_floats(orbit_attention p) { return ((size_t)p->heads * p->q_tokens + 63) / 64 * 64; }
@@ -311,11 +362,13 @@ orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_head
     a.lse = lse;
     a.part = (float*)workspace;
     a.stat = a.part + p->slots * p->kv_heads * attention_part((int)D);
-    for (int which : {kAttnForward, kAttnFew}) {
+    const std::pair<int, AttnWay> ways[] = {{kAttnForwardWide, kAttnWide}, {kAttnForward, kAttnWhole}, {kAttnFew, kAttnShared}};
+    for (const auto& [which, way] : ways) {
         a.tiles = (const AttnTile*)(lists + p->at[which]);
         a.count = (int)p->count[which];
+        a.lead = (int)p->lead[which];
         if (!a.count) continue;
-        const hipError_t e = launch_attention(a, which == kAttnFew, (hipStream_t)stream);
+        const hipError_t e = launch_attention(a, way, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, who);
     }
     a.joins = (const AttnJoin*)(lists + p->at[kAttnJoins]);
@@ -387,6 +440,7 @@ orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, cons
     for (const auto& s : steps) {
         if (s.list >= 0) {
             a.count = (int)p->count[s.list];
+            a.lead = (int)p->lead[s.list];
             a.tiles = (const AttnTile*)(lists + p->at[s.list]);
             a.joins = (const AttnJoin*)(lists + p->at[s.list]);
         }

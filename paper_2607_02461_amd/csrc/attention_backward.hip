@@ -74,7 +74,7 @@ __global__ __launch_bounds__(256) void attention_delta_kernel(AttnGradParams p) 
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradParams p) {
     __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * 2 * DP];
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
     }
     const bool live = t.first + row < rows;
     if (t.slot >= 0)
-        store_column_f32<DP>(dq, 1.f, p.part + (((int64_t)t.slot * p.kv_heads + kv) * kAttnRows + row) * DP, DP, lane, live);
+        store_column_f32<DP>(dq, 1.f, p.part + ((int64_t)t.slot * p.kv_heads + kv * kAttnRows + row) * DP, DP, lane, live);
     else
         store_column<DP>(dq, p.out_scale, (uint16_t*)at(p.dq, t.q_start + token, head), p.D, lane, live);
 }
@@ -180,7 +180,7 @@ template <int DP, int NK>
 __global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_kernel(AttnGradParams p) {
     constexpr int kTile = 64 * 2 * DP, kBuffer = 2 * kTile + 1024, kWaves = 4 / NK;
     extern __shared__ __attribute__((aligned(1024))) char key_lds[];
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_
     for (int m = 0; m < NK; ++m) {
         const bool live = key[m] < t.k_len;
         if (t.slot >= 0) {
-            const int64_t to = (((int64_t)t.slot * p.kv_heads + kv) * kAttnRows + 32 * (NK * wave + m) + (lane & 31)) * DP;
+            const int64_t to = ((int64_t)t.slot * p.kv_heads + kv * kAttnRows + 32 * (NK * wave + m) + (lane & 31)) * DP;
             store_column_f32<DP>(dk[m], 1.f, p.part + to, DP, lane, live);
             store_column_f32<DP>(dv[m], 1.f, p.part2 + to, DP, lane, live);
         } else {
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams
         const float* const part = which ? p.part2 : p.part;
         float sum[8] = {};
         for (int i = 0; i < j.count; ++i) {
-            const float* const from = part + (((int64_t)(j.slot + i) * p.kv_heads + kv) * kAttnRows + row) * DP + d;
+            const float* const from = part + ((int64_t)(j.slot + i * kAttnRows) * p.kv_heads + kv * kAttnRows + row) * DP + d;
             const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
 #pragma unroll
             for (int c = 0; c < 4; ++c) sum[c] += lo[c], sum[4 + c] += hi[c];
@@ -333,7 +333,7 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams
 
 template <int DP>
 hipError_t launch(const AttnGradParams& p, AttnGradStep step, hipStream_t stream) {
-    const unsigned grid = step == kAttnDelta ? 0 : (unsigned)places(p.count, p.kv_heads);
+    const unsigned grid = step == kAttnDelta ? 0 : (unsigned)places(p.lead, p.count, p.kv_heads);
     switch (step) {
         case kAttnDelta:
             attention_delta_kernel<DP><<<(unsigned)std::min<int64_t>((p.q_tokens * p.heads * (DP / 8) + 255) / 256, 1 << 20), 256, 0, stream>>>(p);

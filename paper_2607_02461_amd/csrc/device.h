@@ -309,7 +309,7 @@ struct NormParams {
     int64_t w_batch, b_batch;
     int w_f32, modulate;   // modulate: the gain is 1 + w
     int N;
-    int joined;            // the batches' rows are one group (they share weights and their gradients)
+    int joined;            // rows of one group are those of several batches, whose strides differ
     int64_t rows, L;       // rows of a group; rows of a batch
     float eps;
     int stream;            // rows are loaded and stored non-temporally
@@ -320,12 +320,13 @@ struct NormParams {
 
 hipError_t launch_layer_norm(const NormParams& p, int groups, bool x_f32, bool y_f32, int cus, hipStream_t stream);
 // Workgroups to a group of the backward pass, each with a row of sums.
-int layer_norm_parts(int64_t rows, int groups, int cus);
+int layer_norm_parts(int64_t rows, int groups, int64_t N, int cus);
 // rows = 0 gives zeros in dw and db.
 hipError_t launch_layer_norm_backward(const NormParams& p, int groups, bool x_f32, bool g_f32, int cus, hipStream_t stream);
 
 // Attention of packed sequences, grouped heads.
 constexpr int kAttnRows = 128;     // rows of a workgroup's tile: queries x heads of a group, or keys
+constexpr int kAttnWideRows = 256; // of a tile where there are enough of them: half the loads of keys and values
 constexpr int kAttnFewRows = 32;   // of a sequence, up to which a workgroup's waves share the rows and divide the keys
 constexpr int kAttnMaxDim = 128;
 
@@ -334,13 +335,13 @@ struct AttnTile {             // what one workgroup computes for each key head
     int32_t k_start, k_len;
     int32_t first;            // of the tile's rows (token * group + head of the group), or of its keys
     int32_t begin, end;       // of the keys that it goes over, or of the queries
-    int32_t slot;             // where its partial sums lie, or -1: it has them all
+    int32_t slot;             // first row of its partial sums, or -1: it has them all
 };
 
 struct AttnJoin {             // partial sums of one tile
     int32_t q_start, q_len, k_start, k_len, first;
-    int32_t slot, count;
-    int32_t pad;
+    int32_t slot, count;      // first row of the first part, and the parts
+    int32_t rows;             // of the tile: from one part to the next
 };
 
 struct AttnHeads {            // [token][head][D] bf16 values (or fp32, results), strides in elements
@@ -351,26 +352,27 @@ struct AttnHeads {            // [token][head][D] bf16 values (or fp32, results)
 struct AttnParams {
     const AttnTile* tiles;
     const AttnJoin* joins;
-    int count;                // of the tiles, or of the joins
+    int count, lead;          // of the tiles, or of the joins; of the tiles that go first
     int heads, kv_heads, group, D;
     int causal;
     float scale;              // of the scores, times log2(e)
     AttnHeads q, k, v, o;
     int out_f32;
     float* lse;               // [token][heads] or null
-    float* part;              // [slot][key head][row][padded D] of tiles that share their rows' keys
-    float* stat;              // [slot][key head][row][2]: largest scaled score, sum
+    float* part;              // of tiles that share their rows' keys: tile by tile [key head][row][padded D]
+    float* stat;              // the same rows' largest scaled score and sum
 };
 
-// Floats of a slot's sums.
-constexpr int64_t attention_part(int D) { return (int64_t)kAttnRows * (D > 64 ? 128 : 64); }
-hipError_t launch_attention(const AttnParams& p, bool few, hipStream_t stream);
+// Floats of a row's sums.
+constexpr int attention_part(int D) { return D > 64 ? 128 : 64; }
+enum AttnWay { kAttnWhole, kAttnWide, kAttnShared };   // tiles of kAttnRows, of kAttnWideRows, of kAttnFewRows
+hipError_t launch_attention(const AttnParams& p, AttnWay way, hipStream_t stream);
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream);
 
 struct AttnGradParams {
     const AttnTile* tiles;
     const AttnJoin* joins;
-    int count;                // of the tiles, or of the joins
+    int count, lead;          // of the tiles, or of the joins; of the tiles that go first
     int heads, kv_heads, group, D;
     int causal, o_f32;
     int64_t q_tokens;
@@ -378,7 +380,7 @@ struct AttnGradParams {
     AttnHeads q, k, v, o, g, dq, dk, dv;   // g: the output's gradient
     const float* lse;         // [token][heads]
     float *lse2, *delta;      // [key head][token * group + head of the group]
-    float *part, *part2;      // [slot][key head][row or key][padded D]: of dq; of dk and of dv
+    float *part, *part2;      // as AttnParams: of dq; of dk and of dv
 };
 
 enum AttnGradStep { kAttnDelta, kAttnRowGrad, kAttnKeyGrad, kAttnRowJoin, kAttnKeyJoin };

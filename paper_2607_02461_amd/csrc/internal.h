@@ -88,15 +88,15 @@ struct orbit_lora_s {
 
 // Sequences of queries and keys, as the kernels' lists (device.h): tiles of rows, those of few rows, and the joins of
 // tiles whose keys several workgroups share; and for the backward pass tiles of rows and tiles of keys.
-enum AttnList { kAttnForward, kAttnFew, kAttnJoins, kAttnRowGrads, kAttnKeyGrads, kAttnRowJoins, kAttnKeyJoins, kAttnLists };
+enum AttnList { kAttnForward, kAttnForwardWide, kAttnFew, kAttnJoins, kAttnRowGrads, kAttnKeyGrads, kAttnRowJoins, kAttnKeyJoins, kAttnLists };
 struct orbit_attention_s {
     int32_t heads = 0, kv_heads = 0, causal = 0;
     bool shared_keys = false;                  // two sequences have a key in common
     int64_t q_tokens = 0, k_tokens = 0;        // behind the last query, and the last key
     std::vector<unsigned char> lists;
     size_t at[kAttnLists] = {};                // byte offsets
-    int64_t count[kAttnLists] = {};
-    int64_t slots = 0, row_slots = 0, key_slots = 0;   // of partial sums: forward, and of the two lists of the backward pass
+    int64_t count[kAttnLists] = {}, lead[kAttnLists] = {};   // entries, and tiles that go before the others
+    int64_t slots = 0, row_slots = 0, key_slots = 0;         // rows of partial sums: forward, and of the backward pass's two lists
     std::mutex mu;
     unsigned char* dev_lists[orbit::kMaxDevices] = {};
 };

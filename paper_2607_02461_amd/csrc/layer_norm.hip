@@ -33,29 +33,15 @@ typedef u32x4 u32x4_any __attribute__((aligned(2)));
 typedef u32x2 u32x2_any __attribute__((aligned(2)));
 typedef f32x4 f32x4_any __attribute__((aligned(4)));
 
-// V values at any element: 8 of bf16 or 4 of either type are one access
-template <typename T, int V>
+// kPiece values in a row, at any element.  (Eight values of bf16 in 16 bytes: the backward pass of 32760 x 5120 took 345 us
+// instead of 201, that of 2 x 4429 x 3072 55 instead of 46; forward 133 and 131.)
+constexpr int kPiece = 4;
+
+template <typename T>
 struct Piece;
 
 template <>
-struct Piece<bf16_t, 8> {
-    u32x4 r;
-    __device__ __forceinline__ void load(const bf16_t* p, bool nt) { r = nt ? __builtin_nontemporal_load((const u32x4_any*)p) : *(const u32x4_any*)p; }
-    __device__ __forceinline__ void get(float* v) const {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) v[2 * i] = bf16_low(r[i]), v[2 * i + 1] = bf16_high(r[i]);
-    }
-    static __device__ __forceinline__ void store(bf16_t* p, const float* v, bool nt) {
-        const u32x4 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
-        if (nt)
-            __builtin_nontemporal_store(w, (u32x4_any*)p);
-        else
-            *(u32x4_any*)p = w;
-    }
-};
-
-template <>
-struct Piece<bf16_t, 4> {
+struct Piece<bf16_t> {
     u32x2 r;
     __device__ __forceinline__ void load(const bf16_t* p, bool nt) { r = nt ? __builtin_nontemporal_load((const u32x2_any*)p) : *(const u32x2_any*)p; }
     __device__ __forceinline__ void get(float* v) const { v[0] = bf16_low(r.x), v[1] = bf16_high(r.x), v[2] = bf16_low(r.y), v[3] = bf16_high(r.y); }
@@ -69,7 +55,7 @@ struct Piece<bf16_t, 4> {
 };
 
 template <>
-struct Piece<float, 4> {
+struct Piece<float> {
     f32x4 r;
     __device__ __forceinline__ void load(const float* p, bool nt) { r = nt ? __builtin_nontemporal_load((const f32x4_any*)p) : *(const f32x4_any*)p; }
     __device__ __forceinline__ void get(float* v) const { v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w; }
@@ -82,79 +68,109 @@ struct Piece<float, 4> {
     }
 };
 
-// Values to an access: as many as both types have in 16 bytes
-template <typename A, typename B>
-constexpr int values_of() {
-    return sizeof(A) + sizeof(B) == 4 ? 8 : 4;
-}
-
 __device__ __forceinline__ float value(const bf16_t* p) { return __uint_as_float((uint32_t)p->bits << 16); }
 __device__ __forceinline__ float value(const float* p) { return *p; }
 __device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = (uint16_t)pack_bf16(v, 0.f); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 
-// A thread's part of a row: C pieces of V values, T pieces apart.  The piece that the row's end cuts is read and written value
-// by value (`cut`: the values that it has), those behind it not at all.
-template <int V, int C>
+// How rows are accessed: as they come, non-temporally, or with a piece that the row's end cuts.
+enum Access { kPlain, kStream, kCut };
+
+// A thread's part of a row: C pieces of kPiece values, blockDim.x pieces apart.  The piece that the row's end cuts begins further left, so
+// that it is a whole one: its first `skip` values are its neighbour's and stay out of sums.  (Value by value, one after the other
+// and with a branch each, such a piece held up the whole wave: a backward pass of 32760 x 5120 370 us for 230, whose last
+// pieces were idle and not even cut.)  A row of less than a piece is one thread's, value by value.
+template <int C, Access A>
 struct Columns {
     int at[C];     // first column
-    int have[C];   // values: V, fewer, or 0
+    int skip[C];
+    bool have[C];
+    int small;     // values of a row of less than a piece, or 0
     __device__ __forceinline__ Columns(int N) {
+        small = A == kCut && N < kPiece ? N : 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            at[c] = (c * (int)blockDim.x + (int)threadIdx.x) * V;
-            have[c] = min(max(N - at[c], 0), V);
+            at[c] = (c * (int)blockDim.x + (int)threadIdx.x) * kPiece;
+            have[c] = at[c] < N;
+            skip[c] = 0;
+            if (A == kCut && have[c] && at[c] + kPiece > N && !small) skip[c] = at[c] + kPiece - N, at[c] = N - kPiece;
         }
     }
+    // whether value i of piece c is this thread's own
+    __device__ __forceinline__ bool own(int c, int i) const { return A != kCut ? have[c] : small ? have[c] && i < small : have[c] && i >= skip[c]; }
 };
 
 // Pieces on their way from memory, and their values; values that the row does not have are zeros.
-template <typename T, int V, int C, bool NT>
+template <typename T, int C, Access A>
 struct Part {
-    Piece<T, V> piece[C];
-    __device__ __forceinline__ void load(const T* row, const Columns<V, C>& k) {
+    Piece<T> piece[C];
+    __device__ __forceinline__ void load(const T* row, const Columns<C, A>& k) {
+        if (k.small) return;
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (k.have[c] == V) piece[c].load(row + k.at[c], NT);
+            if (k.have[c]) piece[c].load(row + k.at[c], A == kStream);
     }
-    __device__ __forceinline__ void get(const T* row, const Columns<V, C>& k, float (&v)[C][V]) const {
+    __device__ __forceinline__ void get(const T* row, const Columns<C, A>& k, float (&v)[C][kPiece]) const {
+        if (k.small) {
+#pragma unroll
+            for (int c = 0; c < C; ++c)
+#pragma unroll
+                for (int i = 0; i < kPiece; ++i) v[c][i] = k.own(c, i) ? value(row + i) : 0.f;
+            return;
+        }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (k.have[c] == V) {
+            if (k.have[c]) {
                 piece[c].get(v[c]);
             } else {
 #pragma unroll
-                for (int i = 0; i < V; ++i) v[c][i] = i < k.have[c] ? value(row + k.at[c] + i) : 0.f;
+                for (int i = 0; i < kPiece; ++i) v[c][i] = 0.f;
             }
         }
     }
-    static __device__ __forceinline__ void store(T* row, const Columns<V, C>& k, const float (&v)[C][V]) {
+    static __device__ __forceinline__ void store(T* row, const Columns<C, A>& k, const float (&v)[C][kPiece]) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (k.have[c] == V) {
-                Piece<T, V>::store(row + k.at[c], v[c], NT);
-            } else {
+            if (k.small) {
 #pragma unroll
-                for (int i = 0; i < V; ++i)
-                    if (i < k.have[c]) put(row + k.at[c] + i, v[c][i]);
+                for (int i = 0; i < kPiece; ++i)
+                    if (k.own(c, i)) put(row + i, v[c][i]);
+            } else if (k.have[c]) {
+                Piece<T>::store(row + k.at[c], v[c], A == kStream);
             }
         }
     }
 };
 
-// A batch's weights of the thread's columns, `none` where there are none
-template <int V, int C>
-__device__ __forceinline__ void load_weights(const void* w, bool f32, int64_t first, float none, float add, const Columns<V, C>& k, float (&v)[C][V]) {
+// A batch's weights of the thread's columns, `none` where there are none, and `add` to them where there are
+template <typename T, int C, Access A>
+__device__ __forceinline__ void load_weights(const T* w, float add, const Columns<C, A>& k, float (&v)[C][kPiece]) {
+    Piece<T> piece[C];
 #pragma unroll
     for (int c = 0; c < C; ++c)
+        if (k.have[c] && !k.small) piece[c].load(w + k.at[c], false);
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            v[c][i] = none;
-            if (w && i < k.have[c]) {
-                const int64_t at = first + k.at[c] + i;
-                v[c][i] = (f32 ? ((const float*)w)[at] : value((const bf16_t*)w + at)) + add;
-            }
-        }
+    for (int c = 0; c < C; ++c) {
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[c][i] = k.small && k.own(c, i) ? value(w + i) : 0.f;
+        if (k.have[c] && !k.small) piece[c].get(v[c]);
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) v[c][i] += add;
+    }
+}
+
+template <int C, Access A>
+__device__ __forceinline__ void load_weights(const void* w, bool f32, int64_t first, float none, float add, const Columns<C, A>& k, float (&v)[C][kPiece]) {
+    if (!w) {
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < kPiece; ++i) v[c][i] = none;
+    } else if (f32) {
+        load_weights<float, C, A>((const float*)w + first, add, k, v);
+    } else {
+        load_weights<bf16_t, C, A>((const bf16_t*)w + first, add, k, v);
+    }
 }
 
 template <int CTRL>
@@ -175,30 +191,30 @@ __device__ __forceinline__ float wave_sum(float v) {
 }
 
 // Values of the row that wave w holds
-template <int V, int C>
+template <int C>
 __device__ __forceinline__ int wave_values(int w, int N) {
     int n = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) n += min(max(N - (c * (int)blockDim.x + 64 * w) * V, 0), 64 * V);
+    for (int c = 0; c < C; ++c) n += min(max(N - (c * (int)blockDim.x + 64 * w) * kPiece, 0), 64 * kPiece);
     return n;
 }
 
-// A wave's mean, the deviations from it in v's place (zeros for what the row does not have) and their sum of squares
-template <int V, int C>
-__device__ __forceinline__ void wave_statistics(float (&v)[C][V], const Columns<V, C>& k, float n, float* mean, float* squares) {
+// A wave's mean, the deviations from it in v's place and their sum of squares
+template <int C, Access A>
+__device__ __forceinline__ void wave_statistics(float (&v)[C][kPiece], const Columns<C, A>& k, float n, float* mean, float* squares) {
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < V; ++i) sum += v[c][i];
+        for (int i = 0; i < kPiece; ++i) sum += A != kCut || k.own(c, i) ? v[c][i] : 0.f;
     *mean = n ? wave_sum(sum) / n : 0.f;   // a quotient: a row of equal values has that value for a mean
     float sq = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            v[c][i] = i < k.have[c] ? v[c][i] - *mean : 0.f;
-            sq += v[c][i] * v[c][i];
+        for (int i = 0; i < kPiece; ++i) {
+            v[c][i] -= *mean;
+            sq += k.own(c, i) ? v[c][i] * v[c][i] : 0.f;
         }
     *squares = wave_sum(sq);
 }
@@ -232,30 +248,29 @@ __device__ __forceinline__ T* row_of(const NormRows& t, int64_t b, int64_t l) {
 }
 
 // Workgroup p of group g: rows p, p + parts, ... of the group, which is a batch, or all batches' rows where they share their weights
-template <typename TX, typename TY, int C, bool NT>
-__global__ __launch_bounds__((C * values_of<TX, TY>() > 8 ? 512 : 1024)) void layer_norm_kernel(NormParams p) {
-    constexpr int V = values_of<TX, TY>();
+template <typename TX, typename TY, int C, Access A>
+__global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormParams p) {
     __shared__ float part[2][kMostWaves][2];
     __shared__ float count[kMostWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const Columns<V, C> k(p.N);
-    const int n = wave_values<V, C>(wave, p.N);
+    const Columns<C, A> k(p.N);
+    const int n = wave_values<C>(wave, p.N);
     const float inv_N = 1.f / p.N;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
     const int64_t g = blockIdx.x / (uint32_t)p.parts;
     int64_t row = blockIdx.x % (uint32_t)p.parts, b = g, l = row;
     auto locate = [&]() {
-        if (p.joined) b = row / p.L, l = row - b * p.L;
+        if (p.joined) b = row / p.L, l = row - b * p.L;   // only of batches that do not follow each other row by row
         else l = row;
     };
     locate();
-    Part<TX, V, C, NT> next;
+    Part<TX, C, A> next;
     next.load(row_of<const TX>(p.x, b, l), k);
-    float gain[C][V], offset[C][V];
-    load_weights<V, C>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
-    load_weights<V, C>(p.b, p.w_f32, g * p.b_batch, 0.f, 0.f, k, offset);
+    float gain[C][kPiece], offset[C][kPiece];
+    load_weights<C, A>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
+    load_weights<C, A>(p.b, p.w_f32, g * p.b_batch, 0.f, 0.f, k, offset);
     for (int turn = 0; row < p.rows; turn ^= 1) {
-        float v[C][V];
+        float v[C][kPiece];
         next.get(row_of<const TX>(p.x, b, l), k, v);
         TY* const y = row_of<TY>(p.y, b, l);
         row += p.parts;
@@ -264,7 +279,7 @@ __global__ __launch_bounds__((C * values_of<TX, TY>() > 8 ? 512 : 1024)) void la
             next.load(row_of<const TX>(p.x, b, l), k);
         }
         float mean, squares;
-        wave_statistics<V, C>(v, k, n, &mean, &squares);
+        wave_statistics<C, A>(v, k, n, &mean, &squares);
         if ((threadIdx.x & 63) == 0) part[turn][wave][0] = mean, part[turn][wave][1] = squares;
         __syncthreads();
         const Joined j = join<2>(part[turn], count, waves, wave, p.N);
@@ -272,42 +287,41 @@ __global__ __launch_bounds__((C * values_of<TX, TY>() > 8 ? 512 : 1024)) void la
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[c][i] = (v[c][i] + j.shift) * r * gain[c][i] + offset[c][i];
-        Part<TY, V, C, NT>::store(y, k, v);
+            for (int i = 0; i < kPiece; ++i) v[c][i] = (v[c][i] + j.shift) * r * gain[c][i] + offset[c][i];
+        Part<TY, C, A>::store(y, k, v);
     }
 }
 
-template <typename TX, typename TG, int C, bool NT>
-__global__ __launch_bounds__((C * values_of<TX, TG>() > 8 ? 512 : 1024)) void layer_norm_backward_kernel(NormParams p) {
-    constexpr int V = values_of<TX, TG>();
+template <typename TX, typename TG, int C, Access A>
+__global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel(NormParams p) {
     __shared__ float part[2][kMostWaves][4];
     __shared__ float count[kMostWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const Columns<V, C> k(p.N);
-    const int n = wave_values<V, C>(wave, p.N);
+    const Columns<C, A> k(p.N);
+    const int n = wave_values<C>(wave, p.N);
     const float inv_N = 1.f / p.N;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
     const int64_t g = blockIdx.x / (uint32_t)p.parts;
     int64_t row = blockIdx.x % (uint32_t)p.parts, b = g, l = row;
     auto locate = [&]() {
-        if (p.joined) b = row / p.L, l = row - b * p.L;
+        if (p.joined) b = row / p.L, l = row - b * p.L;   // only of batches that do not follow each other row by row
         else l = row;
     };
-    Part<TX, V, C, NT> next_x;
-    Part<TG, V, C, NT> next_g;
+    Part<TX, C, A> next_x;
+    Part<TG, C, A> next_g;
     if (row < p.rows) {
         locate();
         next_x.load(row_of<const TX>(p.x, b, l), k);
         next_g.load(row_of<const TG>(p.g, b, l), k);
     }
-    float gain[C][V], dw[C][V], db[C][V];
-    load_weights<V, C>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
+    float gain[C][kPiece], dw[C][kPiece], db[C][kPiece];
+    load_weights<C, A>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < V; ++i) dw[c][i] = db[c][i] = 0.f;
+        for (int i = 0; i < kPiece; ++i) dw[c][i] = db[c][i] = 0.f;
     for (int turn = 0; row < p.rows; turn ^= 1) {
-        float v[C][V], h[C][V];
+        float v[C][kPiece], h[C][kPiece];
         next_x.get(row_of<const TX>(p.x, b, l), k, v);
         next_g.get(row_of<const TG>(p.g, b, l), k, h);
         TX* const y = row_of<TX>(p.y, b, l);
@@ -318,12 +332,12 @@ __global__ __launch_bounds__((C * values_of<TX, TG>() > 8 ? 512 : 1024)) void la
             next_g.load(row_of<const TG>(p.g, b, l), k);
         }
         float mean, squares, sum = 0.f, dot = 0.f;
-        wave_statistics<V, C>(v, k, n, &mean, &squares);
+        wave_statistics<C, A>(v, k, n, &mean, &squares);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float hg = h[c][i] * gain[c][i];
+            for (int i = 0; i < kPiece; ++i) {
+                const float hg = k.own(c, i) ? h[c][i] * gain[c][i] : 0.f;
                 sum += hg;
                 dot += hg * v[c][i];
             }
@@ -340,13 +354,13 @@ __global__ __launch_bounds__((C * values_of<TX, TG>() > 8 ? 512 : 1024)) void la
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
+            for (int i = 0; i < kPiece; ++i) {
                 const float unit = (v[c][i] + j.shift) * r;
                 db[c][i] += h[c][i];
-                if (i < k.have[c]) dw[c][i] += h[c][i] * unit;
+                dw[c][i] += h[c][i] * unit;
                 v[c][i] = r * (h[c][i] * gain[c][i] - mean_h - unit * mean_hn);
             }
-        Part<TX, V, C, NT>::store(y, k, v);
+        Part<TX, C, A>::store(y, k, v);
     }
     // [group][workgroup][2][N]
     float* const out = p.part + (int64_t)blockIdx.x * 2 * p.N;
@@ -354,14 +368,14 @@ __global__ __launch_bounds__((C * values_of<TX, TG>() > 8 ? 512 : 1024)) void la
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i < k.have[c]) out[k.at[c] + i] = dw[c][i];
+            for (int i = 0; i < kPiece; ++i)
+                if (k.own(c, i)) out[k.at[c] + i] = dw[c][i];
     if (p.db)
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                if (i < k.have[c]) out[p.N + k.at[c] + i] = db[c][i];
+            for (int i = 0; i < kPiece; ++i)
+                if (k.own(c, i)) out[p.N + k.at[c] + i] = db[c][i];
 }
 
 // A group's gradients from its workgroups' sums, in a fixed order: 32 columns to a workgroup of 1024, 32 of its threads to a
@@ -388,83 +402,97 @@ __global__ __launch_bounds__(1024) void layer_norm_sum_kernel(NormParams p) {
     if (at == 0 && d < p.N) out[g * p.N + d] = part[0][col];
 }
 
-constexpr int kMostValues = 24;  // of a row to a thread: kNormMaxWidth in 512 threads
+constexpr int kMostPieces = 6;   // to a thread: kNormMaxWidth in 8 waves
 
-// Threads to a row, and pieces to a thread.  As few threads as hold a row with kMostValues each; where there are too few rows to
-// fill the card, 8 values each in up to 1024, for latency.
+// Waves that share a row, and pieces to a thread: the fewest of 1, 2, 3, 4 and 8 waves, which lie evenly on a compute unit's SIMDs
+// (rows of 5120 fp32 values to bf16: 4 and 5 194 us, 5 and 4 242).  Where there are too few rows to fill the card, up to kMostWaves
+// waves with up to 2 pieces, for latency.
 struct Shape {
-    int threads, pieces;
+    int waves, pieces;
 };
 
-Shape shape(int64_t rows, int N, int V, int cus) {
-    const int most = rows < 2 * (int64_t)cus && N <= 8 * 64 * kMostWaves ? 8 : kMostValues;
-    int threads = 64;
-    while (threads * most < N) threads *= 2;
-    return {threads, (N + threads * V - 1) / (threads * V)};
+Shape shape(int N, int64_t rows, int cus) {
+    const int groups = (N + 64 * kPiece - 1) / (64 * kPiece);   // of 64 pieces
+    if (rows < 2 * (int64_t)cus && groups <= 2 * kMostWaves) {
+        const int each = (groups + kMostWaves - 1) / kMostWaves;
+        return {(groups + each - 1) / each, each};
+    }
+    int waves = 1;
+    while (waves * kMostPieces < groups) waves = waves < 4 ? waves + 1 : 8;
+    return {waves, (groups + waves - 1) / waves};
 }
 
-// The kernel's pieces as a template parameter.  16-byte accesses of bf16 take 3 at most for kMostValues, of fp32 6.
-template <int V, typename F>
+// The kernel's pieces as a template parameter.
+template <typename F>
 hipError_t with_pieces(int pieces, F f) {
     switch (pieces) {
         case 1: f(std::integral_constant<int, 1>()); break;
         case 2: f(std::integral_constant<int, 2>()); break;
         case 3: f(std::integral_constant<int, 3>()); break;
-        case 4: f(std::integral_constant<int, V == 4 ? 4 : 1>()); break;
-        case 5: f(std::integral_constant<int, V == 4 ? 5 : 1>()); break;
-        case 6: f(std::integral_constant<int, V == 4 ? 6 : 1>()); break;
+        case 4: f(std::integral_constant<int, 4>()); break;
+        case 5: f(std::integral_constant<int, 5>()); break;
+        case 6: f(std::integral_constant<int, 6>()); break;
         default: return hipErrorInvalidConfiguration;
     }
     return hipGetLastError();
 }
 
-template <typename TX, typename TY, bool NT>
+template <typename TX, typename TY, Access A>
 hipError_t launch_forward(NormParams p, int groups, int cus, hipStream_t stream) {
-    constexpr int V = values_of<TX, TY>();
-    const Shape s = shape(p.rows * groups, p.N, V, cus);
-    return with_pieces<V>(s.pieces, [&](auto c) {
+    const Shape s = shape(p.N, p.rows * groups, cus);
+    return with_pieces(s.pieces, [&](auto c) {
         constexpr int C = decltype(c)::value;
-        const int resident = resident_blocks((const void*)layer_norm_kernel<TX, TY, C, NT>, s.threads, 0);
+        const int resident = resident_blocks((const void*)layer_norm_kernel<TX, TY, C, A>, 64 * s.waves, 0);
         p.parts = (int)std::min<int64_t>(p.rows, ((int64_t)resident * cus + groups - 1) / groups);
-        layer_norm_kernel<TX, TY, C, NT><<<(unsigned)(p.parts * groups), s.threads, 0, stream>>>(p);
+        layer_norm_kernel<TX, TY, C, A><<<(unsigned)(p.parts * groups), 64 * s.waves, 0, stream>>>(p);
     });
 }
 
-template <typename TX, typename TG, bool NT>
+template <typename TX, typename TG, Access A>
 hipError_t launch_backward(const NormParams& p, int groups, int cus, hipStream_t stream) {
-    constexpr int V = values_of<TX, TG>();
-    const Shape s = shape(p.rows * groups, p.N, V, cus);
-    const hipError_t e = with_pieces<V>(s.pieces, [&](auto c) {
-        layer_norm_backward_kernel<TX, TG, decltype(c)::value, NT><<<(unsigned)(p.parts * groups), s.threads, 0, stream>>>(p);
+    const Shape s = shape(p.N, p.rows * groups, cus);
+    const hipError_t e = with_pieces(s.pieces, [&](auto c) {
+        layer_norm_backward_kernel<TX, TG, decltype(c)::value, A><<<(unsigned)(p.parts * groups), 64 * s.waves, 0, stream>>>(p);
     });
     if (e != hipSuccess || (!p.dw && !p.db)) return e;
     layer_norm_sum_kernel<<<dim3((unsigned)((p.N + 31) / 32 * groups), 2), 1024, 0, stream>>>(p);
     return hipGetLastError();
 }
 
+template <typename TX, typename TO, bool BACK>
+hipError_t launch(const NormParams& p, int groups, int cus, hipStream_t stream) {
+    auto go = [&](auto access) {
+        constexpr Access A = decltype(access)::value;
+        if constexpr (BACK)
+            return launch_backward<TX, TO, A>(p, groups, cus, stream);
+        else
+            return launch_forward<TX, TO, A>(p, groups, cus, stream);
+    };
+    if (p.N % kPiece) return go(std::integral_constant<Access, kCut>());
+    return p.stream ? go(std::integral_constant<Access, kStream>()) : go(std::integral_constant<Access, kPlain>());
+}
+
+template <bool BACK>
+hipError_t launch(const NormParams& p, int groups, bool x_f32, bool o_f32, int cus, hipStream_t stream) {
+    if (x_f32) return o_f32 ? launch<float, float, BACK>(p, groups, cus, stream) : launch<float, bf16_t, BACK>(p, groups, cus, stream);
+    return o_f32 ? launch<bf16_t, float, BACK>(p, groups, cus, stream) : launch<bf16_t, bf16_t, BACK>(p, groups, cus, stream);
+}
+
 }  // namespace
 
 hipError_t launch_layer_norm(const NormParams& p, int groups, bool x_f32, bool y_f32, int cus, hipStream_t stream) {
-    if (p.stream) {
-        if (x_f32) return y_f32 ? launch_forward<float, float, true>(p, groups, cus, stream) : launch_forward<float, bf16_t, true>(p, groups, cus, stream);
-        return y_f32 ? launch_forward<bf16_t, float, true>(p, groups, cus, stream) : launch_forward<bf16_t, bf16_t, true>(p, groups, cus, stream);
-    }
-    if (x_f32) return y_f32 ? launch_forward<float, float, false>(p, groups, cus, stream) : launch_forward<float, bf16_t, false>(p, groups, cus, stream);
-    return y_f32 ? launch_forward<bf16_t, float, false>(p, groups, cus, stream) : launch_forward<bf16_t, bf16_t, false>(p, groups, cus, stream);
+    return launch<false>(p, groups, x_f32, y_f32, cus, stream);
 }
 
-int layer_norm_parts(int64_t rows, int groups, int cus) {
-    const int64_t each = std::max<int64_t>(1, (2 * (int64_t)cus + groups - 1) / groups);
-    return (int)std::max<int64_t>(1, std::min(rows, each));
+// 8 waves to a compute unit: more add to the sums that are written and read again, fewer leave loads without cover (2 x 4429 x
+// 3072 in bf16: 4, 8, 12 and 16 waves 83, 51, 46 and 46 us; 32760 x 5120: 4, 8 and 16 waves 306, 201 and 215).
+int layer_norm_parts(int64_t rows, int groups, int64_t N, int cus) {
+    const int64_t most = std::max<int64_t>(1, 8 / shape((int)N, rows * groups, cus).waves) * cus;
+    return (int)std::max<int64_t>(1, std::min(rows, (most + groups - 1) / groups));
 }
 
 hipError_t launch_layer_norm_backward(const NormParams& p, int groups, bool x_f32, bool g_f32, int cus, hipStream_t stream) {
-    if (p.stream) {
-        if (x_f32) return g_f32 ? launch_backward<float, float, true>(p, groups, cus, stream) : launch_backward<float, bf16_t, true>(p, groups, cus, stream);
-        return g_f32 ? launch_backward<bf16_t, float, true>(p, groups, cus, stream) : launch_backward<bf16_t, bf16_t, true>(p, groups, cus, stream);
-    }
-    if (x_f32) return g_f32 ? launch_backward<float, float, false>(p, groups, cus, stream) : launch_backward<float, bf16_t, false>(p, groups, cus, stream);
-    return g_f32 ? launch_backward<bf16_t, float, false>(p, groups, cus, stream) : launch_backward<bf16_t, bf16_t, false>(p, groups, cus, stream);
+    return launch<true>(p, groups, x_f32, g_f32, cus, stream);
 }
 
 }  // namespace orbit

@@ -60,6 +60,9 @@ orbit_status check_weight(const char* who, const char* name, const void* w, int6
     return ORBIT_OK;
 }
 
+// Whether the batches' rows follow each other at one stride
+bool flat(const NormRows& t, int64_t B, int64_t L) { return B <= 1 || L == 0 || t.batch == L * t.row; }
+
 // Groups of rows with weights of their own, and the rows of one
 int groups_of(int64_t B, bool joined) { return joined ? 1 : (int)B; }
 int64_t rows_of(int64_t B, int64_t L, bool joined) { return joined ? B * L : L; }
@@ -67,7 +70,7 @@ int64_t rows_of(int64_t B, int64_t L, bool joined) { return joined ? B * L : L; 
 size_t workspace_bytes_of(int64_t B, int64_t L, int64_t N, bool joined, int cus) {
     if (B == 0 && !joined) return 0;
     const int groups = groups_of(B, joined);
-    return (size_t)groups * layer_norm_parts(rows_of(B, L, joined), groups, cus) * 2 * N * sizeof(float);
+    return (size_t)groups * layer_norm_parts(rows_of(B, L, joined), groups, N, cus) * 2 * N * sizeof(float);
 }
 
 }  // namespace
@@ -105,6 +108,7 @@ orbit_status layer_norm(const orbit_rows* x, const orbit_rows* y, int64_t B, int
     p.eps = eps;
     p.stream = B * L * N * (size_of(x->dtype) + size_of(y->dtype)) > kStreamBytes;
     const int groups = groups_of(B, p.joined);
+    if (flat(p.x, B, L) && flat(p.y, B, L)) p.joined = 0;
     if ((int64_t)groups * 1024 > kMostThreads) return fail(ORBIT_EUNSUPPORTED, "%s: more than 2^22 - 1 batches with weights of their own", who);
     const hipError_t e = launch_layer_norm(p, groups, x->dtype == ORBIT_OUT_F32, y->dtype == ORBIT_OUT_F32, info.cus, (hipStream_t)stream);
     return e == hipSuccess ? ORBIT_OK : hip_fail(e, who);
@@ -163,11 +167,12 @@ orbit_status layer_norm_backward(const orbit_rows* dy, const orbit_rows* x, cons
     p.dw = dweight;
     p.db = dbias;
     const int groups = groups_of(B, p.joined);
-    p.parts = layer_norm_parts(p.rows, groups, info.cus);
+    p.parts = layer_norm_parts(p.rows, groups, N, info.cus);
+    const size_t bytes = workspace_bytes_of(B, L, N, p.joined, info.cus);
+    if (flat(p.x, B, L) && flat(p.y, B, L) && flat(p.g, B, L)) p.joined = 0;
     if ((int64_t)groups * std::max<int64_t>(1024 * p.parts, (N + 31) / 32 * 1024) > kMostThreads)
         return fail(ORBIT_EUNSUPPORTED, "%s: too many batches with gradients of their own for one launch", who);
     if (dweight || dbias) {
-        const size_t bytes = workspace_bytes_of(B, L, N, p.joined, info.cus);
         if (!workspace || !aligned(workspace, 16) || workspace_bytes < bytes)
             return fail(ORBIT_EINVAL, "%s: takes a workspace of %zu bytes, aligned to 16", who, bytes);
         p.part = (float*)workspace;
