@@ -179,35 +179,21 @@ __device__ __forceinline__ int seen_keys(int causal, int q_len, int k_len, int t
 }
 
 // Workgroups go round the 8 dies.  Those of one key head go to as few as they can, so that its keys and values stay in their
-// L2: all on one die where the heads are a multiple of 8, on 8 / kv_heads dies where they are a divisor of it.  The list's first
-// `lead` tiles go before the others, which are parts of tiles and level out the end.
+// L2: all on one die where the heads are a multiple of 8, on 8 / kv_heads dies where they are a divisor of it.
 struct Place {
-    int head, tile;
+    int head, tile;   // tile: `tiles` or more where there is none
 };
 
-__device__ __forceinline__ Place place_in(uint32_t id, uint32_t kv_heads, uint32_t tiles) {
+__device__ __forceinline__ Place place_of(uint32_t id, int kv_heads, int tiles) {
     const uint32_t die = id & 7, turn = id >> 3;
-    if (kv_heads % 8 == 0) return {(int)(die + 8 * (turn / tiles)), (int)(turn % tiles)};
-    if (8 % kv_heads == 0) return {(int)(die % kv_heads), (int)(turn * (8 / kv_heads) + die / kv_heads)};
-    return {(int)(id % kv_heads), (int)(id / kv_heads)};
+    if (kv_heads % 8 == 0) return {(int)(die + 8 * (turn / (uint32_t)tiles)), (int)(turn % (uint32_t)tiles)};
+    if (8 % kv_heads == 0) return {(int)(die % (uint32_t)kv_heads), (int)(turn * (8 / kv_heads) + die / (uint32_t)kv_heads)};
+    return {(int)(id % (uint32_t)kv_heads), (int)(id / (uint32_t)kv_heads)};
 }
 
 // Workgroups of a launch for that
-__host__ __device__ inline int64_t places_in(int64_t tiles, int kv_heads) {
+inline int64_t places(int64_t tiles, int kv_heads) {
     return kv_heads % 8 && 8 % kv_heads == 0 ? 8 * ((tiles + 8 / kv_heads - 1) / (8 / kv_heads)) : tiles * kv_heads;
 }
-
-// tile: `tiles` or more where there is none
-__device__ __forceinline__ Place place_of(uint32_t id, int kv_heads, int lead, int tiles) {
-    const uint32_t before = (uint32_t)places_in(lead, kv_heads);
-    if (id < before) {
-        const Place p = place_in(id, kv_heads, lead);
-        return {p.head, p.tile < lead ? p.tile : tiles};
-    }
-    const Place p = place_in(id - before, kv_heads, tiles - lead);
-    return {p.head, lead + p.tile};
-}
-
-inline int64_t places(int64_t lead, int64_t tiles, int kv_heads) { return places_in(lead, kv_heads) + places_in(tiles - lead, kv_heads); }
 
 }  // namespace orbit

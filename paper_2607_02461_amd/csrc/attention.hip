@@ -145,7 +145,7 @@ __device__ __forceinline__ void finish(const AttnParams& p, const AttnTile& t, i
 template <int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_kernel(AttnParams p) {
     __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * 2 * DP];
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -188,7 +188,7 @@ template <int DP>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     extern __shared__ __attribute__((aligned(1024))) char few_lds[];
     constexpr int kTile = 32 * 2 * DP;
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -252,42 +252,46 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     finish<DP, kAttnFewRows>(p, t, kv, row, mine, l, lane);
 }
 
-// Rows whose keys several workgroups shared: a wave to a row, in the order of the slots.
+// Rows whose keys several workgroups shared, in the order of their parts: DP / 8 lanes to a row, 8 values to a lane.
 template <int DP>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
-    const int lane = threadIdx.x & 63;
-    const uint32_t id = blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int row = id % kAttnWideRows, kv = id / kAttnWideRows % (uint32_t)p.kv_heads;
+    constexpr int kLanes = DP / 8;
+    const uint32_t id = (blockIdx.x * 256 + threadIdx.x) / kLanes;
+    const int row = id % kAttnWideRows, kv = id / kAttnWideRows % (uint32_t)p.kv_heads, d = threadIdx.x % kLanes * 8;
     const AttnJoin j = p.joins[id / kAttnWideRows / (uint32_t)p.kv_heads];
     const int r = j.first + row;
     if (row >= j.rows || r >= j.q_len * p.group) return;
-    float m = kLowest, l = 0.f, o[DP / 64] = {};
-    auto place = [&](int i) { return (int64_t)(j.slot + i * j.rows) * p.kv_heads + kv * j.rows + row; };
-    for (int i = 0; i < j.count; ++i) m = fmaxf(m, p.stat[2 * place(i)]);
+    float m = kLowest, l = 0.f, o[8] = {};
+    const int64_t first = (int64_t)j.slot * p.kv_heads + kv * j.rows + row, step = (int64_t)j.rows * p.kv_heads;
+#pragma unroll 4
+    for (int i = 0; i < j.count; ++i) m = fmaxf(m, p.stat[2 * (first + i * step)]);
+#pragma unroll 4
     for (int i = 0; i < j.count; ++i) {
-        const float factor = exp2_fast(p.stat[2 * place(i)] - m);
-        l += factor * p.stat[2 * place(i) + 1];
+        const f32x2 stat = *(const f32x2*)(p.stat + 2 * (first + i * step));
+        const float* const from = p.part + (first + i * step) * DP + d;
+        const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
+        const float factor = exp2_fast(stat.x - m);
+        l += factor * stat.y;
 #pragma unroll
-        for (int b = 0; b < DP / 64; ++b) o[b] += factor * p.part[place(i) * DP + 64 * b + lane];
+        for (int c = 0; c < 4; ++c) o[c] += factor * lo[c], o[4 + c] += factor * hi[c];
     }
     const int token = r / p.group, head = kv * p.group + r % p.group;
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    const int64_t to = (int64_t)(j.q_start + token) * p.o.token + head * p.o.head;
-#pragma unroll
-    for (int b = 0; b < DP / 64; ++b) {
-        const int d = 64 * b + lane;
-        if (d >= p.D) continue;
-        if (p.out_f32)
-            ((float*)p.o.p)[to + d] = o[b] * inv;
-        else
-            ((uint16_t*)p.o.p)[to + d] = (uint16_t)pack_bf16(o[b] * inv, 0.f);
+    const int64_t to = (int64_t)(j.q_start + token) * p.o.token + head * p.o.head + d;
+    if (p.lse && d == 0) p.lse[(int64_t)(j.q_start + token) * p.heads + head] = l == 0.f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
+    if (d >= p.D) return;
+    if (p.out_f32) {
+        *(f32x4*)((float*)p.o.p + to) = (f32x4){o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+        *(f32x4*)((float*)p.o.p + to + 4) = (f32x4){o[4] * inv, o[5] * inv, o[6] * inv, o[7] * inv};
+    } else {
+        *(u32x4*)((uint16_t*)p.o.p + to) = (u32x4){pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
+                                                  pack_bf16(o[4] * inv, o[5] * inv), pack_bf16(o[6] * inv, o[7] * inv)};
     }
-    if (p.lse && lane == 0) p.lse[(int64_t)(j.q_start + token) * p.heads + head] = l == 0.f ? -__builtin_inff() : (m + __builtin_log2f(l)) * kLn2;
 }
 
 template <int DP>
 hipError_t launch(const AttnParams& p, AttnWay way, hipStream_t stream) {
-    const unsigned grid = (unsigned)places(p.lead, p.count, p.kv_heads);
+    const unsigned grid = (unsigned)places(p.count, p.kv_heads);
     if (way != kAttnShared) {
         if (way == kAttnWide)
             attention_kernel<DP, 8><<<grid, 512, 0, stream>>>(p);
@@ -310,7 +314,7 @@ hipError_t launch_attention(const AttnParams& p, AttnWay way, hipStream_t stream
 }
 
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream) {
-    const unsigned grid = (unsigned)((int64_t)p.count * p.kv_heads * (kAttnWideRows / 4));
+    const unsigned grid = (unsigned)((int64_t)p.count * p.kv_heads * kAttnWideRows * (p.D > 64 ? 16 : 8) / 256);
     if (p.D > 64)
         attention_join_kernel<128><<<grid, 256, 0, stream>>>(p);
     else

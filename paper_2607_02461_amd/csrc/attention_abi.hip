@@ -40,48 +40,22 @@ struct Card {
     int64_t least;   // units that a part has at least
 };
 
-// Divides tiles along the other side where whole ones would leave the card partly idle; parts leave their sums in rows of their own,
-// which a join adds up.
-//   Slots that have less than two of the longest tiles each: parts of about half of what a slot has on average.
-//   A few rounds of tiles of one size: those of the last, partial round are divided so that all slots share them (or those of the last
-//   two).  With 1728 equal tiles on 512 slots the last round is 0.4 long instead of 1, of 3.4.
-// The longest tiles come first, then the parts: workgroups start in the list's order.
-void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t* slot_rows, std::vector<AttnJoin>* joins, std::vector<AttnTile>* out,
-            int64_t* lead) {
-    std::stable_sort(work.begin(), work.end(), [](const Work& a, const Work& b) { return a.cost > b.cost; });
-    const int64_t n = (int64_t)work.size(), all = n * kv_heads;
-    int64_t total = 0;
-    for (const Work& w : work) total += w.cost;
-    int64_t whole = n, part = 1;   // tiles that stay whole, and the size of the others' parts
-    if (n && total * kv_heads < 2 * work[0].cost * card.slots) {
-        part = std::max(card.least, ceil_div(total * kv_heads, 2 * card.slots));
-        whole = 0;
-    } else if (n && all < 12 * card.slots && 2 * work[n - 1].cost > work[0].cost) {
-        const int64_t rounds = all / card.slots, rest = all % card.slots;
-        const double cost = (double)total / n;
-        double best = rest ? 1.0 - 0.06 * (rounds + 1) : 0.0;   // of a round; a gain below 6% is none
-        for (int64_t more = 0; more <= 1 && more < rounds; ++more)
-            for (int64_t k = 2; k <= 6 && rest && cost >= k * card.least; ++k) {
-                const int64_t parts = (more * card.slots + rest) * k;
-                const double time = (double)ceil_div(parts, card.slots) * (1.0 / k + 1.5 / cost) - more;   // a part's begin and end: 1.5 units
-                if (time < best) {
-                    best = time;
-                    whole = n - ceil_div(more * card.slots + rest, kv_heads);
-                    part = ceil_div(work[0].cost, k);
-                }
-            }
-    }
-    *lead = whole;
-    std::vector<Work> parts;
-    for (int64_t i = 0; i < n; ++i) {
-        const Work& w = work[i];
+// Divides long tiles along the other side where whole ones would leave the card partly idle: where a slot has less than two of the
+// longest, into parts of about half of what a slot has.  Parts leave their sums in rows of their own, which a join adds up.  The
+// longest come first: workgroups start in the list's order, so the last to start are the shortest.
+// (Dividing the last, partial round of several as well, 1728 equal tiles on 512 slots for example, gained nothing, 502 and 504 us:
+// the workgroups of that round run alone on their compute units and take half the time.)
+void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t* slot_rows, std::vector<AttnJoin>* joins, std::vector<AttnTile>* out) {
+    int64_t total = 0, longest = 0;
+    for (const Work& w : work) total += w.cost, longest = std::max(longest, w.cost);
+    const bool few = total * kv_heads < 2 * longest * card.slots;
+    const int64_t part = few ? std::max(card.least, ceil_div(total * kv_heads, 2 * card.slots)) : longest;
+    std::vector<Work> all;
+    for (const Work& w : work) {
         const AttnTile& t = w.tile;
-        const int64_t k = i < whole ? 1 : std::max<int64_t>(1, (w.cost + part / 2) / part);
+        const int64_t k = few ? std::max<int64_t>(1, (w.cost + part / 2) / part) : 1;
         if (k == 1) {
-            if (i < whole)
-                out->push_back(t);
-            else
-                parts.push_back(w);
+            all.push_back(w);
             continue;
         }
         joins->push_back({t.q_start, t.q_len, t.k_start, t.k_len, t.first, (int32_t)*slot_rows, (int32_t)k, (int32_t)card.rows});
@@ -93,11 +67,11 @@ void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t
             piece.tile.end = (int32_t)std::min<int64_t>(t.end, t.begin + to * card.step);
             piece.tile.slot = (int32_t)*slot_rows;
             *slot_rows += card.rows;
-            parts.push_back(piece);
+            all.push_back(piece);
         }
     }
-    std::stable_sort(parts.begin(), parts.end(), [](const Work& a, const Work& b) { return a.cost > b.cost; });
-    for (const Work& w : parts) out->push_back(w.tile);
+    std::stable_sort(all.begin(), all.end(), [](const Work& a, const Work& b) { return a.cost > b.cost; });
+    for (const Work& w : all) out->push_back(w.tile);
 }
 
 // Lists of checked sequences.
@@ -141,11 +115,11 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
     std::vector<AttnTile> list[kAttnLists];
     std::vector<AttnJoin> joins, row_joins, key_joins;
     // resident on 256 compute units: two workgroups of four waves, one of eight, or one whose buffers take the LDS
-    divide(whole, p->kv_heads, {512, kAttnRows, 64, 4}, &p->slots, &joins, &list[kAttnForward], &p->lead[kAttnForward]);
-    divide(wide, p->kv_heads, {256, kAttnWideRows, 64, 4}, &p->slots, &joins, &list[kAttnForwardWide], &p->lead[kAttnForwardWide]);
-    divide(few, p->kv_heads, {256, kAttnFewRows, 128, 2}, &p->slots, &joins, &list[kAttnFew], &p->lead[kAttnFew]);
-    divide(every, p->kv_heads, {512, kAttnRows, 64, 4}, &p->row_slots, &row_joins, &list[kAttnRowGrads], &p->lead[kAttnRowGrads]);
-    divide(keys, p->kv_heads, {512, kAttnRows, queries, 4}, &p->key_slots, &key_joins, &list[kAttnKeyGrads], &p->lead[kAttnKeyGrads]);
+    divide(whole, p->kv_heads, {512, kAttnRows, 64, 4}, &p->slots, &joins, &list[kAttnForward]);
+    divide(wide, p->kv_heads, {256, kAttnWideRows, 64, 4}, &p->slots, &joins, &list[kAttnForwardWide]);
+    divide(few, p->kv_heads, {256, kAttnFewRows, 128, 2}, &p->slots, &joins, &list[kAttnFew]);
+    divide(every, p->kv_heads, {512, kAttnRows, 64, 4}, &p->row_slots, &row_joins, &list[kAttnRowGrads]);
+    divide(keys, p->kv_heads, {512, kAttnRows, queries, 4}, &p->key_slots, &key_joins, &list[kAttnKeyGrads]);
 
     std::vector<unsigned char>& blob = p->lists;
     auto append = [&](int which, const void* data, size_t count, size_t size) {
@@ -366,7 +340,6 @@ orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_head
     for (const auto& [which, way] : ways) {
         a.tiles = (const AttnTile*)(lists + p->at[which]);
         a.count = (int)p->count[which];
-        a.lead = (int)p->lead[which];
         if (!a.count) continue;
         const hipError_t e = launch_attention(a, way, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, who);
@@ -436,15 +409,12 @@ orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, cons
     const struct {
         AttnGradStep step;
         int list;
-    } steps[] = {{kAttnDelta, -1}, {kAttnRowGrad, kAttnRowGrads}, {kAttnRowJoin, kAttnRowJoins}, {kAttnKeyGrad, kAttnKeyGrads}, {kAttnKeyJoin, kAttnKeyJoins}};
+    } steps[] = {{kAttnRowGrad, kAttnRowGrads}, {kAttnRowJoin, kAttnRowJoins}, {kAttnKeyGrad, kAttnKeyGrads}, {kAttnKeyJoin, kAttnKeyJoins}};
     for (const auto& s : steps) {
-        if (s.list >= 0) {
-            a.count = (int)p->count[s.list];
-            a.lead = (int)p->lead[s.list];
-            a.tiles = (const AttnTile*)(lists + p->at[s.list]);
-            a.joins = (const AttnJoin*)(lists + p->at[s.list]);
-        }
-        if (s.list >= 0 ? a.count == 0 : p->q_tokens == 0) continue;
+        a.count = (int)p->count[s.list];
+        a.tiles = (const AttnTile*)(lists + p->at[s.list]);
+        a.joins = (const AttnJoin*)(lists + p->at[s.list]);
+        if (a.count == 0) continue;
         const hipError_t e = launch_attention_grad(a, s.step, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, who);
     }

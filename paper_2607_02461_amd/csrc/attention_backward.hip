@@ -29,52 +29,21 @@ __device__ __forceinline__ const uint16_t* at(const AttnHeads& t, int64_t token,
     return (const uint16_t*)t.p + token * t.token + head * t.head;
 }
 
-// For each row -sum(do o), and -lse in units of the scores (-infinite where the row sees no key: its probabilities are zeros then),
-// [key head][token * group + head of the group]: what the products of the next kernels begin from.  DP / 8 lanes to a row.
-template <int DP>
-__global__ __launch_bounds__(256) void attention_delta_kernel(AttnGradParams p) {
-    constexpr int kLanes = DP / 8;
-    const int d = threadIdx.x % kLanes * 8;
-    const int64_t rows = p.q_tokens * p.heads;
-    for (int64_t id = ((int64_t)blockIdx.x * 256 + threadIdx.x) / kLanes; id < rows; id += (int64_t)gridDim.x * (256 / kLanes)) {
-        const int64_t token = id / p.heads;
-        const int head = (int)(id - token * p.heads);
-        float sum = 0.f;
-        if (d < p.D) {
-            float a[8], b[8];
-            const u32x4 g = *(const u32x4*)(at(p.g, token, head) + d);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) a[2 * i] = bf16_low(g[i]), a[2 * i + 1] = bf16_high(g[i]);
-            const int64_t from = token * p.o.token + head * p.o.head + d;
-            if (p.o_f32) {
-                const f32x4 lo = *(const f32x4*)((const float*)p.o.p + from), hi = *(const f32x4*)((const float*)p.o.p + from + 4);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[i] = lo[i], b[4 + i] = hi[i];
-            } else {
-                const u32x4 o = *(const u32x4*)((const uint16_t*)p.o.p + from);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) b[2 * i] = bf16_low(o[i]), b[2 * i + 1] = bf16_high(o[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum += a[i] * b[i];
-        }
-#pragma unroll
-        for (int apart = 1; apart < kLanes; apart *= 2) sum += __shfl_xor(sum, apart);
-        if (d) continue;
-        const int kv = head / p.group;
-        const int64_t to = (kv * p.q_tokens + token) * p.group + (head - kv * p.group);
-        const float lse = p.lse[token * p.heads + head];
-        p.delta[to] = -sum;
-        p.lse2[to] = lse == -__builtin_inff() ? lse : -lse * kLog2e / p.scale;
-    }
-}
+constexpr int kExactKeys = 256;
 
 // dq of 128 rows, 32 to each wave, over their keys, 64 at a time in two buffers.  Transposed as in the forward pass: a lane has
 // one query.
+//
+// delta comes from the output, which was rounded to its type: an error that all of a row's ds share.  Beside many keys it is
+// small, but where rows see few of them it was half of the gradients' error.  So tiles of up to kExactKeys keys sum p dp first,
+// which is delta to fp32, in a pass of two products more (relative error of dq at 60 keys in bf16 0.0029 -> 0.0025, of causal
+// sequences of 900 0.0027 -> 0.0025).
+// The next kernel finds -delta, and -lse in units of the scores (-infinite where the row sees no key: its probabilities are zeros
+// then), [key head][token * group + head of the group]: what its products begin from.
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradParams p) {
     __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * 2 * DP];
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -91,55 +60,97 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
     u32x4 q[DP / 16], g[DP / 16];
     load_operand<DP>(at(p.q, t.q_start + token, head), p.D, lane, q);
     load_operand<DP>(at(p.g, t.q_start + token, head), p.D, lane, g);
-    const int64_t stat = ((int64_t)kv * p.q_tokens + t.q_start) * p.group + r;
-    const float lse2 = p.lse2[stat] * p.scale, delta = p.delta[stat];
+    const int64_t token_at = t.q_start + token;
+    float delta = 0.f;
+    {
+        // half of a row's values: those that the lane has of do
+        const int64_t from = token_at * p.o.token + head * p.o.head;
+#pragma unroll
+        for (int step = 0; step < DP / 16; ++step) {
+            const int d = 16 * step + 8 * (lane >> 5);
+            if (d >= p.D) continue;
+            float o[8];
+            if (p.o_f32) {
+                const f32x4 lo = *(const f32x4*)((const float*)p.o.p + from + d), hi = *(const f32x4*)((const float*)p.o.p + from + d + 4);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[i] = lo[i], o[4 + i] = hi[i];
+            } else {
+                const u32x4 w = *(const u32x4*)((const uint16_t*)p.o.p + from + d);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[2 * i] = bf16_low(w[i]), o[2 * i + 1] = bf16_high(w[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) delta += bf16_low(g[step][i]) * o[2 * i] + bf16_high(g[step][i]) * o[2 * i + 1];
+        }
+        delta = -(delta + other_half(delta));
+    }
+    const float lse = p.lse[token_at * p.heads + head];
+    const float lse2 = lse == -__builtin_inff() ? lse : -lse * kLog2e;
+    const bool live = t.first + row < rows;
     f32x16 dq[DP / 32];
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) dq[b][i] = 0.f;
     const int seen = seen_keys(p.causal, t.q_len, t.k_len, token), all = seen_keys(p.causal, t.q_len, t.k_len, t.first / p.group);
-    loads_done();
-    __syncthreads();
-    for (int key = t.begin; key < t.end;) {
+    bool last = t.slot >= 0 || t.end - t.begin > kExactKeys;
+    for (;; last = true) {
+        float sum = 0.f;
+        loads_done();
+        __syncthreads();
+        for (int key = t.begin; key < t.end;) {
 #pragma unroll
-        for (int buffer = 0; buffer < 2; ++buffer) {
-            if (key >= t.end) break;
-            if (key + 64 < t.end) load(key + 64, buffer ^ 1);
-            const char *const kt = lds[buffer][0], *const vt = lds[buffer][1];
+            for (int buffer = 0; buffer < 2; ++buffer) {
+                if (key >= t.end) break;
+                if (key + 64 < t.end) load(key + 64, buffer ^ 1);
+                const char *const kt = lds[buffer][0], *const vt = lds[buffer][1];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                f32x16 s, dp;
+                for (int n = 0; n < 2; ++n) {
+                    f32x16 s, dp;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
+                    for (int i = 0; i < 16; ++i) s[i] = dp[i] = 0.f;
 #pragma unroll
-                for (int step = 0; step < DP / 16; ++step) {
-                    s = mfma32(where.rows_of(kt, n, step), q[step], s);
-                    dp = mfma32(where.rows_of(vt, n, step), g[step], dp);
-                }
-                if (key + 64 > all) {
+                    for (int step = 0; step < DP / 16; ++step) {
+                        s = mfma32(where.rows_of(kt, n, step), q[step], s);
+                        dp = mfma32(where.rows_of(vt, n, step), g[step], dp);
+                    }
+                    if (key + 64 > all) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const bool hidden = 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= seen - key;
-                        s[i] = hidden ? -__builtin_inff() : s[i];
-                        dp[i] = hidden ? -delta : dp[i];
+                        for (int i = 0; i < 16; ++i) {
+                            const bool hidden = 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= seen - key;
+                            s[i] = hidden ? -__builtin_inff() : s[i];
+                            dp[i] = hidden ? 0.f : dp[i];
+                        }
+                    }
+                    if (!last) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum += exp2_fast(__builtin_fmaf(s[i], p.scale, lse2)) * dp[i];
+                        continue;
+                    }
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) dp[i] = exp2_fast(__builtin_fmaf(s[i], p.scale, lse2)) * (dp[i] + delta);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const u32x4 ds = as_operand(dp, u);
+#pragma unroll
+                        for (int b = 0; b < DP / 32; ++b) dq[b] = mfma32(where.columns_of(kt, 2 * n + u, b), ds, dq[b]);
                     }
                 }
-#pragma unroll
-                for (int i = 0; i < 16; ++i) dp[i] = exp2_fast(__builtin_fmaf(s[i], p.scale, lse2)) * (dp[i] + delta);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const u32x4 ds = as_operand(dp, u);
-#pragma unroll
-                    for (int b = 0; b < DP / 32; ++b) dq[b] = mfma32(where.columns_of(kt, 2 * n + u, b), ds, dq[b]);
-                }
+                loads_done();
+                __syncthreads();
+                key += 64;
             }
-            loads_done();
-            __syncthreads();
-            key += 64;
         }
+        if (last) break;
+        delta = -(sum + other_half(sum));
+        if (t.begin < t.end) load(t.begin, 0);
     }
-    const bool live = t.first + row < rows;
+    // parts of a tile have the same delta: the first writes it
+    if (live && lane < 32 && t.begin == 0) {
+        const int64_t stat = ((int64_t)kv * p.q_tokens + t.q_start) * p.group + r;
+        p.delta[stat] = delta;
+        p.lse2[stat] = lse2 / p.scale;
+    }
     if (t.slot >= 0)
         store_column_f32<DP>(dq, 1.f, p.part + ((int64_t)t.slot * p.kv_heads + kv * kAttnRows + row) * DP, DP, lane, live);
     else
@@ -180,7 +191,7 @@ template <int DP, int NK>
 __global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_kernel(AttnGradParams p) {
     constexpr int kTile = 64 * 2 * DP, kBuffer = 2 * kTile + 1024, kWaves = 4 / NK;
     extern __shared__ __attribute__((aligned(1024))) char key_lds[];
-    const Place place = place_of(blockIdx.x, p.kv_heads, p.lead, p.count);
+    const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -316,6 +327,7 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams
     for (int which = 0; which < (keys ? 2 : 1); ++which) {
         const float* const part = which ? p.part2 : p.part;
         float sum[8] = {};
+#pragma unroll 4
         for (int i = 0; i < j.count; ++i) {
             const float* const from = part + ((int64_t)(j.slot + i * kAttnRows) * p.kv_heads + kv * kAttnRows + row) * DP + d;
             const f32x4 lo = *(const f32x4*)from, hi = *(const f32x4*)(from + 4);
@@ -333,11 +345,8 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams
 
 template <int DP>
 hipError_t launch(const AttnGradParams& p, AttnGradStep step, hipStream_t stream) {
-    const unsigned grid = step == kAttnDelta ? 0 : (unsigned)places(p.lead, p.count, p.kv_heads);
+    const unsigned grid = (unsigned)places(p.count, p.kv_heads);
     switch (step) {
-        case kAttnDelta:
-            attention_delta_kernel<DP><<<(unsigned)std::min<int64_t>((p.q_tokens * p.heads * (DP / 8) + 255) / 256, 1 << 20), 256, 0, stream>>>(p);
-            break;
         case kAttnRowGrad:
             attention_row_grad_kernel<DP><<<grid, 256, 0, stream>>>(p);
             break;

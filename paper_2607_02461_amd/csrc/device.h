@@ -352,7 +352,7 @@ struct AttnHeads {            // [token][head][D] bf16 values (or fp32, results)
 struct AttnParams {
     const AttnTile* tiles;
     const AttnJoin* joins;
-    int count, lead;          // of the tiles, or of the joins; of the tiles that go first
+    int count;                // of the tiles, or of the joins
     int heads, kv_heads, group, D;
     int causal;
     float scale;              // of the scores, times log2(e)
@@ -372,18 +372,18 @@ hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream);
 struct AttnGradParams {
     const AttnTile* tiles;
     const AttnJoin* joins;
-    int count, lead;          // of the tiles, or of the joins; of the tiles that go first
+    int count;                // of the tiles, or of the joins
     int heads, kv_heads, group, D;
     int causal, o_f32;
     int64_t q_tokens;
     float scale, out_scale;   // of the scores times log2(e), and of dq and dk
     AttnHeads q, k, v, o, g, dq, dk, dv;   // g: the output's gradient
     const float* lse;         // [token][heads]
-    float *lse2, *delta;      // [key head][token * group + head of the group]
+    float *lse2, *delta;      // [key head][token * group + head of the group]: -lse in units of the scores, -sum(do o)
     float *part, *part2;      // as AttnParams: of dq; of dk and of dv
 };
 
-enum AttnGradStep { kAttnDelta, kAttnRowGrad, kAttnKeyGrad, kAttnRowJoin, kAttnKeyJoin };
+enum AttnGradStep { kAttnRowGrad, kAttnKeyGrad, kAttnRowJoin, kAttnKeyJoin };
 hipError_t launch_attention_grad(const AttnGradParams& p, AttnGradStep step, hipStream_t stream);
 
 }  // namespace orbit

@@ -95,8 +95,8 @@ struct orbit_attention_s {
     int64_t q_tokens = 0, k_tokens = 0;        // behind the last query, and the last key
     std::vector<unsigned char> lists;
     size_t at[kAttnLists] = {};                // byte offsets
-    int64_t count[kAttnLists] = {}, lead[kAttnLists] = {};   // entries, and tiles that go before the others
-    int64_t slots = 0, row_slots = 0, key_slots = 0;         // rows of partial sums: forward, and of the backward pass's two lists
+    int64_t count[kAttnLists] = {};
+    int64_t slots = 0, row_slots = 0, key_slots = 0;   // rows of partial sums: forward, and of the backward pass's two lists
     std::mutex mu;
     unsigned char* dev_lists[orbit::kMaxDevices] = {};
 };
