@@ -105,7 +105,7 @@ def _heads(t, name, heads, tokens, D=None, dev=None, dtypes=(torch.bfloat16,)):
     if t.dtype not in dtypes:
         raise ValueError(f"{name} must be {' or '.join(str(d) for d in dtypes)}, got {t.dtype}")
     shape = t.shape
-    if len(shape) != 3 or shape[1] != heads or shape[0] < tokens or (D is not None and shape[2] != D):
+    if len(shape) != 3 or shape[1] != heads or shape[0] < tokens or (D and shape[2] != D):
         raise ValueError(f"{name} must be [at least {tokens} tokens, {heads} heads, {'D' if D is None else D}], got {tuple(shape)}")
     if dev is not None and t.device != dev:
         raise ValueError(f"{name} is on {t.device}, the call runs on {dev}")
@@ -119,8 +119,8 @@ def _output(out, like, name, extent, dtype):
     """(out, its rows): the caller's output, checked, or a new one of `like`'s shape, zeros where no sequence has a token."""
     if out is None:
         whole = extent[0] == extent[1] == like.shape[0]
-        out = (torch.empty if whole else torch.zeros)(like.shape, dtype=dtype, device=like.device)
-        H, D = like.shape[1:]
+        out = (torch.empty_like if whole else torch.zeros_like)(like, dtype=dtype, memory_format=torch.contiguous_format)
+        _, H, D = like.shape
         return out, _pack_heads(out.data_ptr(), 0, H * D, D, H, _TYPES[dtype])
     rows = _heads(out, name, like.shape[1], extent[0], like.shape[2], like.device, (dtype,))
     if out.shape != like.shape:

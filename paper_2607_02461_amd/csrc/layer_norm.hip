@@ -442,8 +442,8 @@ hipError_t launch_forward(NormParams p, int groups, int cus, hipStream_t stream)
     const Shape s = shape(p.N, p.rows * groups, cus);
     return with_pieces(s.pieces, [&](auto c) {
         constexpr int C = decltype(c)::value;
-        const int resident = resident_blocks((const void*)layer_norm_kernel<TX, TY, C, A>, 64 * s.waves, 0);
-        p.parts = (int)std::min<int64_t>(p.rows, ((int64_t)resident * cus + groups - 1) / groups);
+        const int64_t resident = p.rows * groups <= cus ? 1 : resident_blocks((const void*)layer_norm_kernel<TX, TY, C, A>, 64 * s.waves, 0);
+        p.parts = (int)std::min<int64_t>(p.rows, (resident * cus + groups - 1) / groups);
         layer_norm_kernel<TX, TY, C, A><<<(unsigned)(p.parts * groups), 64 * s.waves, 0, stream>>>(p);
     });
 }
