@@ -7,13 +7,15 @@
 // That product's order of keys is then 8 a + 4 (l / 32) + c, in the other operand too: V (or K, Q, dO), whose values of one
 // column it needs, is read from LDS by ds_read_b64_tr_b16, which turns 4 rows x 16 columns for 16 lanes.
 //
-// A tile of rows lies in LDS as it does in memory, DP values of 2 bytes to a row, its 16-byte chunks in an order that differs from
-// row to row (`swizzled`): both ways of reading find their rows in different banks.  Lanes load the chunks in that order
+// DP: the head size, padded to a multiple of 32 (of the products' columns).  A tile of rows lies in LDS as it does in memory, 128 or
+// 256 bytes to a row, its 16-byte chunks in an order that differs from row to row (`swizzled`): both ways of reading find their rows in different banks.  Lanes load the chunks in that order
 // (global_load_lds: lane i's 16 bytes go to the wave's place + 16 i).
 #pragma once
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+
+#include <type_traits>
 
 #include "device.h"
 #include "vec.h"
@@ -44,11 +46,14 @@ __device__ __forceinline__ float other_half(float v) {
     return __uint_as_float((threadIdx.x & 32) ? r[0] : r[1]);
 }
 
+template <int DP>
+constexpr int kRowBytes = DP > 64 ? 256 : 128;   // of a row in LDS
+
 // Chunk c of a row, as it lies in the tile.  16 rows in a row have one chunk in 16 places of the 256 bytes that LDS serves in a
 // clock, and 4 rows that begin at a multiple of 4 have 64 bytes each in different ones.
 template <int DP>
 __device__ __forceinline__ int swizzled(int row, int c) {
-    if (DP == 128) return c ^ ((row & 3) << 2 | (row >> 2 & 3));
+    if (DP > 64) return c ^ ((row & 3) << 2 | (row >> 2 & 3));
     return c ^ ((row >> 1 & 1) << 2 | (row >> 2 & 3));
 }
 
@@ -60,7 +65,7 @@ __device__ __forceinline__ int swizzled(int row, int c) {
 // LDS.  They have no output registers; loads_done() waits for them.
 template <int DP, int ROWS, int WAVES>
 struct TileLoads {
-    static constexpr int kChunks = DP / 8, kEach = 64 / kChunks, kLoads = ROWS / kEach / WAVES;
+    static constexpr int kChunks = kRowBytes<DP> / 16, kEach = 64 / kChunks, kLoads = ROWS / kEach / WAVES;
     const char* rows;       // the sequence's first row
     int64_t stride;         // bytes
     uint32_t from[kLoads];  // bytes from a tile's first row
@@ -110,19 +115,19 @@ struct Operands {
     int row, column;   // bytes: of chunk l / 32 of the lane's row, and of the lane's 4 values in columns 0 .. 31 of rows 4 (l / 32) ..
     __device__ __forceinline__ explicit Operands(int lane) {
         const int r = lane & 31, half = lane >> 5, i = lane & 15, key = 4 * half + (i >> 2), d = 16 * (lane >> 4 & 1) + 4 * (i & 3);
-        row = r * (2 * DP) + 16 * swizzled<DP>(r, half);
-        column = key * (2 * DP) + 16 * swizzled<DP>(key, d / 8) + 2 * (d & 7);
+        row = r * kRowBytes<DP> + 16 * swizzled<DP>(r, half);
+        column = key * kRowBytes<DP> + 16 * swizzled<DP>(key, d / 8) + 2 * (d & 7);
     }
     // rows 32 block .. of the tile, k-step s
     __device__ __forceinline__ u32x4 rows_of(const char* tile, int block, int s) const {
-        return *(const ORBIT_LDS u32x4*)(uintptr_t)(lds_address(tile) + block * 64 * DP + (row ^ 32 * s));
+        return *(const ORBIT_LDS u32x4*)(uintptr_t)(lds_address(tile) + block * 32 * kRowBytes<DP> + (row ^ 32 * s));
     }
     // columns 32 b .., rows 16 step .. of the tile, 8 a + 4 (l / 32) .. of them
     __device__ __forceinline__ u32x4 columns_of(const char* tile, int step, int b) const {
-        const uint32_t at = lds_address(tile) + step * 32 * DP;
+        const uint32_t at = lds_address(tile) + step * 16 * kRowBytes<DP>;
         auto four = [&](int a) {
             return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                                                 (ORBIT_LDS s16x4*)(uintptr_t)(at + 16 * DP * a + (column ^ (64 * b | 32 * a)))));
+                                                 (ORBIT_LDS s16x4*)(uintptr_t)(at + 8 * kRowBytes<DP> * a + (column ^ (64 * b | 32 * a)))));
         };
         const u32x2 lo = four(0), hi = four(1);
         return (u32x4){lo.x, lo.y, hi.x, hi.y};
@@ -194,6 +199,13 @@ __device__ __forceinline__ Place place_of(uint32_t id, int kv_heads, int tiles) 
 // Workgroups of a launch for that
 inline int64_t places(int64_t tiles, int kv_heads) {
     return kv_heads % 8 && 8 % kv_heads == 0 ? 8 * ((tiles + 8 / kv_heads - 1) / (8 / kv_heads)) : tiles * kv_heads;
+}
+
+// The padded head size as a template parameter
+template <typename F>
+hipError_t with_padded_dim(int D, F f) {
+    return D > 96 ? f(std::integral_constant<int, 128>()) : D > 64 ? f(std::integral_constant<int, 96>())
+         : D > 32 ? f(std::integral_constant<int, 64>()) : f(std::integral_constant<int, 32>());
 }
 
 }  // namespace orbit

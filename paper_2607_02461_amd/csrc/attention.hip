@@ -144,7 +144,7 @@ __device__ __forceinline__ void finish(const AttnParams& p, const AttnTile& t, i
 // 32 rows to each wave; 64 keys at a time, shared, in two buffers.
 template <int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, 2) void attention_kernel(AttnParams p) {
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * 2 * DP];
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * kRowBytes<DP>];
     const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
@@ -187,7 +187,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void attention_kernel(AttnParams p) 
 template <int DP>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     extern __shared__ __attribute__((aligned(1024))) char few_lds[];
-    constexpr int kTile = 32 * 2 * DP;
+    constexpr int kTile = 32 * kRowBytes<DP>;
     const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
@@ -256,9 +256,10 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
 template <int DP>
 __global__ __launch_bounds__(256) void attention_join_kernel(AttnParams p) {
     constexpr int kLanes = DP / 8;
-    const uint32_t id = (blockIdx.x * 256 + threadIdx.x) / kLanes;
-    const int row = id % kAttnWideRows, kv = id / kAttnWideRows % (uint32_t)p.kv_heads, d = threadIdx.x % kLanes * 8;
-    const AttnJoin j = p.joins[id / kAttnWideRows / (uint32_t)p.kv_heads];
+    const uint32_t at = blockIdx.x * 256 + threadIdx.x, id = at / kLanes, which = id / kAttnWideRows / (uint32_t)p.kv_heads;
+    const int row = id % kAttnWideRows, kv = id / kAttnWideRows % (uint32_t)p.kv_heads, d = at % kLanes * 8;
+    if (which >= (uint32_t)p.count) return;
+    const AttnJoin j = p.joins[which];
     const int r = j.first + row;
     if (row >= j.rows || r >= j.q_len * p.group) return;
     float m = kLowest, l = 0.f, o[8] = {};
@@ -299,7 +300,7 @@ hipError_t launch(const AttnParams& p, AttnWay way, hipStream_t stream) {
             attention_kernel<DP, 4><<<grid, 256, 0, stream>>>(p);
         return hipGetLastError();
     }
-    constexpr int kBytes = 4 * 4 * 32 * 2 * DP;   // the waves' buffers; their sums and states take less
+    constexpr int kBytes = 4 * 4 * 32 * kRowBytes<DP>;   // the waves' buffers; their sums and states take less
     static std::atomic<uint64_t> raised{0};
     const hipError_t e = raise_lds_limit((const void*)attention_few_kernel<DP>, kBytes, raised);
     if (e != hipSuccess) return e;
@@ -310,16 +311,15 @@ hipError_t launch(const AttnParams& p, AttnWay way, hipStream_t stream) {
 }  // namespace
 
 hipError_t launch_attention(const AttnParams& p, AttnWay way, hipStream_t stream) {
-    return p.D > 64 ? launch<128>(p, way, stream) : launch<64>(p, way, stream);
+    return with_padded_dim(p.D, [&](auto d) { return launch<decltype(d)::value>(p, way, stream); });
 }
 
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream) {
-    const unsigned grid = (unsigned)((int64_t)p.count * p.kv_heads * kAttnWideRows * (p.D > 64 ? 16 : 8) / 256);
-    if (p.D > 64)
-        attention_join_kernel<128><<<grid, 256, 0, stream>>>(p);
-    else
-        attention_join_kernel<64><<<grid, 256, 0, stream>>>(p);
-    return hipGetLastError();
+    return with_padded_dim(p.D, [&](auto d) {
+        constexpr int DP = decltype(d)::value;
+        attention_join_kernel<DP><<<(unsigned)(((int64_t)p.count * p.kv_heads * kAttnWideRows * (DP / 8) + 255) / 256), 256, 0, stream>>>(p);
+        return hipGetLastError();
+    });
 }
 
 }  // namespace orbit

@@ -42,7 +42,7 @@ constexpr int kExactKeys = 256;
 // then), [key head][token * group + head of the group]: what its products begin from.
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradParams p) {
-    __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * 2 * DP];
+    __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * kRowBytes<DP>];
     const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
@@ -157,10 +157,10 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
         store_column<DP>(dq, p.out_scale, (uint16_t*)at(p.dq, t.q_start + token, head), p.D, lane, live);
 }
 
-// Loads of 64 rows (token * group + head of the group) of one key head's queries, as TileLoads.
+// Loads of 64 rows (token * group + head of the group) of one key head's queries by WAVES waves, as TileLoads.
 template <int DP, int WAVES>
 struct RowLoads {
-    static constexpr int kChunks = DP / 8, kEach = 64 / kChunks, kLoads = 64 / kEach / WAVES;
+    static constexpr int kChunks = kRowBytes<DP> / 16, kEach = 64 / kChunks, kLoads = 64 / kEach / WAVES;
     const char* rows;
     int64_t token;    // bytes
     uint32_t head;    // bytes
@@ -184,20 +184,20 @@ struct RowLoads {
     }
 };
 
-// dk and dv of 128 keys, 32 NK to each wave, over the rows that see them, 64 at a time in two buffers: q, do, lse2 and delta.  A lane
-// has one key of each 32.  At D = 128 a wave's keys, values and sums take 192 registers for 32 keys; 64 take all 512 of a wave
-// alone on its SIMD, and each operand that is read from LDS serves twice.
-template <int DP, int NK>
-__global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_kernel(AttnGradParams p) {
-    constexpr int kTile = 64 * 2 * DP, kBuffer = 2 * kTile + 1024, kWaves = 4 / NK;
+// dk and dv of 128 keys, 32 to each wave, over the rows that see them, 64 at a time in two buffers: q, do, lse2 and delta.  A lane
+// has one key.  At D = 128 a wave's keys, values and sums take 192 of its 256 registers, so what follows from the lane is computed
+// again where it is used (kept, it spilled 27).
+template <int DP>
+__global__ __launch_bounds__(256, 2) void attention_key_grad_kernel(AttnGradParams p) {
+    constexpr int kTile = 64 * kRowBytes<DP>, kBuffer = 2 * kTile + 1024;
     extern __shared__ __attribute__((aligned(1024))) char key_lds[];
     const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
     const AttnTile t = p.tiles[place.tile];
     const int kv = place.head, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rows = t.q_len * p.group, begin = t.begin * p.group, end = t.end * p.group;
-    const RowLoads<DP, kWaves> q(at(p.q, t.q_start, kv * p.group), p.q.token, p.q.head, p.group, rows - 1);
-    const RowLoads<DP, kWaves> g(at(p.g, t.q_start, kv * p.group), p.g.token, p.g.head, p.group, rows - 1);
+    const RowLoads<DP, 4> q(at(p.q, t.q_start, kv * p.group), p.q.token, p.q.head, p.group, rows - 1);
+    const RowLoads<DP, 4> g(at(p.g, t.q_start, kv * p.group), p.g.token, p.g.head, p.group, rows - 1);
     const int64_t stat = ((int64_t)kv * p.q_tokens + t.q_start) * p.group;
     const char* const stats = (const char*)((wave & 1 ? p.delta : p.lse2) + stat);
     auto load = [&](int row, int buffer) {
@@ -213,19 +213,16 @@ __global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_
     };
     if (begin < end) load(begin, 0);
     Operands<DP> where(lane);
-    int key[NK];
-    u32x4 k[NK][DP / 16], v[NK][DP / 16];
-    f32x16 dk[NK][DP / 32], dv[NK][DP / 32];
+    const int key = t.first + 32 * wave + (lane & 31);
+    const int64_t token = t.k_start + min(key, t.k_len - 1);
+    u32x4 k[DP / 16], v[DP / 16];
+    f32x16 dk[DP / 32], dv[DP / 32];
+    load_operand<DP>(at(p.k, token, kv), p.D, lane, k);
+    load_operand<DP>(at(p.v, token, kv), p.D, lane, v);
 #pragma unroll
-    for (int m = 0; m < NK; ++m) {
-        key[m] = t.first + 32 * (NK * wave + m) + (lane & 31);
-        load_operand<DP>(at(p.k, t.k_start + min(key[m], t.k_len - 1), kv), p.D, lane, k[m]);
-        load_operand<DP>(at(p.v, t.k_start + min(key[m], t.k_len - 1), kv), p.D, lane, v[m]);
+    for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
-        for (int b = 0; b < DP / 32; ++b)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) dk[m][b][i] = dv[m][b][i] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) dk[b][i] = dv[b][i] = 0.f;
     // the first row that sees all of the tile's keys
     const int shift = t.k_len - t.q_len;
     const int all = p.causal ? max(0, min(t.first + kAttnRows, t.k_len) - 1 - shift) * p.group : 0;
@@ -239,59 +236,41 @@ __global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_
             const char *const qt = key_lds + buffer * kBuffer, *const gt = qt + kTile;
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
-                f32x16 s[NK], dp[NK];
+                f32x16 s, dp;
                 asm volatile("" : "+v"(where.row), "+v"(where.column));
 #pragma unroll
-                for (int m = 0; m < NK; ++m)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const char* const from = gt + kTile + 4 * (32 * n + 8 * (i / 4) + 4 * (lane >> 5));
-                        s[m][i] = (*(const ORBIT_LDS f32x4*)from)[i % 4];
-                        dp[m][i] = (*(const ORBIT_LDS f32x4*)(from + 256))[i % 4];
-                    }
+                for (int i = 0; i < 16; ++i) {
+                    const char* const from = gt + kTile + 4 * (32 * n + 8 * (i / 4) + 4 * (lane >> 5));
+                    s[i] = (*(const ORBIT_LDS f32x4*)from)[i % 4];
+                    dp[i] = (*(const ORBIT_LDS f32x4*)(from + 256))[i % 4];
+                }
 #pragma unroll
                 for (int step = 0; step < DP / 16; ++step) {
-                    const u32x4 a = where.rows_of(qt, n, step), b = where.rows_of(gt, n, step);
-#pragma unroll
-                    for (int m = 0; m < NK; ++m) {
-                        s[m] = mfma32(a, k[m][step], s[m]);
-                        dp[m] = mfma32(b, v[m][step], dp[m]);
-                    }
+                    s = mfma32(where.rows_of(qt, n, step), k[step], s);
+                    dp = mfma32(where.rows_of(gt, n, step), v[step], dp);
                 }
-                const bool masked = row < all || row + 64 > end;
 #pragma unroll
-                for (int m = 0; m < NK; ++m)
+                for (int i = 0; i < 16; ++i) {
+                    s[i] = exp2_fast(s[i] * p.scale);
+                    dp[i] *= s[i];
+                }
+                if (row < all || row + 64 > end) {
+                    const int first = p.causal ? max(0, key - shift) * p.group : 0;   // that sees the lane's key
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        s[m][i] = exp2_fast(s[m][i] * p.scale);
-                        dp[m][i] *= s[m][i];
-                    }
-                if (masked) {
-#pragma unroll
-                    for (int m = 0; m < NK; ++m) {
-                        const int first = p.causal ? max(0, key[m] - shift) * p.group : 0;   // that sees the lane's key
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            const int r = row + 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
-                            const bool live = r >= first && r < end;
-                            s[m][i] = live ? s[m][i] : 0.f;
-                            dp[m][i] = live ? dp[m][i] : 0.f;
-                        }
+                        const int r = row + 32 * n + 8 * (i / 4) + 4 * (lane >> 5) + i % 4;
+                        const bool live = r >= first && r < end;
+                        s[i] = live ? s[i] : 0.f;
+                        dp[i] = live ? dp[i] : 0.f;
                     }
                 }
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    u32x4 pb[NK], ds[NK];
-#pragma unroll
-                    for (int m = 0; m < NK; ++m) pb[m] = as_operand(s[m], u), ds[m] = as_operand(dp[m], u);
+                    const u32x4 pb = as_operand(s, u), ds = as_operand(dp, u);
 #pragma unroll
                     for (int b = 0; b < DP / 32; ++b) {
-                        const u32x4 gc = where.columns_of(gt, 2 * n + u, b), qc = where.columns_of(qt, 2 * n + u, b);
-#pragma unroll
-                        for (int m = 0; m < NK; ++m) {
-                            dv[m][b] = mfma32(gc, pb[m], dv[m][b]);
-                            dk[m][b] = mfma32(qc, ds[m], dk[m][b]);
-                        }
+                        dv[b] = mfma32(where.columns_of(gt, 2 * n + u, b), pb, dv[b]);
+                        dk[b] = mfma32(where.columns_of(qt, 2 * n + u, b), ds, dk[b]);
                     }
                 }
             }
@@ -300,18 +279,14 @@ __global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_
             row += 64;
         }
     }
-#pragma unroll
-    for (int m = 0; m < NK; ++m) {
-        const bool live = key[m] < t.k_len;
-        if (t.slot >= 0) {
-            const int64_t to = ((int64_t)t.slot * p.kv_heads + kv * kAttnRows + 32 * (NK * wave + m) + (lane & 31)) * DP;
-            store_column_f32<DP>(dk[m], 1.f, p.part + to, DP, lane, live);
-            store_column_f32<DP>(dv[m], 1.f, p.part2 + to, DP, lane, live);
-        } else {
-            const int64_t token = t.k_start + min(key[m], t.k_len - 1);
-            store_column<DP>(dk[m], p.out_scale, (uint16_t*)at(p.dk, token, kv), p.D, lane, live);
-            store_column<DP>(dv[m], 1.f, (uint16_t*)at(p.dv, token, kv), p.D, lane, live);
-        }
+    const bool live = key < t.k_len;
+    if (t.slot >= 0) {
+        const int64_t to = ((int64_t)t.slot * p.kv_heads + kv * kAttnRows + 32 * wave + (lane & 31)) * DP;
+        store_column_f32<DP>(dk, 1.f, p.part + to, DP, lane, live);
+        store_column_f32<DP>(dv, 1.f, p.part2 + to, DP, lane, live);
+    } else {
+        store_column<DP>(dk, p.out_scale, (uint16_t*)at(p.dk, token, kv), p.D, lane, live);
+        store_column<DP>(dv, 1.f, (uint16_t*)at(p.dv, token, kv), p.D, lane, live);
     }
 }
 
@@ -319,9 +294,10 @@ __global__ __launch_bounds__(256 / NK, NK == 1 ? 2 : 1) void attention_key_grad_
 template <int DP>
 __global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams p, bool keys) {
     constexpr int kLanes = DP / 8;
-    const uint32_t id = (blockIdx.x * 256 + threadIdx.x) / kLanes;
-    const int row = id % kAttnRows, kv = id / kAttnRows % (uint32_t)p.kv_heads, d = threadIdx.x % kLanes * 8;
-    const AttnJoin j = p.joins[id / kAttnRows / (uint32_t)p.kv_heads];
+    const uint32_t place = blockIdx.x * 256 + threadIdx.x, id = place / kLanes, which_join = id / kAttnRows / (uint32_t)p.kv_heads;
+    const int row = id % kAttnRows, kv = id / kAttnRows % (uint32_t)p.kv_heads, d = place % kLanes * 8;
+    if (which_join >= (uint32_t)p.count) return;
+    const AttnJoin j = p.joins[which_join];
     const int r = j.first + row;
     if (r >= (keys ? j.k_len : j.q_len * p.group) || d >= p.D) return;
     for (int which = 0; which < (keys ? 2 : 1); ++which) {
@@ -351,15 +327,15 @@ hipError_t launch(const AttnGradParams& p, AttnGradStep step, hipStream_t stream
             attention_row_grad_kernel<DP><<<grid, 256, 0, stream>>>(p);
             break;
         case kAttnKeyGrad: {
-            constexpr int kKeys = 1, kBytes = 2 * (2 * 64 * 2 * DP + 1024);
+            constexpr int kBytes = 2 * (2 * 64 * kRowBytes<DP> + 1024);
             static std::atomic<uint64_t> raised{0};
-            const hipError_t e = raise_lds_limit((const void*)attention_key_grad_kernel<DP, kKeys>, kBytes, raised);
+            const hipError_t e = raise_lds_limit((const void*)attention_key_grad_kernel<DP>, kBytes, raised);
             if (e != hipSuccess) return e;
-            attention_key_grad_kernel<DP, kKeys><<<grid, 256 / kKeys, kBytes, stream>>>(p);
+            attention_key_grad_kernel<DP><<<grid, 256, kBytes, stream>>>(p);
             break;
         }
         default:
-            attention_grad_join_kernel<DP><<<(unsigned)((int64_t)p.count * p.kv_heads * kAttnRows * (DP / 8) / 256), 256, 0, stream>>>(p, step == kAttnKeyJoin);
+            attention_grad_join_kernel<DP><<<(unsigned)(((int64_t)p.count * p.kv_heads * kAttnRows * (DP / 8) + 255) / 256), 256, 0, stream>>>(p, step == kAttnKeyJoin);
     }
     return hipGetLastError();
 }
@@ -367,7 +343,7 @@ hipError_t launch(const AttnGradParams& p, AttnGradStep step, hipStream_t stream
 }  // namespace
 
 hipError_t launch_attention_grad(const AttnGradParams& p, AttnGradStep step, hipStream_t stream) {
-    return p.D > 64 ? launch<128>(p, step, stream) : launch<64>(p, step, stream);
+    return with_padded_dim(p.D, [&](auto d) { return launch<decltype(d)::value>(p, step, stream); });
 }
 
 }  // namespace orbit

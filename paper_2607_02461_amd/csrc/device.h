@@ -364,7 +364,7 @@ struct AttnParams {
 };
 
 // Floats of a row's sums.
-constexpr int attention_part(int D) { return D > 64 ? 128 : 64; }
+constexpr int attention_part(int D) { return (D + 31) / 32 * 32; }
 enum AttnWay { kAttnWhole, kAttnWide, kAttnShared };   // tiles of kAttnRows, of kAttnWideRows, of kAttnFewRows
 hipError_t launch_attention(const AttnParams& p, AttnWay way, hipStream_t stream);
 hipError_t launch_attention_join(const AttnParams& p, hipStream_t stream);
