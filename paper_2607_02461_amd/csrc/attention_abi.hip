@@ -37,23 +37,44 @@ struct Card {
     int64_t slots;   // workgroups that are resident
     int64_t rows;    // of a tile
     int64_t step;    // keys (or queries) in a unit of cost
-    int64_t least;   // units that a part has at least
+    double begin;    // units that a workgroup's begin and end take,
+    double join;     // that a join's launch takes,
+    double part;     // and that each part's sums take, written and read again
 };
 
-// Divides long tiles along the other side where whole ones would leave the card partly idle: where a slot has less than two of the
-// longest, into parts of about half of what a slot has.  Parts leave their sums in rows of their own, which a join adds up.  The
-// longest come first: workgroups start in the list's order, so the last to start are the shortest.
+// Divides tiles along the other side where that is estimated to end earlier: where few long tiles leave the card partly idle.  Parts
+// leave their sums in rows of their own, which a join adds up.  A list ends after as many rounds of its longest tile as there are,
+// or after what each slot has and most of one, whichever is earlier.  The longest come first: workgroups start in the list's order, so the last to start are the shortest.
+// Measured, us (D = 128, whole / in parts): forward 1024 tokens in 24 heads, causal, 22 / 30; in 4 heads, not causal, 21 / 17;
+// single tokens over 2000 keys in 8 key heads, 4 sequences, 19 / 12.
 // (Dividing the last, partial round of several as well, 1728 equal tiles on 512 slots for example, gained nothing, 502 and 504 us:
 // the workgroups of that round run alone on their compute units and take half the time.)
 void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t* slot_rows, std::vector<AttnJoin>* joins, std::vector<AttnTile>* out) {
     int64_t total = 0, longest = 0;
     for (const Work& w : work) total += w.cost, longest = std::max(longest, w.cost);
-    const bool few = total * kv_heads < 2 * longest * card.slots;
-    const int64_t part = few ? std::max(card.least, ceil_div(total * kv_heads, 2 * card.slots)) : longest;
+    const double share = (double)total * kv_heads / card.slots;
+    auto ends = [&](int64_t count, int64_t most) {
+        const double each = most + card.begin, rounds = (double)count * kv_heads / card.slots;
+        return rounds <= 1.0 ? each : std::min(std::ceil(rounds) * each, share + rounds * card.begin + 0.8 * each);
+    };
+    auto parts_of = [](int64_t cost, int64_t part) { return std::max<int64_t>(1, (2 * cost + part) / (2 * part)); };
+    int64_t part = INT64_MAX / 4;
+    double best = ends((int64_t)work.size(), longest);
+    for (int64_t size = (longest + 1) / 2; share < longest && size >= 2; size -= 1 + size / 16) {
+        int64_t count = 0, parts = 0, most = 0;
+        for (const Work& w : work) {
+            const int64_t n = parts_of(w.cost, size);
+            count += n;
+            if (n > 1) parts += n;
+            most = std::max(most, ceil_div(w.cost, n));
+        }
+        const double time = ends(count, most) + card.join + card.part * parts * kv_heads;
+        if (time < best) best = time, part = size;
+    }
     std::vector<Work> all;
     for (const Work& w : work) {
         const AttnTile& t = w.tile;
-        const int64_t k = few ? std::max<int64_t>(1, (w.cost + part / 2) / part) : 1;
+        const int64_t k = parts_of(w.cost, part);
         if (k == 1) {
             all.push_back(w);
             continue;
@@ -114,12 +135,14 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
     }
     std::vector<AttnTile> list[kAttnLists];
     std::vector<AttnJoin> joins, row_joins, key_joins;
-    // resident on 256 compute units: two workgroups of four waves, one of eight, or one whose buffers take the LDS
-    divide(whole, p->kv_heads, {512, kAttnRows, 64, 4}, &p->slots, &joins, &list[kAttnForward]);
-    divide(wide, p->kv_heads, {256, kAttnWideRows, 64, 4}, &p->slots, &joins, &list[kAttnForwardWide]);
-    divide(few, p->kv_heads, {256, kAttnFewRows, 128, 2}, &p->slots, &joins, &list[kAttnFew]);
-    divide(every, p->kv_heads, {512, kAttnRows, 64, 4}, &p->row_slots, &row_joins, &list[kAttnRowGrads]);
-    divide(keys, p->kv_heads, {512, kAttnRows, queries, 4}, &p->key_slots, &key_joins, &list[kAttnKeyGrads]);
+    // Resident on 256 compute units: two workgroups of four waves, one of eight, or one whose buffers take the LDS.  A unit takes 0.9
+    // us forward (1.2 of few rows), 1.2 for the rows' gradients and 1.6 for the keys', a join 5 to 8 us, a part's 64 KB (16 of few
+    // rows, 128 of keys) twice their time at 4.7 TB/s.
+    divide(whole, p->kv_heads, {512, kAttnRows, 64, 1.5, 6.0, 0.030}, &p->slots, &joins, &list[kAttnForward]);
+    divide(wide, p->kv_heads, {256, kAttnWideRows, 64, 2.0, 6.0, 0.060}, &p->slots, &joins, &list[kAttnForwardWide]);
+    divide(few, p->kv_heads, {256, kAttnFewRows, 128, 2.5, 3.0, 0.004}, &p->slots, &joins, &list[kAttnFew]);
+    divide(every, p->kv_heads, {512, kAttnRows, 64, 1.5, 5.0, 0.023}, &p->row_slots, &row_joins, &list[kAttnRowGrads]);
+    divide(keys, p->kv_heads, {512, kAttnRows, queries, 1.5, 4.0, 0.035}, &p->key_slots, &key_joins, &list[kAttnKeyGrads]);
 
     std::vector<unsigned char>& blob = p->lists;
     auto append = [&](int which, const void* data, size_t count, size_t size) {

@@ -234,7 +234,7 @@ __global__ __launch_bounds__(256, 2) void attention_key_grad_kernel(AttnGradPara
             if (row >= end) break;
             if (row + 64 < end) load(row + 64, buffer ^ 1);
             const char *const qt = key_lds + buffer * kBuffer, *const gt = qt + kTile;
-#pragma unroll
+#pragma unroll 1
             for (int n = 0; n < 2; ++n) {
                 f32x16 s, dp;
                 asm volatile("" : "+v"(where.row), "+v"(where.column));

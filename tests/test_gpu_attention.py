@@ -167,7 +167,8 @@ def test_layouts_and_fp32_results(layout, D):
     (1, 100, 8, 2, True, ["attention_few_kernel<128>"]),
     (40, 3000, 4, 2, True, ["attention_kernel<128,4>", "attention_join_kernel<128>"]),           # a chunk of new tokens
     (1100, 1100, 4, 4, True, ["attention_kernel<128,4>", "attention_join_kernel<128>"]),         # a prompt that leaves compute units idle
-    (700, 700, 4, 4, False, ["attention_kernel<128,4>", "attention_join_kernel<128>"]),
+    (1300, 1300, 4, 4, False, ["attention_kernel<128,4>", "attention_join_kernel<128>"]),
+    (500, 500, 4, 4, False, ["attention_kernel<128,4>"]),                                        # short ones: a join would take longer
     (300, 70, 120, 120, False, ["attention_kernel<128,4>"]),
     (600, 8200, 180, 180, False, ["attention_kernel<128,8>"]),                                   # long, and enough of them: wide tiles
     (700, 16500, 172, 172, True, ["attention_kernel<128,8>"]),
