@@ -646,7 +646,7 @@ orbit_status attention_workspace_size(orbit_attention p, int64_t D, int32_t back
  *   workspace  attention_workspace_size bytes, aligned to 16; contents and ownership as for orbit_qlinear_ws
  * Scores, maxima and sums are fp32; probabilities enter the product with v in bf16, whose sum is fp32 and is rounded once.
  * The same plan and inputs give the same bits.  A value that is not finite in a key or value may show, as a NaN, in every
- * query of its sequence that shares a tile of 128 rows with one that sees it; rows of other sequences do not depend on it.
+ * query of its sequence that shares a tile of up to 256 rows with one that sees it; rows of other sequences do not depend on it.
  * Data and strides are multiples of 16 bytes, a token's stride at most 2^24 values.  Errors: ORBIT_EINVAL (null pointers,
  * types, strides, alignment, scale, a plan without tables on the device); ORBIT_EUNSUPPORTED (D); ORBIT_EHIP.  A plan
  * without queries returns at once.
