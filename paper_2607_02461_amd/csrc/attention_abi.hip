@@ -44,7 +44,8 @@ struct Card {
 
 // Divides tiles along the other side where that is estimated to end earlier: where few long tiles leave the card partly idle.  Parts
 // leave their sums in rows of their own, which a join adds up.  A list ends after as many rounds of its longest tile as there are,
-// or after what each slot has and most of one, whichever is earlier.  The longest come first: workgroups start in the list's order, so the last to start are the shortest.
+// or after what each slot has and most of one, whichever is earlier.  The longest come first: workgroups start in the list's order, so the last to
+// start are the shortest.
 // Measured, us (D = 128, whole / in parts): forward 1024 tokens in 24 heads, causal, 22 / 30; in 4 heads, not causal, 21 / 17;
 // single tokens over 2000 keys in 8 key heads, 4 sequences, 19 / 12.
 // (Dividing the last, partial round of several as well, 1728 equal tiles on 512 slots for example, gained nothing, 502 and 504 us:
@@ -60,7 +61,7 @@ void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t
     auto parts_of = [](int64_t cost, int64_t part) { return std::max<int64_t>(1, (2 * cost + part) / (2 * part)); };
     int64_t part = INT64_MAX / 4;
     double best = ends((int64_t)work.size(), longest);
-    for (int64_t size = (longest + 1) / 2; share < longest && size >= 2; size -= 1 + size / 16) {
+    for (int64_t size = (longest + 1) / 2; share < longest && size >= 2; size -= 1 + size / (work.size() > 4096 ? 4 : 16)) {
         int64_t count = 0, parts = 0, most = 0;
         for (const Work& w : work) {
             const int64_t n = parts_of(w.cost, size);
@@ -68,6 +69,7 @@ void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t
             if (n > 1) parts += n;
             most = std::max(most, ceil_div(w.cost, n));
         }
+        if (count > (kMaxGroups - 8192) / kv_heads || parts * card.rows > kMaxTokens / 4) break;
         const double time = ends(count, most) + card.join + card.part * parts * kv_heads;
         if (time < best) best = time, part = size;
     }
@@ -108,7 +110,8 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
         wide_tiles += tiles;
         wide_cost += tiles * (p->causal ? (s.k_len + 1) / 2 : s.k_len);
     }
-    const bool widely = wide_tiles * p->kv_heads >= 2 * 256 && wide_cost >= 8192 * wide_tiles;
+    const int64_t wide_groups = wide_tiles * p->kv_heads;
+    const bool widely = wide_groups >= 2 * 256 && wide_groups < kMaxGroups / 2 && wide_cost >= 8192 * wide_tiles;
     for (const Sequence& s : sequences) {
         const int64_t rows = s.q_len * group;
         auto tiles = [&](std::vector<Work>& to, int64_t most, int64_t unit) {
@@ -219,11 +222,13 @@ orbit_status check_heads(const char* who, const char* name, const orbit_heads* t
 
 size_t forward_bytes(orbit_attention p, int64_t D) { return (size_t)p->slots * p->kv_heads * (attention_part((int)D) + 2) * sizeof(float); }
 
-// Of the backward pass: lse and delta of each row, then the parts of dq, whose place those of dk and dv take afterwards.
+// Of the backward pass: lse and delta of each row, then the parts of dq (with those of sum p k, and sum ds of each row, where D <= 64),
+// whose place those of dk and dv take afterwards.
 size_t stat_floats(orbit_attention p) { return ((size_t)p->heads * p->q_tokens + 63) / 64 * 64; }
 
 size_t backward_bytes(orbit_attention p, int64_t D) {
-    return (2 * stat_floats(p) + (size_t)std::max(p->row_slots, 2 * p->key_slots) * p->kv_heads * attention_part((int)D)) * sizeof(float);
+    const int64_t part = attention_part((int)D), of_rows = p->row_slots * (part <= 64 ? 2 * part + 1 : part), of_keys = p->key_slots * 2 * part;
+    return (2 * stat_floats(p) + (size_t)std::max(of_rows, of_keys) * p->kv_heads) * sizeof(float);
 }
 
 // The backward pass finds a tile's heads by 32-bit offsets
@@ -252,9 +257,9 @@ orbit_status attention_plan(int64_t n, const int64_t* q_starts, const int64_t* q
         if (q_starts[i] < 0 || q_lens[i] < 0 || k_starts[i] < 0 || k_lens[i] < 0)
             return fail(ORBIT_EINVAL, "%s: sequence %lld has a negative start or length", who, (long long)i);
         if (q_starts[i] > kMaxTokens || q_lens[i] > kMaxTokens - q_starts[i] || k_starts[i] > kMaxTokens || k_lens[i] > kMaxTokens - k_starts[i] ||
-            q_lens[i] > (kMaxTokens - kAttnRows) / group || k_lens[i] > kMaxTokens - kAttnRows)
+            q_lens[i] > (kMaxTokens - kAttnWideRows) / group || k_lens[i] > kMaxTokens - kAttnWideRows)
             return fail(ORBIT_EUNSUPPORTED, "%s: sequence %lld passes 2^31 rows", who, (long long)i);
-        // keys' tiles too, those of the backward pass; a list divides further only where it has fewer than some 1000 tiles
+        // keys' tiles too, those of the backward pass
         tiles += ceil_div(q_lens[i] * group, kAttnRows) + ceil_div(k_lens[i], kAttnRows);
         if (tiles > (kMaxGroups - 8192) / kv_heads) return fail(ORBIT_EUNSUPPORTED, "%s: more tiles of rows than a launch takes", who);
         if (q_lens[i]) q_tokens = std::max(q_tokens, q_starts[i] + q_lens[i]);
@@ -428,7 +433,7 @@ orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, cons
     a.lse2 = (float*)workspace;
     a.delta = a.lse2 + stat_floats(p);
     a.part = a.delta + stat_floats(p);
-    a.part2 = a.part + p->key_slots * p->kv_heads * attention_part((int)D);
+    a.part_sum = a.part + 2 * p->row_slots * p->kv_heads * attention_part((int)D);
     const struct {
         AttnGradStep step;
         int list;
@@ -438,6 +443,8 @@ orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, cons
         a.tiles = (const AttnTile*)(lists + p->at[s.list]);
         a.joins = (const AttnJoin*)(lists + p->at[s.list]);
         if (a.count == 0) continue;
+        const bool of_rows = s.step == kAttnRowGrad || s.step == kAttnRowJoin;
+        a.part2 = a.part + (of_rows ? p->row_slots : p->key_slots) * p->kv_heads * attention_part((int)D);
         const hipError_t e = launch_attention_grad(a, s.step, (hipStream_t)stream);
         if (e != hipSuccess) return hip_fail(e, who);
     }

@@ -29,19 +29,26 @@ __device__ __forceinline__ const uint16_t* at(const AttnHeads& t, int64_t token,
     return (const uint16_t*)t.p + token * t.token + head * t.head;
 }
 
-constexpr int kExactKeys = 256;
+constexpr int kExactKeys = 512;
 
 // dq of 128 rows, 32 to each wave, over their keys, 64 at a time in two buffers.  Transposed as in the forward pass: a lane has
 // one query.
 //
-// delta comes from the output, which was rounded to its type: an error that all of a row's ds share.  Beside many keys it is
-// small, but where rows see few of them it was half of the gradients' error.  So tiles of up to kExactKeys keys sum p dp first,
-// which is delta to fp32, in a pass of two products more (relative error of dq at 60 keys in bf16 0.0029 -> 0.0025, of causal
-// sequences of 900 0.0027 -> 0.0025).
+// delta comes from the output, which was rounded to its type: an error e that all of a row's ds share, and that reaches dq as
+// e sum p k.  Beside many keys of many values that is small; else it was up to a third of the gradients' error.  The exact delta
+// makes sum ds = 0, so that sum, taken in fp32 before ds is rounded, is e:
+//   - heads of up to 64 values sum p k as well, a product more, and take e times it off at the end (of a tile in parts, where
+//     they are joined).  Error of dq in bf16, as a
+//     multiple of what its own rounding makes: 1.53 -> 1.47 at 40 values, 1.47 -> 1.44 at 64; forward and backward pass of 7
+//     sequences of up to 2048 with 16 heads of 64: 198 -> 210 us.
+//   - wider ones have no registers for it.  Tiles of up to kExactKeys keys sum p dp first, which is delta, in a pass of two
+//     products more: 1.50 -> 1.44 at 400 keys of 96 values, for 233 -> 266 us of 16 sequences with 24 heads.  Longer ones are
+//     left at 1.47 and less: for all of them it cost 970 -> 1100 us at 1163 keys of 128 values.
 // The next kernel finds -delta, and -lse in units of the scores (-infinite where the row sees no key: its probabilities are zeros
 // then), [key head][token * group + head of the group]: what its products begin from.
 template <int DP>
 __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradParams p) {
+    constexpr bool kSums = DP <= 64;
     __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * kRowBytes<DP>];
     const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;
@@ -53,9 +60,13 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
         k.load(key, lds[buffer][0], p.D, lane);
         v.load(key, lds[buffer][1], p.D, lane);
     };
-    if (t.begin < t.end) load(t.begin, 0);
-    const Operands<DP> where(lane);
     const int row = 32 * wave + (lane & 31), rows = t.q_len * p.group;
+    // keys of the tile's last row: of a part of a tile, those of the whole tile
+    const int whole = seen_keys(p.causal, t.q_len, t.k_len, (min(t.first + kAttnRows, rows) - 1) / p.group);
+    bool last = kSums || whole > kExactKeys;
+    int begin = last ? t.begin : 0, end = last ? t.end : whole;
+    if (begin < end) load(begin, 0);
+    const Operands<DP> where(lane);
     const int r = min(t.first + row, rows - 1), token = r / p.group, head = kv * p.group + r % p.group;
     u32x4 q[DP / 16], g[DP / 16];
     load_operand<DP>(at(p.q, t.q_start + token, head), p.D, lane, q);
@@ -87,22 +98,22 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
     const float lse = p.lse[token_at * p.heads + head];
     const float lse2 = lse == -__builtin_inff() ? lse : -lse * kLog2e;
     const bool live = t.first + row < rows;
-    f32x16 dq[DP / 32];
+    f32x16 dq[DP / 32], mean[kSums ? DP / 32 : 1];
 #pragma unroll
     for (int b = 0; b < DP / 32; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) dq[b][i] = 0.f;
+        for (int i = 0; i < 16; ++i) dq[b][i] = mean[kSums ? b : 0][i] = 0.f;
     const int seen = seen_keys(p.causal, t.q_len, t.k_len, token), all = seen_keys(p.causal, t.q_len, t.k_len, t.first / p.group);
-    bool last = t.slot >= 0 || t.end - t.begin > kExactKeys;
-    for (;; last = true) {
-        float sum = 0.f;
+    float sum;
+    for (;; last = true, begin = t.begin, end = t.end) {
+        sum = 0.f;
         loads_done();
         __syncthreads();
-        for (int key = t.begin; key < t.end;) {
+        for (int key = begin; key < end;) {
 #pragma unroll
             for (int buffer = 0; buffer < 2; ++buffer) {
-                if (key >= t.end) break;
-                if (key + 64 < t.end) load(key + 64, buffer ^ 1);
+                if (key >= end) break;
+                if (key + 64 < end) load(key + 64, buffer ^ 1);
                 const char *const kt = lds[buffer][0], *const vt = lds[buffer][1];
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
@@ -128,12 +139,20 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
                         continue;
                     }
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) dp[i] = exp2_fast(__builtin_fmaf(s[i], p.scale, lse2)) * (dp[i] + delta);
+                    for (int i = 0; i < 16; ++i) {
+                        s[i] = exp2_fast(__builtin_fmaf(s[i], p.scale, lse2));
+                        dp[i] = s[i] * (dp[i] + delta);
+                        if constexpr (kSums) sum += dp[i];
+                    }
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const u32x4 ds = as_operand(dp, u);
+                        const u32x4 ds = as_operand(dp, u), weights = as_operand(s, u);
 #pragma unroll
-                        for (int b = 0; b < DP / 32; ++b) dq[b] = mfma32(where.columns_of(kt, 2 * n + u, b), ds, dq[b]);
+                        for (int b = 0; b < DP / 32; ++b) {
+                            const u32x4 keys = where.columns_of(kt, 2 * n + u, b);
+                            dq[b] = mfma32(keys, ds, dq[b]);
+                            if constexpr (kSums) mean[b] = mfma32(keys, weights, mean[b]);
+                        }
                     }
                 }
                 loads_done();
@@ -145,16 +164,27 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
         delta = -(sum + other_half(sum));
         if (t.begin < t.end) load(t.begin, 0);
     }
+    if (kSums) sum += other_half(sum);
+    if (kSums && t.slot < 0) {
+        delta -= sum;
+#pragma unroll
+        for (int b = 0; b < DP / 32; ++b)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dq[b][i] -= sum * mean[kSums ? b : 0][i];
+    }
     // parts of a tile have the same delta: the first writes it
     if (live && lane < 32 && t.begin == 0) {
         const int64_t stat = ((int64_t)kv * p.q_tokens + t.q_start) * p.group + r;
         p.delta[stat] = delta;
         p.lse2[stat] = lse2 / p.scale;
     }
-    if (t.slot >= 0)
-        store_column_f32<DP>(dq, 1.f, p.part + ((int64_t)t.slot * p.kv_heads + kv * kAttnRows + row) * DP, DP, lane, live);
-    else
-        store_column<DP>(dq, p.out_scale, (uint16_t*)at(p.dq, t.q_start + token, head), p.D, lane, live);
+    if (t.slot < 0) return store_column<DP>(dq, p.out_scale, (uint16_t*)at(p.dq, t.q_start + token, head), p.D, lane, live);
+    const int64_t part = (int64_t)t.slot * p.kv_heads + kv * kAttnRows + row;
+    store_column_f32<DP>(dq, 1.f, p.part + part * DP, DP, lane, live);
+    if constexpr (kSums) {
+        store_column_f32<DP>(mean, 1.f, p.part2 + part * DP, DP, lane, live);
+        if (live && lane < 32) p.part_sum[part] = sum;
+    }
 }
 
 // Loads of 64 rows (token * group + head of the group) of one key head's queries by WAVES waves, as TileLoads.
@@ -300,7 +330,13 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams
     const AttnJoin j = p.joins[which_join];
     const int r = j.first + row;
     if (r >= (keys ? j.k_len : j.q_len * p.group) || d >= p.D) return;
-    for (int which = 0; which < (keys ? 2 : 1); ++which) {
+    float first[8], all = 0.f;   // of the rows' parts: sum ds k, and sum ds
+    const bool sums = DP <= 64 && !keys;
+    if (sums) {
+        for (int i = 0; i < j.count; ++i) all += p.part_sum[(int64_t)(j.slot + i * kAttnRows) * p.kv_heads + kv * kAttnRows + row];
+        if (d == 0) p.delta[((int64_t)kv * p.q_tokens + j.q_start) * p.group + r] -= all;
+    }
+    for (int which = 0; which < (keys || sums ? 2 : 1); ++which) {
         const float* const part = which ? p.part2 : p.part;
         float sum[8] = {};
 #pragma unroll 4
@@ -310,7 +346,12 @@ __global__ __launch_bounds__(256) void attention_grad_join_kernel(AttnGradParams
 #pragma unroll
             for (int c = 0; c < 4; ++c) sum[c] += lo[c], sum[4 + c] += hi[c];
         }
-        const float factor = which ? 1.f : p.out_scale;
+        if (sums) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) which ? sum[c] = first[c] - all * sum[c] : first[c] = sum[c];
+            if (!which) continue;
+        }
+        const float factor = keys && which ? 1.f : p.out_scale;
         u32x4 w;
 #pragma unroll
         for (int c = 0; c < 4; ++c) w[c] = pack_bf16(sum[2 * c] * factor, sum[2 * c + 1] * factor);

@@ -380,7 +380,8 @@ struct AttnGradParams {
     AttnHeads q, k, v, o, g, dq, dk, dv;   // g: the output's gradient
     const float* lse;         // [token][heads]
     float *lse2, *delta;      // [key head][token * group + head of the group]: -lse in units of the scores, -sum(do o)
-    float *part, *part2;      // as AttnParams: of dq; of dk and of dv
+    float *part, *part2;      // as AttnParams: of dq and of sum p k (D <= 64); of dk and of dv
+    float* part_sum;          // of sum ds (D <= 64)
 };
 
 enum AttnGradStep { kAttnRowGrad, kAttnKeyGrad, kAttnRowJoin, kAttnKeyJoin };

@@ -150,6 +150,40 @@ def test_attention_and_gradients(ql, kl, heads, kv_heads, D, causal, layout):
     b.check(o, b.backward(o))
 
 
+@pytest.mark.parametrize("D,n", [(40, 60), (64, 700), (128, 60), (96, 512)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_gradients_of_values_alike(D, n, causal):
+    """Values alike, and keys: what the output's rounding takes from delta, e0 <= sum|do| (error of o), is many times what sets ds
+    apart, and e0 sum p k many times dq.  The kernel finds delta again from p and dp, off by (2 E + 10 sqrt(n) u) sum p |dp| and the
+    products' error; a bf16 rounding of what e0 leaves in ds and in the products that take it off is 2 h p e0."""
+    heads = 2
+    b = Batch([n], None, heads, heads, D, causal, 31)
+    b.v.mul_(0.05).add_(1.0)
+    b.k.add_(1.0)
+    o = b.forward()
+    dq, dk, _ = b.backward(o)
+    q, k, v, do = (_f64(t) for t in (b.q, b.k, b.v, b.do))
+    ref, _ = oracle.attention(q, k, v, b.scale, causal)
+    p, _ = oracle.attention_probabilities(q, k, b.scale, causal)
+    want = oracle.attention_backward(do, q, k, v, b.scale, causal)
+    bars = [H * np.abs(t) for t in want[:2]]
+    grown = lambda m: 10 * math.sqrt(m) * U  # noqa: E731
+    for h in range(heads):
+        qh, kh, vh, gh = q[:, h], k[:, h], v[:, h], do[:, h]
+        scores, dp, delta = b.scale * qh @ kh.T, gh @ vh.T, (gh * ref[:, h]).sum(1, keepdims=True)
+        lse = np.log(np.where(p[h] > 0, np.exp(scores), 0).sum(1))
+        E = (2 * grown(D) * (b.scale * np.abs(qh) @ np.abs(kh).T) + 32 * U * (1 + np.abs(scores))).max(1, keepdims=True) + 32 * U * np.abs(lse)[:, None]
+        products = grown(D) * (np.abs(gh) @ np.abs(vh).T).max(1, keepdims=True)
+        e0 = (np.abs(gh) * (2 * H + 2 * E + grown(n)) * (p[h] @ np.abs(vh))).sum(1, keepdims=True)
+        again = (2 * E + grown(n)) * (p[h] * np.abs(dp)).sum(1, keepdims=True)
+        err = p[h] * ((2 * E + H) * np.abs(dp - delta) + 2 * products + again + 2 * H * e0) + T * (1 + np.abs(dp - delta))
+        ds = p[h] * (np.abs(dp - delta) + e0)
+        bars[0][:, h] += b.scale * ((err + grown(n) * ds) @ np.abs(kh) + n * T)
+        bars[1][:, h] += b.scale * ((err + grown(n) * ds).T @ np.abs(qh) + n * T)
+    _within("dq", dq, want[0], bars[0])
+    _within("dk", dk, want[1], bars[1])
+
+
 @pytest.mark.parametrize("layout", ["heads", "padded"])
 @pytest.mark.parametrize("D", [64, 128])
 def test_layouts_and_fp32_results(layout, D):
