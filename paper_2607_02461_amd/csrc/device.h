@@ -320,7 +320,7 @@ struct NormParams {
 
 hipError_t launch_layer_norm(const NormParams& p, int groups, bool x_f32, bool y_f32, int cus, hipStream_t stream);
 // Workgroups to a group of the backward pass, each with a row of sums.
-int layer_norm_parts(int64_t rows, int groups, int64_t N, int cus);
+int layer_norm_parts(int64_t rows, int groups, int64_t N, bool x_f32, int cus);
 // rows = 0 gives zeros in dw and db.
 hipError_t launch_layer_norm_backward(const NormParams& p, int groups, bool x_f32, bool g_f32, int cus, hipStream_t stream);
 

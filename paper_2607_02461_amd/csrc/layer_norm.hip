@@ -484,10 +484,12 @@ hipError_t launch_layer_norm(const NormParams& p, int groups, bool x_f32, bool y
     return launch<false>(p, groups, x_f32, y_f32, cus, stream);
 }
 
-// 8 waves to a compute unit: more add to the sums that are written and read again, fewer leave loads without cover (2 x 4429 x
-// 3072 in bf16: 4, 8, 12 and 16 waves 83, 51, 46 and 46 us; 32760 x 5120: 4, 8 and 16 waves 306, 201 and 215).
-int layer_norm_parts(int64_t rows, int groups, int64_t N, int cus) {
-    const int64_t most = std::max<int64_t>(1, 8 / shape((int)N, rows * groups, cus).waves) * cus;
+// 8 waves to a compute unit, 6 where x is fp32: more add to the sums that are written and read again, and have more rows on their
+// way than the memory serves at once; fewer leave loads without cover.  us of 4, 6, 8, 12 and 16 waves:
+//     x bf16, dy bf16, 32760 x 5120: 270 270 196 248 212    8858 x 3072: 54 45 43 51 57    65536 x 1024: 110 103 88 93 102
+//     x fp32, dy bf16, 32760 x 5120: 293 293 333 347 346    8858 x 3072: 57 56 58 62 70    65536 x 2048: 282 242 259 276 299
+int layer_norm_parts(int64_t rows, int groups, int64_t N, bool x_f32, int cus) {
+    const int64_t most = std::max<int64_t>(1, (x_f32 ? 6 : 8) / shape((int)N, rows * groups, cus).waves) * cus;
     return (int)std::max<int64_t>(1, std::min(rows, (most + groups - 1) / groups));
 }
 

@@ -70,7 +70,7 @@ int64_t rows_of(int64_t B, int64_t L, bool joined) { return joined ? B * L : L; 
 size_t workspace_bytes_of(int64_t B, int64_t L, int64_t N, bool joined, int cus) {
     if (B == 0 && !joined) return 0;
     const int groups = groups_of(B, joined);
-    return (size_t)groups * layer_norm_parts(rows_of(B, L, joined), groups, N, cus) * 2 * N * sizeof(float);
+    return (size_t)groups * layer_norm_parts(rows_of(B, L, joined), groups, N, false, cus) * 2 * N * sizeof(float);
 }
 
 }  // namespace
@@ -167,7 +167,7 @@ orbit_status layer_norm_backward(const orbit_rows* dy, const orbit_rows* x, cons
     p.dw = dweight;
     p.db = dbias;
     const int groups = groups_of(B, p.joined);
-    p.parts = layer_norm_parts(p.rows, groups, N, info.cus);
+    p.parts = layer_norm_parts(p.rows, groups, N, x->dtype == ORBIT_OUT_F32, info.cus);
     const size_t bytes = workspace_bytes_of(B, L, N, p.joined, info.cus);
     if (flat(p.x, B, L) && flat(p.y, B, L) && flat(p.g, B, L)) p.joined = 0;
     if ((int64_t)groups * std::max<int64_t>(1024 * p.parts, (N + 31) / 32 * 1024) > kMostThreads)
