@@ -118,13 +118,22 @@ struct Operands {
         row = r * kRowBytes<DP> + 16 * swizzled<DP>(r, half);
         column = key * kRowBytes<DP> + 16 * swizzled<DP>(key, d / 8) + 2 * (d & 7);
     }
-    // rows 32 block .. of the tile, k-step s
-    __device__ __forceinline__ u32x4 rows_of(const char* tile, int block, int s) const {
-        return *(const ORBIT_LDS u32x4*)(uintptr_t)(lds_address(tile) + block * 32 * kRowBytes<DP> + (row ^ 32 * s));
+    // The same of tiles that lie `bytes` further in LDS, a multiple of a row's: an address then is an exclusive or and a constant
+    __device__ __forceinline__ Operands further(uint32_t bytes) const {
+        Operands other = *this;
+        other.row += bytes;
+        other.column += bytes;
+        return other;
     }
+    // rows 32 block .. of the tile, k-step s
+    __device__ __forceinline__ u32x4 rows_of(uint32_t tile, int block, int s) const {
+        return *(const ORBIT_LDS u32x4*)(uintptr_t)(tile + block * 32 * kRowBytes<DP> + (row ^ 32 * s));
+    }
+    __device__ __forceinline__ u32x4 rows_of(const char* tile, int block, int s) const { return rows_of(lds_address(tile), block, s); }
     // columns 32 b .., rows 16 step .. of the tile, 8 a + 4 (l / 32) .. of them
-    __device__ __forceinline__ u32x4 columns_of(const char* tile, int step, int b) const {
-        const uint32_t at = lds_address(tile) + step * 16 * kRowBytes<DP>;
+    __device__ __forceinline__ u32x4 columns_of(const char* tile, int step, int b) const { return columns_of(lds_address(tile), step, b); }
+    __device__ __forceinline__ u32x4 columns_of(uint32_t tile, int step, int b) const {
+        const uint32_t at = tile + step * 16 * kRowBytes<DP>;
         auto four = [&](int a) {
             return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                                                  (ORBIT_LDS s16x4*)(uintptr_t)(at + 8 * kRowBytes<DP> * a + (column ^ (64 * b | 32 * a)))));

@@ -242,7 +242,8 @@ __global__ __launch_bounds__(256, 2) void attention_key_grad_kernel(AttnGradPara
                          : "memory");
     };
     if (begin < end) load(begin, 0);
-    Operands<DP> where(lane);
+    Operands<DP> where = Operands<DP>(lane).further(lds_address(key_lds));
+    const uint32_t stats_at = lds_address(key_lds) + 16 * (lane >> 5);
     const int key = t.first + 32 * wave + (lane & 31);
     const int64_t token = t.k_start + min(key, t.k_len - 1);
     u32x4 k[DP / 16], v[DP / 16];
@@ -263,21 +264,22 @@ __global__ __launch_bounds__(256, 2) void attention_key_grad_kernel(AttnGradPara
         for (int buffer = 0; buffer < 2; ++buffer) {
             if (row >= end) break;
             if (row + 64 < end) load(row + 64, buffer ^ 1);
-            const char *const qt = key_lds + buffer * kBuffer, *const gt = qt + kTile;
+            const uint32_t qt = buffer * kBuffer, gt = qt + kTile;   // from key_lds
 #pragma unroll 1
             for (int n = 0; n < 2; ++n) {
                 f32x16 s, dp;
                 asm volatile("" : "+v"(where.row), "+v"(where.column));
+                const Operands<DP> rows32 = where.further(n * 32 * kRowBytes<DP>);
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
-                    const char* const from = gt + kTile + 4 * (32 * n + 8 * (i / 4) + 4 * (lane >> 5));
-                    s[i] = (*(const ORBIT_LDS f32x4*)from)[i % 4];
-                    dp[i] = (*(const ORBIT_LDS f32x4*)(from + 256))[i % 4];
+                    const uint32_t from = stats_at + 128 * n + gt + kTile + 32 * (i / 4);
+                    s[i] = (*(const ORBIT_LDS f32x4*)(uintptr_t)from)[i % 4];
+                    dp[i] = (*(const ORBIT_LDS f32x4*)(uintptr_t)(from + 256))[i % 4];
                 }
 #pragma unroll
                 for (int step = 0; step < DP / 16; ++step) {
-                    s = mfma32(where.rows_of(qt, n, step), k[step], s);
-                    dp = mfma32(where.rows_of(gt, n, step), v[step], dp);
+                    s = mfma32(rows32.rows_of(qt, 0, step), k[step], s);
+                    dp = mfma32(rows32.rows_of(gt, 0, step), v[step], dp);
                 }
 #pragma unroll
                 for (int i = 0; i < 16; ++i) {
@@ -299,8 +301,8 @@ __global__ __launch_bounds__(256, 2) void attention_key_grad_kernel(AttnGradPara
                     const u32x4 pb = as_operand(s, u), ds = as_operand(dp, u);
 #pragma unroll
                     for (int b = 0; b < DP / 32; ++b) {
-                        dv[b] = mfma32(where.columns_of(gt, 2 * n + u, b), pb, dv[b]);
-                        dk[b] = mfma32(where.columns_of(qt, 2 * n + u, b), ds, dk[b]);
+                        dv[b] = mfma32(rows32.columns_of(gt, u, b), pb, dv[b]);
+                        dk[b] = mfma32(rows32.columns_of(qt, u, b), ds, dk[b]);
                     }
                 }
             }
