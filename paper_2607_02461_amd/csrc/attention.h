@@ -8,8 +8,9 @@
 // column it needs, is read from LDS by ds_read_b64_tr_b16, which turns 4 rows x 16 columns for 16 lanes.
 //
 // DP: the head size, padded to a multiple of 32 (of the products' columns).  A tile of rows lies in LDS as it does in memory, 128 or
-// 256 bytes to a row, its 16-byte chunks in an order that differs from row to row (`swizzled`): both ways of reading find their rows in different banks.  Lanes load the chunks in that order
-// (global_load_lds: lane i's 16 bytes go to the wave's place + 16 i).
+// 256 bytes to a row, its 16-byte chunks in an order that differs from row to row (`swizzled`): both ways of reading find their
+// rows in different banks (no conflict is counted).  Lanes load the chunks in that order (global_load_lds: lane i's 16 bytes go to
+// the wave's place + 16 i).
 #pragma once
 
 #include <hip/hip_runtime.h>

@@ -7,7 +7,14 @@
 //
 // Bound by the matrix cores (4 D products and sums for each pair of a query and a key), with the exponentials beside them: 64
 // keys x 32 queries take a wave 1024 cycles of MFMA and about 750 of VALU at D = 128, which overlap between the waves of a SIMD.
-// Few queries are bound by HBM: each key and value is read once for each of its heads.
+// Beside that they read 32 KB of LDS, 1400 of the card's 2048 cycles for the two waves of a SIMD.  What 4608 tokens in 24 heads of
+// 128 (two sequences) reach, 1070 TFLOP/s of matrix products, is set by power: the matrix cores are busy 52% of the time at
+// 1.75 GHz, and the same call on zeros runs a third faster.  Few queries are bound by HBM: each key and value is read once for
+// each of its heads, 16 tokens over 4600 keys on average in 8 heads of 128 at 5.1 TB/s.
+//
+// Tried and not kept: 64 queries to a wave (its sums leave the registers, 520 TFLOP/s); three waves to a SIMD at D = 64 (spills,
+// 710); sums of rounded probabilities by dot products (3% faster, but o off by 2^-6 where one key has it all); workgroups that
+// take one tile after the other (435 us over 512 keys, 420 without); waves of different priorities (no difference).
 //
 // Rows: the queries of a group's heads lie together, row = token * group + head of the group, so that one tile of keys serves
 // all heads that share it, and a single token of grouped heads fills as much of a tile as there is.

@@ -18,6 +18,7 @@ namespace {
 constexpr int64_t kMaxTokens = INT32_MAX;
 constexpr int32_t kMaxHeads = 32767;
 constexpr int64_t kMaxGroups = ((int64_t)1 << 24) - 8;   // workgroups of 256 threads to a launch
+constexpr int64_t kMostParts = (int64_t)1 << 20;         // of divided tiles: a join has up to 2048 threads for each
 constexpr int64_t kMaxStride = (int64_t)1 << 24;         // elements from a token to the next: a tile's rows lie within 2^32 bytes
 
 struct Sequence {
@@ -69,7 +70,7 @@ void divide(std::vector<Work>& work, int64_t kv_heads, const Card& card, int64_t
             if (n > 1) parts += n;
             most = std::max(most, ceil_div(w.cost, n));
         }
-        if (count > (kMaxGroups - 8192) / kv_heads || parts * card.rows > kMaxTokens / 4) break;
+        if (count > (kMaxGroups - 8192) / kv_heads || parts > kMostParts / kv_heads) break;
         const double time = ends(count, most) + card.join + card.part * parts * kv_heads;
         if (time < best) best = time, part = size;
     }

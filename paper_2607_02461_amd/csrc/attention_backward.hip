@@ -6,8 +6,12 @@
 // keys, for dq; the other 128 keys and all of their rows, for dk and dv.  So every sum is one workgroup's, in a fixed order, and no
 // result is added up in memory; that costs 7 products of 2 D operations for each pair instead of the 5 that there are.
 //
-// Both are bound by the matrix cores: 3 and 4 products for each pair beside one exponential.  p and ds enter their products in
-// bf16, half a step of 2^-8 relative, as q, k, v and do have it; sums are fp32.
+// Both are bound by the matrix cores and the power that they take: 3 and 4 products for each pair beside one exponential.  At 2 x
+// 4429 tokens in 24 heads of 128 they run at 1050 and 1000 TFLOP/s of these products, busy 54% and 47% of the time.  p and ds enter
+// their products in bf16, half a step of 2^-8 relative, as q, k, v and do have it; sums are fp32.
+//
+// Tried and not kept: 64 keys to a wave of the second kernel (spills); the first kernel's scores of 64 keys before their
+// gradients, so that operands of neighbouring products are shared (spills 38 registers at D = 128, 2320 us for 1655).
 //
 // Rows are those of the forward pass: row = token * group + head of the group; dk and dv sum over a group's heads as over
 // tokens.
@@ -133,7 +137,7 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
                             dp[i] = hidden ? 0.f : dp[i];
                         }
                     }
-                    if (!last) {
+                    if (!kSums && !last) {
 #pragma unroll
                         for (int i = 0; i < 16; ++i) sum += exp2_fast(__builtin_fmaf(s[i], p.scale, lse2)) * dp[i];
                         continue;
@@ -160,7 +164,7 @@ __global__ __launch_bounds__(256, 2) void attention_row_grad_kernel(AttnGradPara
                 key += 64;
             }
         }
-        if (last) break;
+        if (kSums || last) break;
         delta = -(sum + other_half(sum));
         if (t.begin < t.end) load(t.begin, 0);
     }

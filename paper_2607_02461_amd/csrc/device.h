@@ -312,7 +312,6 @@ struct NormParams {
     int joined;            // rows of one group are those of several batches, whose strides differ
     int64_t rows, L;       // rows of a group; rows of a batch
     float eps;
-    int stream;            // rows are loaded and stored non-temporally
     float *dw, *db;        // fp32 [group][N] or null
     float* part;           // [group][parts][2][N], the workgroups' sums
     int parts;

@@ -5,7 +5,8 @@
 // and, with h = dy g,
 //     dx = r (h - mean(h) - n mean(h n)),   dg = sum over rows of dy n,   db = sum over rows of dy.
 // All of it streams its rows once and is bound by HBM: (size of x + size of y) N bytes a row forward, (2 size of x + size
-// of dy) N backward.
+// of dy) N backward: 32760 x 5120 in fp32, results and their gradients in bf16, 194 us (5.2 TB/s) and 295 us (5.7 TB/s), where a
+// copy of 4 GiB runs at 4.75 TB/s.  (Non-temporal loads and stores: no difference from 50 MB to 1.7 GB.)
 //
 // A workgroup walks rows of one batch and keeps in registers what they share: its columns' gains and offsets, or its gains and
 // the two gradients' sums.  (Read again for each row, a batch's fp32 scale and shift are twice the traffic of its bf16
@@ -43,29 +44,17 @@ struct Piece;
 template <>
 struct Piece<bf16_t> {
     u32x2 r;
-    __device__ __forceinline__ void load(const bf16_t* p, bool nt) { r = nt ? __builtin_nontemporal_load((const u32x2_any*)p) : *(const u32x2_any*)p; }
+    __device__ __forceinline__ void load(const bf16_t* p) { r = *(const u32x2_any*)p; }
     __device__ __forceinline__ void get(float* v) const { v[0] = bf16_low(r.x), v[1] = bf16_high(r.x), v[2] = bf16_low(r.y), v[3] = bf16_high(r.y); }
-    static __device__ __forceinline__ void store(bf16_t* p, const float* v, bool nt) {
-        const u32x2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-        if (nt)
-            __builtin_nontemporal_store(w, (u32x2_any*)p);
-        else
-            *(u32x2_any*)p = w;
-    }
+    static __device__ __forceinline__ void store(bf16_t* p, const float* v) { *(u32x2_any*)p = (u32x2){pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}; }
 };
 
 template <>
 struct Piece<float> {
     f32x4 r;
-    __device__ __forceinline__ void load(const float* p, bool nt) { r = nt ? __builtin_nontemporal_load((const f32x4_any*)p) : *(const f32x4_any*)p; }
+    __device__ __forceinline__ void load(const float* p) { r = *(const f32x4_any*)p; }
     __device__ __forceinline__ void get(float* v) const { v[0] = r.x, v[1] = r.y, v[2] = r.z, v[3] = r.w; }
-    static __device__ __forceinline__ void store(float* p, const float* v, bool nt) {
-        const f32x4 w = {v[0], v[1], v[2], v[3]};
-        if (nt)
-            __builtin_nontemporal_store(w, (f32x4_any*)p);
-        else
-            *(f32x4_any*)p = w;
-    }
+    static __device__ __forceinline__ void store(float* p, const float* v) { *(f32x4_any*)p = (f32x4){v[0], v[1], v[2], v[3]}; }
 };
 
 __device__ __forceinline__ float value(const bf16_t* p) { return __uint_as_float((uint32_t)p->bits << 16); }
@@ -73,44 +62,42 @@ __device__ __forceinline__ float value(const float* p) { return *p; }
 __device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = (uint16_t)pack_bf16(v, 0.f); }
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 
-// How rows are accessed: as they come, non-temporally, or with a piece that the row's end cuts.
-enum Access { kPlain, kStream, kCut };
-
-// A thread's part of a row: C pieces of kPiece values, blockDim.x pieces apart.  The piece that the row's end cuts begins further left, so
-// that it is a whole one: its first `skip` values are its neighbour's and stay out of sums.  (Value by value, one after the other
+// A thread's part of a row: C pieces of kPiece values, blockDim.x pieces apart.  With CUT (N is no multiple of kPiece) the piece
+// that the row's end cuts begins further left, so that it is a whole one: its first `skip` values are its neighbour's and stay out
+// of sums.  (Value by value, one after the other
 // and with a branch each, such a piece held up the whole wave: a backward pass of 32760 x 5120 370 us for 230, whose last
 // pieces were idle and not even cut.)  A row of less than a piece is one thread's, value by value.
-template <int C, Access A>
+template <int C, bool CUT>
 struct Columns {
     int at[C];     // first column
     int skip[C];
     bool have[C];
     int small;     // values of a row of less than a piece, or 0
     __device__ __forceinline__ Columns(int N) {
-        small = A == kCut && N < kPiece ? N : 0;
+        small = CUT && N < kPiece ? N : 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             at[c] = (c * (int)blockDim.x + (int)threadIdx.x) * kPiece;
             have[c] = at[c] < N;
             skip[c] = 0;
-            if (A == kCut && have[c] && at[c] + kPiece > N && !small) skip[c] = at[c] + kPiece - N, at[c] = N - kPiece;
+            if (CUT && have[c] && at[c] + kPiece > N && !small) skip[c] = at[c] + kPiece - N, at[c] = N - kPiece;
         }
     }
     // whether value i of piece c is this thread's own
-    __device__ __forceinline__ bool own(int c, int i) const { return A != kCut ? have[c] : small ? have[c] && i < small : have[c] && i >= skip[c]; }
+    __device__ __forceinline__ bool own(int c, int i) const { return !CUT ? have[c] : small ? have[c] && i < small : have[c] && i >= skip[c]; }
 };
 
 // Pieces on their way from memory, and their values; values that the row does not have are zeros.
-template <typename T, int C, Access A>
+template <typename T, int C, bool CUT>
 struct Part {
     Piece<T> piece[C];
-    __device__ __forceinline__ void load(const T* row, const Columns<C, A>& k) {
+    __device__ __forceinline__ void load(const T* row, const Columns<C, CUT>& k) {
         if (k.small) return;
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (k.have[c]) piece[c].load(row + k.at[c], A == kStream);
+            if (k.have[c]) piece[c].load(row + k.at[c]);
     }
-    __device__ __forceinline__ void get(const T* row, const Columns<C, A>& k, float (&v)[C][kPiece]) const {
+    __device__ __forceinline__ void get(const T* row, const Columns<C, CUT>& k, float (&v)[C][kPiece]) const {
         if (k.small) {
 #pragma unroll
             for (int c = 0; c < C; ++c)
@@ -128,7 +115,7 @@ struct Part {
             }
         }
     }
-    static __device__ __forceinline__ void store(T* row, const Columns<C, A>& k, const float (&v)[C][kPiece]) {
+    static __device__ __forceinline__ void store(T* row, const Columns<C, CUT>& k, const float (&v)[C][kPiece]) {
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             if (k.small) {
@@ -136,19 +123,19 @@ struct Part {
                 for (int i = 0; i < kPiece; ++i)
                     if (k.own(c, i)) put(row + i, v[c][i]);
             } else if (k.have[c]) {
-                Piece<T>::store(row + k.at[c], v[c], A == kStream);
+                Piece<T>::store(row + k.at[c], v[c]);
             }
         }
     }
 };
 
 // A batch's weights of the thread's columns, `none` where there are none, and `add` to them where there are
-template <typename T, int C, Access A>
-__device__ __forceinline__ void load_weights(const T* w, float add, const Columns<C, A>& k, float (&v)[C][kPiece]) {
+template <typename T, int C, bool CUT>
+__device__ __forceinline__ void load_weights(const T* w, float add, const Columns<C, CUT>& k, float (&v)[C][kPiece]) {
     Piece<T> piece[C];
 #pragma unroll
     for (int c = 0; c < C; ++c)
-        if (k.have[c] && !k.small) piece[c].load(w + k.at[c], false);
+        if (k.have[c] && !k.small) piece[c].load(w + k.at[c]);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
 #pragma unroll
@@ -159,17 +146,17 @@ __device__ __forceinline__ void load_weights(const T* w, float add, const Column
     }
 }
 
-template <int C, Access A>
-__device__ __forceinline__ void load_weights(const void* w, bool f32, int64_t first, float none, float add, const Columns<C, A>& k, float (&v)[C][kPiece]) {
+template <int C, bool CUT>
+__device__ __forceinline__ void load_weights(const void* w, bool f32, int64_t first, float none, float add, const Columns<C, CUT>& k, float (&v)[C][kPiece]) {
     if (!w) {
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) v[c][i] = none;
     } else if (f32) {
-        load_weights<float, C, A>((const float*)w + first, add, k, v);
+        load_weights<float, C, CUT>((const float*)w + first, add, k, v);
     } else {
-        load_weights<bf16_t, C, A>((const bf16_t*)w + first, add, k, v);
+        load_weights<bf16_t, C, CUT>((const bf16_t*)w + first, add, k, v);
     }
 }
 
@@ -200,13 +187,13 @@ __device__ __forceinline__ int wave_values(int w, int N) {
 }
 
 // A wave's mean, the deviations from it in v's place and their sum of squares
-template <int C, Access A>
-__device__ __forceinline__ void wave_statistics(float (&v)[C][kPiece], const Columns<C, A>& k, float n, float* mean, float* squares) {
+template <int C, bool CUT>
+__device__ __forceinline__ void wave_statistics(float (&v)[C][kPiece], const Columns<C, CUT>& k, float n, float* mean, float* squares) {
     float sum = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-        for (int i = 0; i < kPiece; ++i) sum += A != kCut || k.own(c, i) ? v[c][i] : 0.f;
+        for (int i = 0; i < kPiece; ++i) sum += !CUT || k.own(c, i) ? v[c][i] : 0.f;
     *mean = n ? wave_sum(sum) / n : 0.f;   // a quotient: a row of equal values has that value for a mean
     float sq = 0.f;
 #pragma unroll
@@ -248,12 +235,12 @@ __device__ __forceinline__ T* row_of(const NormRows& t, int64_t b, int64_t l) {
 }
 
 // Workgroup p of group g: rows p, p + parts, ... of the group, which is a batch, or all batches' rows where they share their weights
-template <typename TX, typename TY, int C, Access A>
+template <typename TX, typename TY, int C, bool CUT>
 __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormParams p) {
     __shared__ float part[2][kMostWaves][2];
     __shared__ float count[kMostWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const Columns<C, A> k(p.N);
+    const Columns<C, CUT> k(p.N);
     const int n = wave_values<C>(wave, p.N);
     const float inv_N = 1.f / p.N;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
@@ -264,11 +251,11 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormPara
         else l = row;
     };
     locate();
-    Part<TX, C, A> next;
+    Part<TX, C, CUT> next;
     next.load(row_of<const TX>(p.x, b, l), k);
     float gain[C][kPiece], offset[C][kPiece];
-    load_weights<C, A>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
-    load_weights<C, A>(p.b, p.w_f32, g * p.b_batch, 0.f, 0.f, k, offset);
+    load_weights<C, CUT>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
+    load_weights<C, CUT>(p.b, p.w_f32, g * p.b_batch, 0.f, 0.f, k, offset);
     for (int turn = 0; row < p.rows; turn ^= 1) {
         float v[C][kPiece];
         next.get(row_of<const TX>(p.x, b, l), k, v);
@@ -279,7 +266,7 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormPara
             next.load(row_of<const TX>(p.x, b, l), k);
         }
         float mean, squares;
-        wave_statistics<C, A>(v, k, n, &mean, &squares);
+        wave_statistics<C, CUT>(v, k, n, &mean, &squares);
         if ((threadIdx.x & 63) == 0) part[turn][wave][0] = mean, part[turn][wave][1] = squares;
         __syncthreads();
         const Joined j = join<2>(part[turn], count, waves, wave, p.N);
@@ -288,16 +275,16 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormPara
         for (int c = 0; c < C; ++c)
 #pragma unroll
             for (int i = 0; i < kPiece; ++i) v[c][i] = (v[c][i] + j.shift) * r * gain[c][i] + offset[c][i];
-        Part<TY, C, A>::store(y, k, v);
+        Part<TY, C, CUT>::store(y, k, v);
     }
 }
 
-template <typename TX, typename TG, int C, Access A>
+template <typename TX, typename TG, int C, bool CUT>
 __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel(NormParams p) {
     __shared__ float part[2][kMostWaves][4];
     __shared__ float count[kMostWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
-    const Columns<C, A> k(p.N);
+    const Columns<C, CUT> k(p.N);
     const int n = wave_values<C>(wave, p.N);
     const float inv_N = 1.f / p.N;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
@@ -307,15 +294,15 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel
         if (p.joined) b = row / p.L, l = row - b * p.L;   // only of batches that do not follow each other row by row
         else l = row;
     };
-    Part<TX, C, A> next_x;
-    Part<TG, C, A> next_g;
+    Part<TX, C, CUT> next_x;
+    Part<TG, C, CUT> next_g;
     if (row < p.rows) {
         locate();
         next_x.load(row_of<const TX>(p.x, b, l), k);
         next_g.load(row_of<const TG>(p.g, b, l), k);
     }
     float gain[C][kPiece], dw[C][kPiece], db[C][kPiece];
-    load_weights<C, A>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
+    load_weights<C, CUT>(p.w, p.w_f32, g * p.w_batch, 1.f, p.modulate ? 1.f : 0.f, k, gain);
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -332,7 +319,7 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel
             next_g.load(row_of<const TG>(p.g, b, l), k);
         }
         float mean, squares, sum = 0.f, dot = 0.f;
-        wave_statistics<C, A>(v, k, n, &mean, &squares);
+        wave_statistics<C, CUT>(v, k, n, &mean, &squares);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -360,7 +347,7 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel
                 dw[c][i] += h[c][i] * unit;
                 v[c][i] = r * (h[c][i] * gain[c][i] - mean_h - unit * mean_hn);
             }
-        Part<TX, C, A>::store(y, k, v);
+        Part<TX, C, CUT>::store(y, k, v);
     }
     // [group][workgroup][2][N]
     float* const out = p.part + (int64_t)blockIdx.x * 2 * p.N;
@@ -437,22 +424,22 @@ hipError_t with_pieces(int pieces, F f) {
     return hipGetLastError();
 }
 
-template <typename TX, typename TY, Access A>
+template <typename TX, typename TY, bool CUT>
 hipError_t launch_forward(NormParams p, int groups, int cus, hipStream_t stream) {
     const Shape s = shape(p.N, p.rows * groups, cus);
     return with_pieces(s.pieces, [&](auto c) {
         constexpr int C = decltype(c)::value;
-        const int64_t resident = p.rows * groups <= cus ? 1 : resident_blocks((const void*)layer_norm_kernel<TX, TY, C, A>, 64 * s.waves, 0);
+        const int64_t resident = p.rows * groups <= cus ? 1 : resident_blocks((const void*)layer_norm_kernel<TX, TY, C, CUT>, 64 * s.waves, 0);
         p.parts = (int)std::min<int64_t>(p.rows, (resident * cus + groups - 1) / groups);
-        layer_norm_kernel<TX, TY, C, A><<<(unsigned)(p.parts * groups), 64 * s.waves, 0, stream>>>(p);
+        layer_norm_kernel<TX, TY, C, CUT><<<(unsigned)(p.parts * groups), 64 * s.waves, 0, stream>>>(p);
     });
 }
 
-template <typename TX, typename TG, Access A>
+template <typename TX, typename TG, bool CUT>
 hipError_t launch_backward(const NormParams& p, int groups, int cus, hipStream_t stream) {
     const Shape s = shape(p.N, p.rows * groups, cus);
     const hipError_t e = with_pieces(s.pieces, [&](auto c) {
-        layer_norm_backward_kernel<TX, TG, decltype(c)::value, A><<<(unsigned)(p.parts * groups), 64 * s.waves, 0, stream>>>(p);
+        layer_norm_backward_kernel<TX, TG, decltype(c)::value, CUT><<<(unsigned)(p.parts * groups), 64 * s.waves, 0, stream>>>(p);
     });
     if (e != hipSuccess || (!p.dw && !p.db)) return e;
     layer_norm_sum_kernel<<<dim3((unsigned)((p.N + 31) / 32 * groups), 2), 1024, 0, stream>>>(p);
@@ -461,15 +448,14 @@ hipError_t launch_backward(const NormParams& p, int groups, int cus, hipStream_t
 
 template <typename TX, typename TO, bool BACK>
 hipError_t launch(const NormParams& p, int groups, int cus, hipStream_t stream) {
-    auto go = [&](auto access) {
-        constexpr Access A = decltype(access)::value;
+    auto go = [&](auto cut) {
+        constexpr bool CUT = decltype(cut)::value;
         if constexpr (BACK)
-            return launch_backward<TX, TO, A>(p, groups, cus, stream);
+            return launch_backward<TX, TO, CUT>(p, groups, cus, stream);
         else
-            return launch_forward<TX, TO, A>(p, groups, cus, stream);
+            return launch_forward<TX, TO, CUT>(p, groups, cus, stream);
     };
-    if (p.N % kPiece) return go(std::integral_constant<Access, kCut>());
-    return p.stream ? go(std::integral_constant<Access, kStream>()) : go(std::integral_constant<Access, kPlain>());
+    return p.N % kPiece ? go(std::true_type()) : go(std::false_type());
 }
 
 template <bool BACK>

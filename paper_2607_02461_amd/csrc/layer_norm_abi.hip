@@ -14,7 +14,6 @@ namespace {
 
 constexpr int64_t kMaxReach = (int64_t)1 << 46;         // elements from a tensor's first to its last row
 constexpr int64_t kMostThreads = (int64_t)UINT32_MAX;   // of a launch grid
-constexpr int64_t kStreamBytes = (int64_t)160 << 20;
 
 bool is_type(int32_t t) { return t == ORBIT_OUT_F32 || t == ORBIT_OUT_BF16; }
 int size_of(int32_t t) { return t == ORBIT_OUT_F32 ? 4 : 2; }
@@ -106,7 +105,6 @@ orbit_status layer_norm(const orbit_rows* x, const orbit_rows* y, int64_t B, int
     p.rows = rows_of(B, L, p.joined);
     p.L = L;
     p.eps = eps;
-    p.stream = B * L * N * (size_of(x->dtype) + size_of(y->dtype)) > kStreamBytes;
     const int groups = groups_of(B, p.joined);
     if (flat(p.x, B, L) && flat(p.y, B, L)) p.joined = 0;
     if ((int64_t)groups * 1024 > kMostThreads) return fail(ORBIT_EUNSUPPORTED, "%s: more than 2^22 - 1 batches with weights of their own", who);
@@ -163,7 +161,6 @@ orbit_status layer_norm_backward(const orbit_rows* dy, const orbit_rows* x, cons
     p.rows = rows_of(B, L, p.joined);
     p.L = L;
     p.eps = eps;
-    p.stream = B * L * N * (2 * size_of(x->dtype) + size_of(dy->dtype)) > kStreamBytes;
     p.dw = dweight;
     p.db = dbias;
     const int groups = groups_of(B, p.joined);
