@@ -14,7 +14,8 @@
 //
 // Tried and not kept: 64 queries to a wave (its sums leave the registers, 520 TFLOP/s); three waves to a SIMD at D = 64 (spills,
 // 710); sums of rounded probabilities by dot products (3% faster, but o off by 2^-6 where one key has it all); workgroups that
-// take one tile after the other (435 us over 512 keys, 420 without); waves of different priorities (no difference).
+// take one tile after the other, which was to hide a tile's begin (32760 tokens over 512 keys 435 us for 420; with the next tile's
+// first keys on their way during the last ones 439); waves of different priorities (no difference).
 //
 // Rows: the queries of a group's heads lie together, row = token * group + head of the group, so that one tile of keys serves
 // all heads that share it, and a single token of grouped heads fills as much of a tile as there is.
