@@ -12,8 +12,7 @@
 // 1.75 GHz, and the same call on zeros runs a third faster.  Few queries are bound by HBM: each key and value is read once for
 // each of its heads, 16 tokens over 4600 keys on average in 8 heads of 128 at 5.1 TB/s.
 //
-// Tried and not kept: 64 queries to a wave (its sums leave the registers, 520 TFLOP/s); three waves to a SIMD at D = 64 (spills,
-// 710); sums of rounded probabilities by dot products (3% faster, but o off by 2^-6 where one key has it all); workgroups that
+// Tried and not kept: 64 queries to a wave (its sums leave the registers, 520 TFLOP/s); sums of rounded probabilities by dot products (3% faster, but o off by 2^-6 where one key has it all); workgroups that
 // take one tile after the other, which was to hide a tile's begin (32760 tokens over 512 keys 435 us for 420; with the next tile's
 // first keys on their way during the last ones 439); waves of different priorities (no difference).
 //
@@ -74,7 +73,7 @@ struct Queries {
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        constexpr int kParts = 2 * NB * (DP / 32), kFirst = kParts < 8 ? kParts : 8;
+        constexpr int kParts = 2 * NB * (DP / 32), kFirst = DP <= 64 ? (kParts < 4 ? kParts : 4) : 8;
         u32x4 c[kParts];
 #pragma unroll
         for (int i = 0; i < kFirst; ++i) c[i] = at.columns_of(v, i / (DP / 32), i % (DP / 32));
@@ -149,9 +148,11 @@ __device__ __forceinline__ void finish(const AttnParams& p, const AttnTile& t, i
         p.lse[(int64_t)(t.q_start + token) * p.heads + head] = l == 0.f ? -__builtin_inff() : (mine.m + __builtin_log2f(l)) * kLn2;
 }
 
-// 32 rows to each wave; 64 keys at a time, shared, in two buffers.
+// 32 rows to each wave; 64 keys at a time, shared, in two buffers.  Heads of up to 64 values have three waves to a SIMD, for which
+// fewer of V's operands are read ahead: 2048 tokens in 16 heads over 4 of 64, 16 sequences, causal, 217 -> 195 us, whole 326 ->
+// 302; 8 of 4096 in 16 heads 630 -> 593.
 template <int DP, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void attention_kernel(AttnParams p) {
+__global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void attention_kernel(AttnParams p) {
     __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * kRowBytes<DP>];
     const Place place = place_of(blockIdx.x, p.kv_heads, p.count);
     if (place.tile >= p.count) return;

@@ -11,7 +11,8 @@
 // their products in bf16, half a step of 2^-8 relative, as q, k, v and do have it; sums are fp32.
 //
 // Tried and not kept: 64 keys to a wave of the second kernel (spills); the first kernel's scores of 64 keys before their
-// gradients, so that operands of neighbouring products are shared (spills 38 registers at D = 128, 2320 us for 1655).
+// gradients, so that operands of neighbouring products are shared (spills 38 registers at D = 128, 2320 us for 1655); three
+// waves to a SIMD for the first kernel at D = 64 (spills 22, 1480 us for 1320).
 //
 // Rows are those of the forward pass: row = token * group + head of the group; dk and dv sum over a group's heads as over
 // tokens.
