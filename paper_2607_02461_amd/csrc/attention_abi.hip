@@ -45,8 +45,8 @@ struct Card {
 
 // Divides tiles along the other side where that is estimated to end earlier: where few long tiles leave the card partly idle.  Parts
 // leave their sums in rows of their own, which a join adds up.  A list ends after as many rounds of its longest tile as there are,
-// or after what each slot has and most of one, whichever is earlier.  The longest come first: workgroups start in the list's order, so the last to
-// start are the shortest.
+// or after what each slot has and most of one, whichever is earlier.  The longest come first: workgroups start in the list's order,
+// so the last to start are the shortest.
 // Measured, us (D = 128, whole / in parts): forward 1024 tokens in 24 heads, causal, 22 / 30; in 4 heads, not causal, 21 / 17;
 // single tokens over 2000 keys in 8 key heads, 4 sequences, 19 / 12.
 // (Dividing the last, partial round of several as well, 1728 equal tiles on 512 slots for example, gained nothing, 502 and 504 us:

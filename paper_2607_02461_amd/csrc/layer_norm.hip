@@ -122,6 +122,11 @@ struct Part {
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i)
                     if (k.own(c, i)) put(row + i, v[c][i]);
+            } else if (CUT && k.skip[c]) {
+                // the neighbour's values are its own: another wave's mean and deviations round otherwise
+#pragma unroll
+                for (int i = 1; i < kPiece; ++i)
+                    if (i >= k.skip[c]) put(row + k.at[c] + i, v[c][i]);
             } else if (k.have[c]) {
                 Piece<T>::store(row + k.at[c], v[c]);
             }

@@ -128,6 +128,20 @@ def test_means_far_from_zero(N, dtype):
     _check(x, None, None, False, oq.layer_norm(x, out_dtype=F32), _rows(1, 5, N, F32, 7), oq.layer_norm_backward(_rows(1, 5, N, F32, 7), x))
 
 
+@pytest.mark.parametrize("N", [257, 1025, 1538, 2049])
+@pytest.mark.parametrize("rows", [8, 700])
+def test_last_values_alone_in_their_wave(N, rows):
+    # the row's last values, a piece that its end cuts, are another wave's than the values before them, and far from them: 10^6
+    # times their size.  Each wave writes its own values alone: the others', by deviations from its own mean, would be off by
+    # half an ulp of 10^6, up to N / 128 times the bar
+    x = _rows(1, rows, N, F32, 31)
+    x[..., N // 4 * 4:] = 1e6
+    dy = _rows(1, rows, N, F32, 32)
+    y, grads = oq.layer_norm(x), oq.layer_norm_backward(dy, x)
+    _check(x, None, None, False, y, dy, grads)
+    assert torch.equal(oq.layer_norm(x), y) and torch.equal(oq.layer_norm_backward(dy, x)[0], grads[0])
+
+
 def test_rows_without_variance_and_values_that_are_not_finite():
     x = _rows(1, 8, 300, F32, 8)
     x[0, 1], x[0, 2], x[0, 4, 7], x[0, 6, 299] = 0.0, 3.0, float("nan"), float("inf")
