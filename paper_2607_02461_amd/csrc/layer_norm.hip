@@ -63,28 +63,34 @@ __device__ __forceinline__ void put(bf16_t* p, float v) { p->bits = (uint16_t)pa
 __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 
 // A thread's part of a row: C pieces of kPiece values, blockDim.x pieces apart.  With CUT (N is no multiple of kPiece) the piece
-// that the row's end cuts begins further left, so that it is a whole one: its first `skip` values are its neighbour's and stay out
-// of sums.  (Value by value, one after the other
-// and with a branch each, such a piece held up the whole wave: a backward pass of 32760 x 5120 370 us for 230, whose last
-// pieces were idle and not even cut.)  A row of less than a piece is one thread's, value by value.
+// that the row's end cuts begins further left, so that it is a whole one: its first values are its neighbour's and stay out of
+// sums and stores.  (Value by value, one after the other and with a branch each, such a piece held up the whole wave: a backward
+// pass of 32760 x 5120 370 us for 230, whose last pieces were idle and not even cut.)  A row of less than a piece is one thread's, value
+// by value.
 template <int C, bool CUT>
 struct Columns {
     int at[C];     // first column
-    int skip[C];
-    bool have[C];
+    int cut;       // values of the last piece that are its neighbour's
+    bool within[C], last;   // whether the pieces are the row's, and the last one is
     int small;     // values of a row of less than a piece, or 0
     __device__ __forceinline__ Columns(int N) {
         small = CUT && N < kPiece ? N : 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             at[c] = (c * (int)blockDim.x + (int)threadIdx.x) * kPiece;
-            have[c] = at[c] < N;
-            skip[c] = 0;
-            if (CUT && have[c] && at[c] + kPiece > N && !small) skip[c] = at[c] + kPiece - N, at[c] = N - kPiece;
+            within[c] = at[c] < N;
         }
+        last = at[C - 1] < N;
+        cut = 0;
+        if (CUT && last && at[C - 1] + kPiece > N && !small) cut = at[C - 1] + kPiece - N, at[C - 1] = N - kPiece;
     }
     // whether value i of piece c is this thread's own
-    __device__ __forceinline__ bool own(int c, int i) const { return !CUT ? have[c] : small ? have[c] && i < small : have[c] && i >= skip[c]; }
+    __device__ __forceinline__ bool own(int c, int i) const { return have(c) && (!CUT || (C == 1 && small ? i < small : i >= skip(c))); }
+    // Only the last piece can lie behind the row (`shape` gives the fewest).  Said with CUT: 32760 x 5118 930 -> 297 us backward and
+    // 234 -> 197 forward in fp32.  Not without it, where a branch for each piece is faster: 32760 x 5120 294 us for 335 backward in
+    // fp32, with as many rows on their way as there are else with 8 waves, though 8858 x 3072 in bf16 20.4 for 19.0 forward.
+    __device__ __forceinline__ bool have(int c) const { return !CUT ? within[c] : c < C - 1 || last; }
+    __device__ __forceinline__ int skip(int c) const { return c < C - 1 ? 0 : cut; }
 };
 
 // Pieces on their way from memory, and their values; values that the row does not have are zeros.
@@ -95,7 +101,7 @@ struct Part {
         if (k.small) return;
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (k.have[c]) piece[c].load(row + k.at[c]);
+            if (k.have(c)) piece[c].load(row + k.at[c]);
     }
     __device__ __forceinline__ void get(const T* row, const Columns<C, CUT>& k, float (&v)[C][kPiece]) const {
         if (k.small) {
@@ -107,7 +113,7 @@ struct Part {
         }
 #pragma unroll
         for (int c = 0; c < C; ++c) {
-            if (k.have[c]) {
+            if (k.have(c)) {
                 piece[c].get(v[c]);
             } else {
 #pragma unroll
@@ -122,12 +128,12 @@ struct Part {
 #pragma unroll
                 for (int i = 0; i < kPiece; ++i)
                     if (k.own(c, i)) put(row + i, v[c][i]);
-            } else if (CUT && k.skip[c]) {
+            } else if (CUT && k.skip(c)) {
                 // the neighbour's values are its own: another wave's mean and deviations round otherwise
 #pragma unroll
                 for (int i = 1; i < kPiece; ++i)
-                    if (i >= k.skip[c]) put(row + k.at[c] + i, v[c][i]);
-            } else if (k.have[c]) {
+                    if (i >= k.skip(c)) put(row + k.at[c] + i, v[c][i]);
+            } else if (k.have(c)) {
                 Piece<T>::store(row + k.at[c], v[c]);
             }
         }
@@ -140,12 +146,12 @@ __device__ __forceinline__ void load_weights(const T* w, float add, const Column
     Piece<T> piece[C];
 #pragma unroll
     for (int c = 0; c < C; ++c)
-        if (k.have[c] && !k.small) piece[c].load(w + k.at[c]);
+        if (k.have(c) && !k.small) piece[c].load(w + k.at[c]);
 #pragma unroll
     for (int c = 0; c < C; ++c) {
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) v[c][i] = k.small && k.own(c, i) ? value(w + i) : 0.f;
-        if (k.have[c] && !k.small) piece[c].get(v[c]);
+        if (k.have(c) && !k.small) piece[c].get(v[c]);
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) v[c][i] += add;
     }
