@@ -12,9 +12,16 @@
 // the two gradients' sums.  (Read again for each row, a batch's fp32 scale and shift are twice the traffic of its bf16
 // rows, from L2.)  The next row's loads are on their way while a row is reduced.
 //
-// Statistics: each wave has the mean and the sum of squared deviations of its own part of the row, two sums in registers, and
-// parts are joined as by Chan, Golub and LeVeque: sum of squares = sum_w (M2_w + n_w (m_w - m)^2).  No difference of large
-// squares is taken, and a row costs one barrier.  sum h (x - m) is joined the same way, from sum_w h and sum_w h (x - m_w).
+// Statistics: each wave has the mean and the sum of squared deviations of its own part of the row, and parts are joined as by
+// Chan, Golub and LeVeque: sum of squares = sum_w (M2_w + n_w (m_w - m)^2).  No difference of large squares is taken, and a
+// row costs one barrier.  sum h (x - m) is joined the same way, from sum_w h and sum_w h (x - m_w).
+//
+// A mean in fp32 is off by some steps of its last place, which a row that varies by no more than that shows whole: 5120 values of
+// 3333.3 came out up to 0.9 from 0 at eps = 1e-6.  So a wave's mean is that quotient m' and the mean of the deviations from it,
+// which is as small as they are, and waves' means meet as differences from the first one's.  Of bf16 values within a factor of 4
+// sums of up to kNormMaxWidth < 2^14 are exact (10 bits above their last place), so one fma finds that mean: sum - n m'.  Of fp32
+// values it is a sum of its own: 33272 x 5120 198.0 -> 199.3 us forward, 32760 x 5120 296 -> 296.5 backward, of bf16 values 8858 x
+// 3072 20.4 -> 21.0 and 39.4 -> 39.6.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -64,7 +71,8 @@ __device__ __forceinline__ void put(float* p, float v) { *p = v; }
 
 // A thread's part of a row: C pieces of kPiece values, blockDim.x pieces apart.  With CUT (N is no multiple of kPiece) the piece
 // that the row's end cuts begins further left, so that it is a whole one: its first values are its neighbour's and stay out of
-// sums and stores.  (Value by value, one after the other and with a branch each, such a piece held up the whole wave: a backward
+// sums and stores; threads behind the end load it too, so that no branch holds up the next row's loads (32760 x 5118 344 -> 312 us
+// backward in fp32).  (Value by value, one after the other and with a branch each, such a piece held up the whole wave: a backward
 // pass of 32760 x 5120 370 us for 230, whose last pieces were idle and not even cut.)  A row of less than a piece is one thread's, value
 // by value.
 template <int C, bool CUT>
@@ -74,7 +82,7 @@ struct Columns {
     bool within[C], last;   // whether the pieces are the row's, and the last one is
     int small;     // values of a row of less than a piece, or 0
     __device__ __forceinline__ Columns(int N) {
-        small = CUT && N < kPiece ? N : 0;
+        small = CUT && C == 1 && N < kPiece ? N : 0;
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             at[c] = (c * (int)blockDim.x + (int)threadIdx.x) * kPiece;
@@ -82,7 +90,7 @@ struct Columns {
         }
         last = at[C - 1] < N;
         cut = 0;
-        if (CUT && last && at[C - 1] + kPiece > N && !small) cut = at[C - 1] + kPiece - N, at[C - 1] = N - kPiece;
+        if (CUT && at[C - 1] + kPiece > N && !small) cut = last ? at[C - 1] + kPiece - N : 0, at[C - 1] = N - kPiece;
     }
     // whether value i of piece c is this thread's own
     __device__ __forceinline__ bool own(int c, int i) const { return have(c) && (!CUT || (C == 1 && small ? i < small : i >= skip(c))); }
@@ -101,7 +109,7 @@ struct Part {
         if (k.small) return;
 #pragma unroll
         for (int c = 0; c < C; ++c)
-            if (k.have(c)) piece[c].load(row + k.at[c]);
+            if (CUT || k.have(c)) piece[c].load(row + k.at[c]);
     }
     __device__ __forceinline__ void get(const T* row, const Columns<C, CUT>& k, float (&v)[C][kPiece]) const {
         if (k.small) {
@@ -197,21 +205,30 @@ __device__ __forceinline__ int wave_values(int w, int N) {
     return n;
 }
 
-// A wave's mean, the deviations from it in v's place and their sum of squares
-template <int C, bool CUT>
-__device__ __forceinline__ void wave_statistics(float (&v)[C][kPiece], const Columns<C, CUT>& k, float n, float* mean, float* squares) {
-    float sum = 0.f;
+// A wave's mean, as a quotient and the rest of it, the deviations from both in v's place and their sum of squares
+template <typename T, int C, bool CUT>
+__device__ __forceinline__ void wave_statistics(float (&v)[C][kPiece], const Columns<C, CUT>& k, float n, float inv_n, float* mean, float* rest, float* squares) {
+    constexpr bool kExact = std::is_same<T, bf16_t>::value;
+    float sum = 0.f, left = 0.f, sq = 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) sum += !CUT || k.own(c, i) ? v[c][i] : 0.f;
-    *mean = n ? wave_sum(sum) / n : 0.f;   // a quotient: a row of equal values has that value for a mean
-    float sq = 0.f;
+    sum = wave_sum(sum);
+    *mean = n ? sum / n : 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
         for (int i = 0; i < kPiece; ++i) {
             v[c][i] -= *mean;
+            if (!kExact) left += k.own(c, i) ? v[c][i] : 0.f;
+        }
+    *rest = (kExact ? __builtin_fmaf(-n, *mean, sum) : wave_sum(left)) * inv_n;
+#pragma unroll
+    for (int c = 0; c < C; ++c)
+#pragma unroll
+        for (int i = 0; i < kPiece; ++i) {
+            v[c][i] -= *rest;
             sq += k.own(c, i) ? v[c][i] * v[c][i] : 0.f;
         }
     *squares = wave_sum(sq);
@@ -222,17 +239,18 @@ struct Joined {
     float squares, sum, dot;
 };
 
-// What the waves found of a row, joined.  part[w]: n_w times its mean, squares, and backward sum h and sum h (x - m_w).
+// What the waves found of a row, joined.  part[w]: its mean and the rest of it, squares, and backward sum h and sum h (x - m_w).
 template <int Q>
-__device__ __forceinline__ Joined join(const float (*part)[Q], const float* count, int waves, int wave, float N) {
+__device__ __forceinline__ Joined join(const float (*part)[Q], const float* count, int waves, int wave, float inv_N) {
+    const float first = part[0][0];
     float total = 0.f;
-    for (int w = 0; w < waves; ++w) total += part[w][0] * count[w];
-    const float mean = total / N;
-    Joined j{part[wave][0] - mean, 0.f, 0.f, 0.f};
+    for (int w = 0; w < waves; ++w) total += (part[w][0] - first + part[w][1]) * count[w];
+    const float mean = total * inv_N;   // from `first`
+    Joined j{part[wave][0] - first + part[wave][1] - mean, 0.f, 0.f, 0.f};
     for (int w = 0; w < waves; ++w) {
-        const float d = part[w][0] - mean;
-        j.squares += part[w][1] + count[w] * d * d;
-        if (Q == 4) {
+        const float d = part[w][0] - first + part[w][1] - mean;
+        j.squares += part[w][2] + count[w] * d * d;
+        if (Q == 5) {
             j.sum += part[w][Q - 2];
             j.dot += part[w][Q - 1] + d * part[w][Q - 2];
         }
@@ -248,12 +266,12 @@ __device__ __forceinline__ T* row_of(const NormRows& t, int64_t b, int64_t l) {
 // Workgroup p of group g: rows p, p + parts, ... of the group, which is a batch, or all batches' rows where they share their weights
 template <typename TX, typename TY, int C, bool CUT>
 __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormParams p) {
-    __shared__ float part[2][kMostWaves][2];
+    __shared__ float part[2][kMostWaves][3];
     __shared__ float count[kMostWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const Columns<C, CUT> k(p.N);
     const int n = wave_values<C>(wave, p.N);
-    const float inv_N = 1.f / p.N;
+    const float inv_N = 1.f / p.N, inv_n = n ? 1.f / n : 0.f;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
     const int64_t g = blockIdx.x / (uint32_t)p.parts;
     int64_t row = blockIdx.x % (uint32_t)p.parts, b = g, l = row;
@@ -276,11 +294,11 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormPara
             locate();
             next.load(row_of<const TX>(p.x, b, l), k);
         }
-        float mean, squares;
-        wave_statistics<C, CUT>(v, k, n, &mean, &squares);
-        if ((threadIdx.x & 63) == 0) part[turn][wave][0] = mean, part[turn][wave][1] = squares;
+        float mean, rest, squares;
+        wave_statistics<TX, C, CUT>(v, k, n, inv_n, &mean, &rest, &squares);
+        if ((threadIdx.x & 63) == 0) part[turn][wave][0] = mean, part[turn][wave][1] = rest, part[turn][wave][2] = squares;
         __syncthreads();
-        const Joined j = join<2>(part[turn], count, waves, wave, p.N);
+        const Joined j = join<3>(part[turn], count, waves, wave, inv_N);
         const float r = rsqrtf(j.squares * inv_N + p.eps);
 #pragma unroll
         for (int c = 0; c < C; ++c)
@@ -292,12 +310,12 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_kernel(NormPara
 
 template <typename TX, typename TG, int C, bool CUT>
 __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel(NormParams p) {
-    __shared__ float part[2][kMostWaves][4];
+    __shared__ float part[2][kMostWaves][5];
     __shared__ float count[kMostWaves];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const Columns<C, CUT> k(p.N);
     const int n = wave_values<C>(wave, p.N);
-    const float inv_N = 1.f / p.N;
+    const float inv_N = 1.f / p.N, inv_n = n ? 1.f / n : 0.f;
     if ((threadIdx.x & 63) == 0) count[wave] = n;
     const int64_t g = blockIdx.x / (uint32_t)p.parts;
     int64_t row = blockIdx.x % (uint32_t)p.parts, b = g, l = row;
@@ -329,8 +347,8 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel
             next_x.load(row_of<const TX>(p.x, b, l), k);
             next_g.load(row_of<const TG>(p.g, b, l), k);
         }
-        float mean, squares, sum = 0.f, dot = 0.f;
-        wave_statistics<C, CUT>(v, k, n, &mean, &squares);
+        float mean, rest, squares, sum = 0.f, dot = 0.f;
+        wave_statistics<TX, C, CUT>(v, k, n, inv_n, &mean, &rest, &squares);
 #pragma unroll
         for (int c = 0; c < C; ++c)
 #pragma unroll
@@ -342,11 +360,11 @@ __global__ __launch_bounds__(C > 2 ? 512 : 1024) void layer_norm_backward_kernel
         sum = wave_sum(sum);
         dot = wave_sum(dot);
         if ((threadIdx.x & 63) == 0) {
-            part[turn][wave][0] = mean, part[turn][wave][1] = squares;
-            part[turn][wave][2] = sum, part[turn][wave][3] = dot;
+            part[turn][wave][0] = mean, part[turn][wave][1] = rest, part[turn][wave][2] = squares;
+            part[turn][wave][3] = sum, part[turn][wave][4] = dot;
         }
         __syncthreads();
-        const Joined j = join<4>(part[turn], count, waves, wave, p.N);
+        const Joined j = join<5>(part[turn], count, waves, wave, inv_N);
         const float r = rsqrtf(j.squares * inv_N + p.eps);
         const float mean_h = j.sum * inv_N, mean_hn = r * (j.dot * inv_N);
 #pragma unroll

@@ -142,6 +142,42 @@ def test_last_values_alone_in_their_wave(N, rows):
     assert torch.equal(oq.layer_norm(x), y) and torch.equal(oq.layer_norm_backward(dy, x)[0], grads[0])
 
 
+@pytest.mark.parametrize("N", [300, 1999, 5120, 12288])
+@pytest.mark.parametrize("rows", [3, 700])
+@pytest.mark.parametrize("dtype,spread", [(F32, 0.0), (F32, 1e-3), (BF16, None)])
+def test_rows_that_vary_by_less_than_their_means_rounding(N, rows, dtype, spread):
+    """A wave's mean is a quotient off by at most 40 u |x| and the mean of the deviations from it, which are exact (values within
+    a factor of two of the quotient) and themselves up to 40 u |x| beside a row's own; their mean is off by 41 u of that.  The waves'
+    means meet as differences of up to 80 u |x|, off by (16 + 4) u of what is summed, and the row's by as much: D = 2^13 u^2 |x| in
+    all.  A unit is off by r D, and by 64 u of itself: r, whose squares are of deviations."""
+    g = torch.Generator().manual_seed(41)
+    place = torch.linspace(1000.1, 3333.3, rows)[:, None]
+    if spread is None:                            # one value a few of its steps from the others
+        x = place.expand(rows, N).clone()
+        x[:, N // 3] *= 1.03125
+    else:
+        x = place + spread * torch.randn((rows, N), generator=g)
+    x = x.to(dtype)[None].to(DEV)
+    (w, b), dy = _weights(1, N, F32, 42, False), _rows(1, rows, N, F32, 43)
+    y, (dx, dw, db) = oq.layer_norm(x, w, b, out_dtype=F32), oq.layer_norm_backward(dy, x, w)
+    x64, dy64, gain, shift = _f64(x), _f64(dy), _f64(w), _f64(b)
+    x64 = x64 - x64[..., :1]                      # exact: the same deviations, without the oracle's own rounding of the mean
+    r = 1 / np.sqrt(x64.var(-1, keepdims=True) + EPS)
+    off = r * 2.0 ** 13 * U * U * 3400.0
+    unit = r * np.abs(x64 - x64.mean(-1, keepdims=True))
+    ref = oracle.layer_norm(x64, gain, shift, EPS)
+    _within("y", y, ref, U * np.abs(ref) + (64 * U * unit + off) * np.abs(gain) + 2 * U * np.abs(shift))
+    want, gains, shifts = oracle.layer_norm_backward(dy64, x64, gain, EPS)
+    h = np.abs(dy64 * gain)
+    most = unit + off
+    mean_hn = (h * most).mean(-1, keepdims=True)
+    size = r * (64 * U * (h + h.mean(-1, keepdims=True) + 2 * most * mean_hn) + off * (mean_hn + most * h.mean(-1, keepdims=True)))
+    _within("dx", dx, want, HALF[dtype] * np.abs(want) + size)
+    grow = (10 * rows ** 0.5 + 64) * U
+    _within("dw", dw, gains.sum((0, 1)), grow * (np.abs(dy64) * unit).sum((0, 1)) + 1.01 * (np.abs(dy64) * off).sum((0, 1)))
+    _within("db", db, shifts.sum((0, 1)), grow * np.abs(dy64).sum((0, 1)))
+
+
 def test_rows_without_variance_and_values_that_are_not_finite():
     x = _rows(1, 8, 300, F32, 8)
     x[0, 1], x[0, 2], x[0, 4, 7], x[0, 6, 299] = 0.0, 3.0, float("nan"), float("inf")
