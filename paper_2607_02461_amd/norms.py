@@ -47,9 +47,9 @@ def _rows(t, name, like=None, dtype=None):
 def _output(out, like, name, dtype):
     """(out, its rows): the caller's output, checked, or a new one of `like`'s shape."""
     if out is None:
-        out = torch.empty_like(like, dtype=dtype)      # dense, and its last dimension contiguous as like's is
-        if out.shape[-1] == 1:
-            out = out.contiguous()
+        out = torch.empty_like(like, dtype=dtype)      # in like's order of dimensions, for sliding windows in another one
+        if out.stride(-1) != 1:
+            out = torch.empty(like.shape, dtype=dtype, device=like.device)
         return out, _pack_rows(out.data_ptr(), out.stride(0) if out.dim() == 3 else 0, out.stride(-2), _TYPES[dtype])
     rows = _rows(out, name, like, dtype)[0]
     _rows_apart(out, name)

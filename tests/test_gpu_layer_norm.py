@@ -219,6 +219,17 @@ def test_in_place_broadcast_inputs_and_rows_beside_the_outputs(modulate):
     assert all(torch.equal(s, t) for s, t in zip(got, want))
 
 
+@pytest.mark.parametrize("rows,step", [(37, 1), (200, 1), (37, 3)])
+def test_rows_that_are_windows_of_a_signal(rows, step):
+    # windows of 64 values that lie `step` apart
+    signal = _rows(2, 1, (rows - 1) * step + 64, BF16, 51)[:, 0]
+    for x in (signal[0].unfold(0, 64, step), signal.unfold(1, 64, step)):
+        assert x.shape[-2:] == (rows, 64) and x.stride()[-2:] == (step, 1)
+        dy = _rows(1, rows, 64, BF16, 52)[0].expand(x.shape)
+        assert torch.equal(oq.layer_norm(x), oq.layer_norm(x.contiguous()))
+        assert all(torch.equal(a, b) for a, b in zip(oq.layer_norm_backward(dy, x), oq.layer_norm_backward(dy, x.contiguous())))
+
+
 def test_one_scale_for_each_token_of_many():
     # batches of one row each, more of them than a grid's second dimension holds
     B, N = 70000, 24

@@ -4,8 +4,10 @@ GPU work)."""
 import ctypes
 
 import pytest
+import torch
 
 import paper_2607_02461_amd as oq
+from paper_2607_02461_amd import norms
 
 
 class Heads(ctypes.Structure):   # orbit_heads of the C header
@@ -146,3 +148,19 @@ def test_layer_norm_validates_before_launch():
     n = ctypes.c_size_t(7)
     assert lib.layer_norm_backward_workspace_size(1, 1, 0, 0, ctypes.byref(n)) == 1 and n.value == 0
     assert lib.layer_norm_backward_workspace_size(1, 1, 8, 0, None) == 1
+
+
+@pytest.mark.parametrize("like", [
+    torch.zeros(100).unfold(0, 64, 1), torch.zeros(200).unfold(0, 64, 1), torch.zeros(3, 100).unfold(1, 64, 1), torch.zeros(100).unfold(0, 64, 3),
+    torch.zeros(1, 64).expand(5, 64), torch.zeros(2, 1, 64).expand(2, 7, 64), torch.zeros(7, 2, 64).transpose(0, 1), torch.zeros(2, 9, 1),
+    torch.zeros(9, 2, 1).transpose(0, 1), torch.zeros(64, 1).t(), torch.zeros(2, 9, 70)[..., 3:67], torch.zeros(0, 9, 64)])
+def test_new_outputs_of_layer_norms_are_rows(like):
+    # whatever order the input's dimensions have in memory: contiguous rows that do not overlap
+    assert like.stride(-1) == 1 or like.shape[-1] == 1
+    out, _ = norms._output(None, like, "out", torch.bfloat16)
+    assert out.shape == like.shape and out.dtype == torch.bfloat16 and out.stride(-1) == 1
+    reach = 0
+    for stride, size in sorted(zip(out.stride(), out.shape)):
+        if size > 1:
+            assert stride > reach
+            reach += stride * (size - 1)
