@@ -109,6 +109,14 @@ __device__ __forceinline__ void loads_done() {
     asm volatile("" ::: "memory");
 }
 
+// Waits for the wave's reads of LDS: a tile may be loaded over another that the wave alone has read (where waves share it, a
+// barrier does)
+__device__ __forceinline__ void reads_done() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+    asm volatile("" ::: "memory");
+}
+
 // Where a lane reads operands of a tile: rows of it (row l % 32 of 32, chunk l / 32 of each pair), and columns of it.  A chunk's
 // place is an exclusive or of its number and the row's, so the other places are one such operation from the first.
 template <int DP>

@@ -221,6 +221,7 @@ __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     const int all = seen_keys(p.causal, t.q_len, t.k_len, t.first / p.group);
     for (int buffer = 0; key < t.end; key += 128, buffer ^= 1) {
         if (key + 128 < t.end) {
+            reads_done();
             load(key + 128, buffer ^ 1);
             loads_done<kLoads>();
         } else {

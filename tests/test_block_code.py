@@ -1,6 +1,8 @@
 """What the compiler made of the kernels of the layer norms and of attention, read off the built library."""
 
 import re
+import subprocess
+import tempfile
 
 import pytest
 
@@ -31,3 +33,81 @@ def test_two_waves_fit_a_simd(kernels, name):
     for n, k in kernels.items():
         if re.search(rf"\d{name}I", n):
             assert k[".vgpr_count"] + k.get(".agpr_count", 0) <= 256, n
+
+
+def _code(names):
+    """{kernel: its instructions as (mnemonic, operands, place of the branch's target or None)} of kernels whose names match."""
+    out = {}
+    for elf in code_objects.code_objects():
+        with tempfile.NamedTemporaryFile(suffix=".elf") as f:
+            f.write(elf)
+            f.flush()
+            text = subprocess.run([code_objects.OBJDUMP, "-d", "--mcpu=gfx950", "--no-show-raw-insn", f.name], check=True, capture_output=True,
+                                  text=True).stdout
+        body = None
+        for line in text.splitlines():
+            label = re.match(r"([0-9a-f]+) <(\S+)>:", line)
+            if label:
+                body = out.setdefault(label[2], (int(label[1], 16), [])) if re.search(names, label[2]) else None
+            elif body and line.startswith("\t"):
+                code, _, rest = line.partition("//")
+                name, _, operands = code.strip().partition(" ")
+                if not rest:        # padding behind the code
+                    continue
+                target = re.search(r"<\S+?(?:\+0x([0-9a-f]+))?>", rest) if "branch" in name else None
+                body[1].append((int(rest.split(":")[0], 16) - body[0], name, operands.strip(), int(target[1] or "0", 16) if target else None))
+    return {n: _placed(code) for n, (_, code) in out.items()}
+
+
+def _placed(code):
+    """Addresses of branches' targets as places in the code."""
+    place = {at: i for i, (at, *_) in enumerate(code)}
+    return [(name, operands, None if to is None else place[to]) for _, name, operands, to in code]
+
+
+def _loads_beside_reads(code):
+    """The places of loads into LDS that a read of LDS may reach along some way without a wait for all of them between."""
+    found, seen, todo = set(), set(), [(0, False)]
+    while todo:
+        at, reads = todo.pop()
+        if (at, reads) in seen or at >= len(code):
+            continue
+        seen.add((at, reads))
+        name, operands, to = code[at]
+        if name.startswith("ds_read"):
+            reads = True
+        elif name == "s_waitcnt" and ("lgkmcnt(0)" in operands or operands.strip() == "0"):
+            reads = False
+        elif "load_lds" in name and reads:
+            found.add(at)
+        if to is not None:
+            todo.append((to, reads))
+        if name not in ("s_branch", "s_endpgm", "s_setpc_b64"):
+            todo.append((at + 1, reads))
+    return sorted(found)
+
+
+def test_loads_beside_reads_are_seen():
+    read, load, wait = ("ds_read_b128", "v[0:3], v4", None), ("global_load_lds_dwordx4", "v2, s[4:5]", None), ("s_waitcnt", "lgkmcnt(0)", None)
+    some, again, end = ("s_waitcnt", "vmcnt(0) lgkmcnt(3)", None), ("s_cbranch_vccnz", "65533", 0), ("s_endpgm", "", None)
+    assert _loads_beside_reads([load, read, wait, again, end]) == []
+    assert _loads_beside_reads([load, read, some, again, end]) == [0]      # round the loop
+    assert _loads_beside_reads([read, ("s_branch", "1", 3), wait, load, end]) == [3]
+    assert _loads_beside_reads([read, wait, load, end]) == [] and _loads_beside_reads([read, end, load]) == []
+
+
+def test_tiles_are_loaded_over_ones_that_have_been_read():
+    # a load into LDS begins when the reads before it have arrived: of the tile that it replaces, among them
+    kernels = _code(r"\d+attention_(few_|row_grad_|key_grad_)?kernelI")
+    assert len(kernels) == 20
+    for n, code in kernels.items():
+        assert any("load_lds" in i[0] for i in code) and any(i[0].startswith("ds_read") for i in code), n
+        assert _loads_beside_reads(code) == [], n
+
+
+def test_waits_for_reads_are_in_the_source():
+    # a wave of few rows refills a buffer that it alone has read, without a barrier
+    with open(code_objects.oq.__path__[0] + "/csrc/attention.hip") as f:
+        few = re.search(r"void attention_few_kernel.*?\n}\n", f.read(), re.S)[0]
+    loop = few[few.index("for (int buffer"):]
+    assert re.search(r"reads_done\(\);\s*load\(", loop) and loop.count(" load(") == 1
