@@ -63,7 +63,8 @@ __device__ __forceinline__ int swizzled(int row, int c) {
 // 400 cycles of a tile's 1024.)  Columns behind D are other columns of the row: the other operand has zeros there.
 //
 // The loads are inline asm because the compiler, which cannot tell the buffers apart, would wait for them before the next read of
-// LDS.  They have no output registers; loads_done() waits for them.
+// LDS.  They have no output registers; loads_done() waits for them.  m0 is not in their list of clobbers because the compiler reserves
+// it and warns of its name there; nothing else in these kernels may use it.
 template <int DP, int ROWS, int WAVES>
 struct TileLoads {
     static constexpr int kChunks = kRowBytes<DP> / 16, kEach = 64 / kChunks, kLoads = ROWS / kEach / WAVES;

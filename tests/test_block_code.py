@@ -111,3 +111,36 @@ def test_waits_for_reads_are_in_the_source():
         few = re.search(r"void attention_few_kernel.*?\n}\n", f.read(), re.S)[0]
     loop = few[few.index("for (int buffer"):]
     assert re.search(r"reads_done\(\);\s*load\(", loop) and loop.count(" load(") == 1
+
+
+def _strays_of_m0(code):
+    """The places where m0 is used otherwise than by a move to it, a wait state and the load into LDS that takes it."""
+    found = []
+    for at, (name, operands, _) in enumerate(code):
+        words = re.split(r"[ ,\[\]:]+", operands)
+        if "load_lds" in name:
+            before = [i[:2] for i in code[max(0, at - 2):at]]
+            ok = len(before) == 2 and before[0][0] == "s_mov_b32" and before[0][1].startswith("m0,") and before[1] == ("s_nop", "0")
+        elif name == "s_mov_b32" and words[0] == "m0":
+            ok = at + 2 < len(code) and "load_lds" in code[at + 2][0]
+        else:   # instructions that name it, or take it unsaid: moves indexed by it, messages
+            ok = "m0" not in words and not name.startswith(("v_movrel", "s_movrel", "s_sendmsg", "ds_gws", "ds_ordered"))
+        if not ok:
+            found.append(at)
+    return found
+
+
+def test_strays_of_m0_are_seen():
+    move, wait, load = ("s_mov_b32", "m0, s4", None), ("s_nop", "0", None), ("global_load_lds_dwordx4", "v2, s[4:5]", None)
+    assert _strays_of_m0([move, wait, load, move, wait, load]) == []
+    assert _strays_of_m0([move, wait, load, wait, load]) == [4] and _strays_of_m0([move, load]) == [0, 1]
+    assert _strays_of_m0([("v_readlane_b32", "s3, v1, m0", None)]) == [0] and _strays_of_m0([("v_movrels_b32_e32", "v1, v2", None)]) == [0]
+
+
+def test_loads_into_lds_have_m0_to_themselves():
+    # the inline assembly that writes m0 does not say so: the compiler reserves the register, warns of its name in a list of
+    # clobbers, and must keep nothing of its own in it across a load
+    kernels = _code(r"\d+attention_(few_|row_grad_|key_grad_)?kernelI")
+    assert len(kernels) == 20
+    for n, code in kernels.items():
+        assert any("load_lds" in i[0] for i in code) and _strays_of_m0(code) == [], n
