@@ -90,14 +90,14 @@ _workspace_bytes = {}
 def _workspace(B, L, N, per_batch, dev):
     """A workspace and its bytes, which the sizes and the device alone decide."""
     key = (B, L, N, per_batch, dev)
-    if key not in _workspace_bytes:
-        n = ctypes.c_size_t(0)
+    n = _workspace_bytes.get(key)      # read once: another thread may empty the list
+    if n is None:
+        size = ctypes.c_size_t(0)
         with torch.cuda.device(dev):
-            _check("layer_norm_backward_workspace_size", lib().layer_norm_backward_workspace_size(B, L, N, per_batch, ctypes.byref(n)))
+            _check("layer_norm_backward_workspace_size", lib().layer_norm_backward_workspace_size(B, L, N, per_batch, ctypes.byref(size)))
         if len(_workspace_bytes) > 1024:
             _workspace_bytes.clear()
-        _workspace_bytes[key] = n.value
-    n = _workspace_bytes[key]
+        n = _workspace_bytes[key] = size.value
     return torch.empty((max(n, 16),), dtype=torch.uint8, device=dev), n
 
 

@@ -1,7 +1,9 @@
 """Plans of attention on the host, and what the entry points of attention and of the layer norms refuse before any launch (no
 GPU work)."""
 
+import contextlib
 import ctypes
+import types
 
 import pytest
 import torch
@@ -164,3 +166,31 @@ def test_new_outputs_of_layer_norms_are_rows(like):
         if size > 1:
             assert stride > reach
             reach += stride * (size - 1)
+
+
+@pytest.mark.parametrize("known", [False, True])
+def test_workspace_sizes_survive_another_threads_clearing(monkeypatch, known):
+    # the list of known sizes is emptied when it is long; another thread may do so between any two steps of this one
+    class Emptied(dict):
+        def __contains__(self, key):
+            found = super().__contains__(key)
+            self.clear()
+            return found
+
+        def __setitem__(self, key, value):
+            super().__setitem__(key, value)
+            self.clear()
+
+    def size(B, L, N, per_batch, out):
+        out._obj.value = 48
+        return 0
+
+    cpu = torch.device("cpu")
+    sizes = Emptied()
+    if known:
+        dict.__setitem__(sizes, (1, 2, 3, 0, cpu), 48)
+    monkeypatch.setattr(norms, "_workspace_bytes", sizes)
+    monkeypatch.setattr(norms, "lib", lambda: types.SimpleNamespace(layer_norm_backward_workspace_size=size))
+    monkeypatch.setattr(torch.cuda, "device", lambda dev: contextlib.nullcontext())
+    ws, n = norms._workspace(1, 2, 3, 0, cpu)
+    assert n == 48 and ws.numel() == 48
