@@ -641,15 +641,15 @@ orbit_status attention_workspace_size(orbit_attention p, int64_t D, int32_t back
  *   out        [token][head][D], bf16 or fp32; it does not overlap the inputs (one that begins where an input does is
  *              refused).  A query that sees no key gets zeros; tokens of no sequence are left as they were
  *   D          a multiple of 8 up to 128
- *   scale      finite, above 0
+ *   scale      finite, above 0, and so 1.44 times it
  *   lse        device, fp32 [token][heads], or NULL: the logarithm of each row's sum of exponentials, -inf where it sees no key
  *   workspace  attention_workspace_size bytes, aligned to 16; contents and ownership as for orbit_qlinear_ws
  * Scores, maxima and sums are fp32; probabilities enter the product with v in bf16, whose sum is fp32 and is rounded once.
  * The same plan and inputs give the same bits.  A value that is not finite in a key or value may show, as a NaN, in every
  * query of its sequence that shares a tile of up to 256 rows with one that sees it; rows of other sequences do not depend on it.
  * Data and strides are multiples of 16 bytes, a token's stride at most 2^24 values.  Errors: ORBIT_EINVAL (null pointers,
- * types, strides, alignment, scale, a plan without tables on the device); ORBIT_EUNSUPPORTED (D); ORBIT_EHIP.  A plan
- * without queries returns at once.
+ * types, strides, alignment, scale, a plan without tables on the device); ORBIT_EUNSUPPORTED (D, scale beyond 2.3e38);
+ * ORBIT_EHIP.  A plan without queries returns at once.
  */
 orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_heads* k, const orbit_heads* v,
                        const orbit_heads* out, int64_t D, float scale, float* lse, void* workspace, size_t workspace_bytes,
@@ -667,7 +667,7 @@ orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_head
  * Sums are fp32, in a fixed order (the same bits each time); p and ds enter their products in bf16.  Refused
  * (ORBIT_EINVAL) for a plan whose sequences share keys.  Values that are not finite spread as with attention, over keys that
  * share a tile of 128 too.  Other limits and errors as for attention; ORBIT_EUNSUPPORTED also where the heads of a group in
- * q or dout lie more than 2^29 values apart.
+ * q or dout lie more than 2^29 values apart, and for scales below 2^-100 (lse / scale leaves fp32's range).
  */
 orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, const orbit_heads* q, const orbit_heads* k,
                                 const orbit_heads* v, const orbit_heads* out, const float* lse, const orbit_heads* dq,

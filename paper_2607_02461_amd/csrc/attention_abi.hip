@@ -2,6 +2,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -232,6 +233,17 @@ size_t backward_bytes(orbit_attention p, int64_t D) {
     return (2 * stat_floats(p) + (size_t)std::max(of_rows, of_keys) * p->kv_heads) * sizeof(float);
 }
 
+constexpr double kLog2e = 1.4426950408889634;
+
+// `least`: backward, so that rows' sums in units of scores, -lse / scale, stay within fp32's range.
+orbit_status check_scale(const char* who, float scale, float least) {
+    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ORBIT_EINVAL, "%s: scale must be finite and above 0", who);
+    if (scale * kLog2e > FLT_MAX || scale < least) return fail(ORBIT_EUNSUPPORTED, "%s: scale %g is beyond fp32's range of scores", who, scale);
+    return ORBIT_OK;
+}
+
+constexpr float kLeastBackward = 0x1p-100f;
+
 // The backward pass finds a tile's heads by 32-bit offsets
 orbit_status check_group(const char* who, const char* name, const AttnHeads& t, int group) {
     if (group > 1 && t.head > ((int64_t)1 << 29) / group) return fail(ORBIT_EUNSUPPORTED, "%s: %s's heads lie more than 2^29 values apart", who, name);
@@ -335,7 +347,8 @@ orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_head
     clear_error();
     orbit_status st = check_dim(who, p, D);
     if (st != ORBIT_OK) return st;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ORBIT_EINVAL, "%s: scale must be finite and above 0", who);
+    st = check_scale(who, scale, 0.f);
+    if (st != ORBIT_OK) return st;
     if (p->q_tokens == 0) return ORBIT_OK;
     AttnParams a{};
     st = check_heads(who, "q", q, p->q_tokens, p->heads, D, false, false, &a.q);
@@ -360,7 +373,7 @@ orbit_status attention(orbit_attention p, const orbit_heads* q, const orbit_head
     a.group = p->heads / p->kv_heads;
     a.D = (int)D;
     a.causal = p->causal;
-    a.scale = (float)(scale * 1.4426950408889634);
+    a.scale = (float)(scale * kLog2e);
     a.out_f32 = out->dtype == ORBIT_OUT_F32;
     a.lse = lse;
     a.part = (float*)workspace;
@@ -387,7 +400,8 @@ orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, cons
     clear_error();
     orbit_status st = check_dim(who, p, D);
     if (st != ORBIT_OK) return st;
-    if (!(scale > 0.f) || !std::isfinite(scale)) return fail(ORBIT_EINVAL, "%s: scale must be finite and above 0", who);
+    st = check_scale(who, scale, kLeastBackward);
+    if (st != ORBIT_OK) return st;
     if (p->shared_keys) return fail(ORBIT_EINVAL, "%s: two of the plan's sequences have a key in common", who);
     AttnGradParams a{};
     st = check_heads(who, "dout", dout, p->q_tokens, p->heads, D, false, false, &a.g);
@@ -428,7 +442,7 @@ orbit_status attention_backward(orbit_attention p, const orbit_heads* dout, cons
     a.causal = p->causal;
     a.o_f32 = out && out->dtype == ORBIT_OUT_F32;
     a.q_tokens = p->q_tokens;
-    a.scale = (float)(scale * 1.4426950408889634);
+    a.scale = (float)(scale * kLog2e);
     a.out_scale = scale;
     a.lse = lse;
     a.lse2 = (float*)workspace;

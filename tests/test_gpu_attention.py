@@ -257,6 +257,15 @@ def test_flat_and_sharp_rows(sharp):
     b.check(o, b.backward(o))
 
 
+@pytest.mark.parametrize("scale,size", [(2.0 ** -100, 1.0), (2.0 ** 100, 2.0 ** -101)])
+def test_smallest_and_large_scales(scale, size):
+    b = Batch([90], [130], 4, 2, 64, True, 32, sharp=scale * 8.0)
+    assert b.scale == scale
+    b.q.mul_(size)
+    o = b.forward()
+    b.check(o, b.backward(o))
+
+
 def test_scores_that_rise_and_fall_along_the_keys():
     # the running maximum rises at every tile, or is the first key's; both after and before keys with no weight
     b = Batch([40], [640], 1, 1, 64, False, 7)

@@ -194,3 +194,19 @@ def test_workspace_sizes_survive_another_threads_clearing(monkeypatch, known):
     monkeypatch.setattr(torch.cuda, "device", lambda dev: contextlib.nullcontext())
     ws, n = norms._workspace(1, 2, 3, 0, cpu)
     assert n == 48 and ws.numel() == 48
+
+
+@pytest.mark.parametrize("scale,backward", [(2.4e38, 0), (3.4e38, 0), (3.4e38, 1), (1e-38, 1), (1e-45, 1), (5e-31, 1)])
+def test_scales_whose_scores_leave_fp32_are_refused(scale, backward):
+    # forward, scores in units of log 2 are scale * 1.44; the backward pass measures rows' sums in units of scores, lse / scale
+    plan = oq.attention_plan([40], [50], heads=4, kv_heads=2)
+
+    def heads(i, n):
+        return ctypes.byref(Heads(FAKE[i], 0, n * 64, 64, n, 1))
+
+    q, k, v, out, dout, dq, dk, dv = (heads(i, n) for i, n in enumerate((4, 2, 2, 4, 4, 4, 2, 2)))
+    if backward:
+        st = oq.lib().attention_backward(plan.handle, dout, q, k, v, out, 1 << 20, dq, dk, dv, 64, scale, FAKE[8], 1 << 40, None)
+    else:
+        st = oq.lib().attention(plan.handle, q, k, v, out, 64, scale, None, None, 0, None)
+    assert st == 2 and "scale" in oq.lib().orbit_last_error().decode()
