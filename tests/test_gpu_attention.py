@@ -219,6 +219,55 @@ def test_ways_of_the_forward_pass(rows, keys, heads, kv_heads, causal, ways):
     assert [r.kernel for r in launches(lambda: b.forward(out=o))] == ways
 
 
+@pytest.mark.parametrize("D,instance", [(24, 32), (64, 64), (96, 96), (128, 128)])
+@pytest.mark.parametrize("causal", [False, True])
+def test_wide_tiles_of_every_head_size_and_in_parts(D, instance, causal):
+    # 64 sequences of up to 256 rows over one cache, one of them over many times the others' keys: its tile is divided, and parts
+    # of 256 rows are joined
+    heads, ql, most = 8, [256, 250, 130] + [256] * 61, (16500, 120000) if causal else (8200, 60000)
+    kl = [most[0] + i for i in range(63)] + [most[1]]
+    b = Batch(ql, kl, heads, heads, D, causal, 33, k_starts=[0] * 64)
+    o = b.forward()
+    for i in (0, 2, 63):
+        nq, nk = ql[i], kl[i]
+        for first, end in ((0, 20), (nq - 20, nq)):
+            rows, keys = slice(b.qs[i] + first, b.qs[i] + end), slice(0, nk - (nq - end) if causal else nk)
+            for h in (0, 7):
+                one = slice(h, h + 1)
+                _check_sequence(f"sequence {i} from {first}, head {h}", b.q[rows, one], b.k[keys, one], b.v[keys, one], b.scale, causal, o[rows, one],
+                                b.lse[rows, one])
+    assert [r.kernel for r in launches(lambda: b.forward(out=o))] == [f"attention_kernel<{instance},8>", f"attention_join_kernel<{instance}>"]
+    assert torch.equal(b.forward(), o)
+
+
+def test_a_long_clip_against_sampled_rows():
+    # 32760 tokens: rows from the beginning, a tile's edges and the end, forward and backward
+    n, heads, D = 32760, 2, 128
+    b = Batch([n], None, heads, heads, D, False, 34)
+    o = b.forward()
+    dq, dk, dv = b.backward(o)
+    rows = [0, 1, 127, 128, 20000, n - 1]
+    _check_sequence("rows", b.q[rows], b.k, b.v, b.scale, False, o[rows], b.lse[rows])
+    # dq of those rows alone: as if they were all the queries that there are (their bars do not depend on other rows)
+    q, k, v, do = (_f64(t) for t in (b.q[rows], b.k, b.v, b.do[rows]))
+    ref, lse = oracle.attention(q, k, v, b.scale)
+    p, _ = oracle.attention_probabilities(q, k, b.scale, False)
+    want = oracle.attention_backward(do, q, k, v, b.scale)[0]
+    grown = lambda m: 10 * math.sqrt(m) * U  # noqa: E731
+    for h in range(heads):
+        qh, kh, vh, gh = q[:, h], k[:, h], v[:, h], do[:, h]
+        dp, delta = gh @ vh.T, (gh * ref[:, h]).sum(1, keepdims=True)
+        E = (2 * grown(D) * (b.scale * np.abs(qh) @ np.abs(kh).T) + 32 * U * (1 + np.abs(b.scale * qh @ kh.T))).max(1, keepdims=True) + 32 * U * np.abs(lse[:, h:h + 1])
+        off_o = HALF[BF16] * np.abs(ref[:, h]) + (H + 2 * E + grown(n)) * (p[h] @ np.abs(vh)) + T * (1 + np.abs(vh)).sum(0)
+        err = p[h] * ((2 * E + H) * np.abs(dp - delta) + grown(D) * (np.abs(gh) @ np.abs(vh).T + (np.abs(gh) * np.abs(ref[:, h])).sum(1, keepdims=True))
+                      + (np.abs(gh) * off_o).sum(1, keepdims=True)) + T * (1 + np.abs(dp - delta))
+        bar = HALF[BF16] * np.abs(want[:, h]) + b.scale * ((err + grown(n) * p[h] * np.abs(dp - delta)) @ np.abs(kh) + n * T)
+        _within(f"dq, head {h}", dq[rows, h], want[:, h], bar)
+    # every row of p sums to 1, so the sum of dv over keys is that of do; each dv is off by half an ulp and 2 h of its terms
+    off = HALF[BF16] * dv.double().abs().sum(0) + 2.1 * H * b.do.double().abs().sum(0)
+    assert ((dv.double().sum(0) - b.do.double().sum(0)).abs() <= off).all()
+
+
 @pytest.mark.parametrize("rows,keys,heads,kv_heads,causal,joins", [
     (900, 60, 2, 2, False, 1), (60, 900, 4, 2, True, 1), (600, 600, 4, 1, True, 2), (200, 200, 64, 64, True, 0)])
 def test_ways_of_the_backward_pass(rows, keys, heads, kv_heads, causal, joins):

@@ -219,6 +219,30 @@ def test_in_place_broadcast_inputs_and_rows_beside_the_outputs(modulate):
     assert all(torch.equal(s, t) for s, t in zip(got, want))
 
 
+@pytest.mark.parametrize("modulate", [False, True])
+@pytest.mark.parametrize("N", [63, 640])
+def test_gradients_against_differences(N, modulate):
+    # fp32 throughout: each gradient is within 256 u of its terms' size, and a central difference of step s within s^2 of the third
+    # derivative: 1e-4 in fp64 leaves some 1e-8 of a loss of that size, and its rounding 1e-16 / 1e-4
+    x, (w, b), dy = _rows(2, 9, N, F32, 61), _weights(2, N, F32, 62, modulate), _rows(2, 9, N, F32, 63)
+    forward, backward = (oq.layer_norm_modulate, oq.layer_norm_modulate_backward) if modulate else (oq.layer_norm, oq.layer_norm_backward)
+    grads = [_f64(t) for t in backward(dy, x, w)]
+    r = np.random.default_rng(3)
+    values = [_f64(t) for t in (x, w, b)]
+    along = [r.standard_normal(t.shape) for t in values]
+
+    def loss(step):
+        x, w, b = (t + step * d for t, d in zip(values, along))
+        return float((oracle.layer_norm(x, *((1 + w[:, None], b[:, None]) if modulate else (w, b))) * _f64(dy)).sum())
+
+    want = (loss(1e-4) - loss(-1e-4)) / 2e-4
+    got = sum(float((g * d).sum()) for g, d in zip(grads, along))
+    size = np.sqrt(sum(float(((g * d) ** 2).sum()) for g, d in zip(grads, along)))
+    terms = sum(float(np.abs(g * d).sum()) for g, d in zip(grads, along))
+    assert abs(got - want) <= 1e-6 * size + 256 * U * terms, (got, want, size)
+    assert forward(x, w, b).dtype == F32
+
+
 @pytest.mark.parametrize("rows,step", [(37, 1), (200, 1), (37, 3)])
 def test_rows_that_are_windows_of_a_signal(rows, step):
     # windows of 64 values that lie `step` apart
