@@ -15,6 +15,7 @@ For example p = 1.7e-41 beside do = 0.8 is the whole of a dv at 150 x 400 pairs 
 """
 
 import math
+import threading
 
 import numpy as np
 import pytest
@@ -429,6 +430,51 @@ def test_streams_devices_and_graphs():
             torch.cuda.synchronize()
         fresh = both()
         assert all(torch.equal(a, c) for h in held for a, c in zip(h, fresh))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_inputs_that_are_broadcast(D):
+    # heads, and tokens, that share their memory, given and in place of the other operands one after the other
+    b = Batch([70, 130], [90, 200], 8, 2, D, True, 35)
+    for name in ("q", "k", "v", "do"):
+        for at in ((slice(None), slice(0, 1)), (slice(0, 1),)):
+            whole = getattr(b, name)
+            view = whole[at].expand(whole.shape)
+            assert 0 in view.stride()
+            results = []
+            for t in (view, view.contiguous()):
+                setattr(b, name, t)
+                o = b.forward()
+                results.append((o, b.lse.clone()) + tuple(b.backward(o)))
+            setattr(b, name, whole)
+            assert all(torch.equal(x, y) for x, y in zip(*results)), name
+
+
+def test_calls_of_two_threads():
+    b = Batch([200, 1, 33], [300, 2000, 64], 8, 2, 64, True, 36)
+    o = b.forward()
+    want = (o,) + tuple(b.backward(o))
+    torch.cuda.synchronize()
+    errors = []
+
+    def work():
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(20):
+                    lse = torch.empty_like(b.lse)
+                    out = oq.attention(b.plan, b.q, b.k, b.v, scale=b.scale, lse=lse)
+                    got = (out,) + tuple(oq.attention_backward(b.plan, b.do, b.q, b.k, b.v, out, lse, scale=b.scale))
+                    torch.cuda.current_stream().synchronize()
+                    assert all(torch.equal(x, y) for x, y in zip(got, want))
+        except BaseException as e:  # noqa: BLE001 (of a thread: raised below)
+            errors.append(e)
+
+    threads = [threading.Thread(target=work) for _ in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not errors, errors
 
 
 def test_many_short_sequences_and_many_heads():

@@ -219,6 +219,19 @@ def test_in_place_broadcast_inputs_and_rows_beside_the_outputs(modulate):
     assert all(torch.equal(s, t) for s, t in zip(got, want))
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("N", [300, 1999, 5120])
+@pytest.mark.parametrize("size", [2.0 ** 66, 2.0 ** 100])
+def test_rows_whose_variance_passes_fp32(dtype, N, size):
+    # r is 0: the bias, and no gradient but the bias's
+    x = _rows(1, 5, N, dtype, 71) * size
+    (w, b), dy = _weights(1, N, F32, 72, False), _rows(1, 5, N, F32, 73)
+    assert torch.equal(oq.layer_norm(x, w, b, out_dtype=F32), b.expand(1, 5, N))
+    dx, dw, db = oq.layer_norm_backward(dy, x, w)
+    assert not dx.any() and not dw.any()
+    _within("db", db, _f64(dy).sum((0, 1)), (10 * 5 ** 0.5 + 64) * U * np.abs(_f64(dy)).sum((0, 1)))
+
+
 @pytest.mark.parametrize("modulate", [False, True])
 @pytest.mark.parametrize("N", [63, 640])
 def test_gradients_against_differences(N, modulate):
