@@ -573,8 +573,9 @@ typedef struct {
  * layer_norm -- the norm of each row, with a weight and a bias or modulated by its batch's scale and shift (the
  * adaptive norms of a diffusion transformer, whose scale and shift the AdaLN projection makes):
  *     y = (x - mean(x)) / sqrt(mean((x - mean(x))^2) + eps) * g + bias,     g = weight, or 1 + weight with `modulate`.
- * Computed in fp32 and rounded once; the sum of squares is one of deviations from means, also where the mean is large.
- * A row whose variance passes fp32's range gives its bias.
+ * Computed in fp32 and rounded once; the sum of squares is one of deviations from means, and a mean is kept to more than
+ * fp32's last place, also where it is large beside the deviations.  A row whose variance passes fp32's range gives its bias
+ * (and no gradient but the bias's), for values below 2^100 and sums of |dy g| over a row below 2^27.
  *   x, y       [B][L][N]; y may be x
  *   weight, bias   device, rows [N] of w_dtype, or NULL (g = 1; 0); weight_batch, bias_batch: elements from one batch's row
  *              to the next's, 0 where the batches share one.  A view of the modulation projection's output is such rows
@@ -644,7 +645,9 @@ orbit_status attention_workspace_size(orbit_attention p, int64_t D, int32_t back
  *   scale      finite, above 0, and so 1.44 times it
  *   lse        device, fp32 [token][heads], or NULL: the logarithm of each row's sum of exponentials, -inf where it sees no key
  *   workspace  attention_workspace_size bytes, aligned to 16; contents and ownership as for orbit_qlinear_ws
- * Scores, maxima and sums are fp32; probabilities enter the product with v in bf16, whose sum is fp32 and is rounded once.
+ * Scores, maxima and sums are fp32; probabilities enter the product with v in bf16, whose sum is fp32 and is rounded once
+ * (fp32 results have the error of bf16 probabilities, 2^-8 relative in each).  That sum, before it is divided, is up to 2^8
+ * times the values of v for each key: it stays within fp32's range for values up to 2^100 over 2^18 keys.
  * The same plan and inputs give the same bits.  A value that is not finite in a key or value may show, as a NaN, in every
  * query of its sequence that shares a tile of up to 256 rows with one that sees it; rows of other sequences do not depend on it.
  * Data and strides are multiples of 16 bytes, a token's stride at most 2^24 values.  Errors: ORBIT_EINVAL (null pointers,

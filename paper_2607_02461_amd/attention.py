@@ -141,8 +141,8 @@ def _inputs(plan, q, k, v):
 def attention(plan: AttentionPlan, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, scale: float = None,
               out: torch.Tensor = None, out_dtype: torch.dtype = None, lse: torch.Tensor = None) -> torch.Tensor:
     """softmax(scale q k^T) v for each query over the keys that the plan lets it see: q [tokens, heads, D], k and v [tokens,
-    kv_heads, D], scale 1 / sqrt(D) if none is given.  The output is bf16 (or fp32 with out_dtype) in q's shape: zeros where
-    a query sees no key; tokens of no sequence are left as they were in `out`, zeros in a new tensor.  `lse`: an fp32 tensor
+    kv_heads, D], scale 1 / sqrt(D) if none is given.  The output is bf16 (or fp32 with out_dtype: not rounded at the end, but
+    of probabilities that enter the product with v in bf16, 2^-8 relative, all the same) in q's shape: zeros where a query sees no key; tokens of no sequence are left as they were in `out`, zeros in a new tensor.  `lse`: an fp32 tensor
     [tokens, heads] that receives the logarithms of the rows' sums for the backward pass."""
     D, hq, hk, hv = _inputs(plan, q, k, v)
     if out_dtype is None:
@@ -161,7 +161,7 @@ def attention_backward(plan: AttentionPlan, dout: torch.Tensor, q: torch.Tensor,
                        lse: torch.Tensor, scale: float = None, q_grad: torch.Tensor = None, k_grad: torch.Tensor = None,
                        v_grad: torch.Tensor = None):
     """(q_grad, k_grad, v_grad), bf16 in the shapes of q, k and v, from dout, the gradient of attention's output in bf16, its
-    inputs, its output and its lse.  Tokens of no sequence are left as they were in gradients that are given (views of a
+    inputs, its output and its lse.  Probabilities and their gradients enter the products in bf16.  Tokens of no sequence are left as they were in gradients that are given (views of a
     fused projection's gradient, for example), zeros in new ones.  The plan's sequences share no keys."""
     D, hq, hk, hv = _inputs(plan, q, k, v)
     dev = q.device

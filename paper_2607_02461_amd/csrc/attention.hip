@@ -8,13 +8,14 @@
 // Bound by the matrix cores (4 D products and sums for each pair of a query and a key), with the exponentials beside them: 64
 // keys x 32 queries take a wave 1024 cycles of MFMA and about 750 of VALU at D = 128, which overlap between the waves of a SIMD.
 // Beside that they read 32 KB of LDS, 1400 of the card's 2048 cycles for the two waves of a SIMD.  What 4608 tokens in 24 heads of
-// 128 (two sequences) reach, 1070 TFLOP/s of matrix products, is set by power: the matrix cores are busy 52% of the time at
-// 1.75 GHz, and the same call on zeros runs a third faster.  Few queries are bound by HBM: each key and value is read once for
+// 128 (two sequences) reach, 1060 TFLOP/s of matrix products, is set by power: the matrix cores are busy 53% of the time at 1.65
+// to 1.8 GHz, and the same call on zeros runs a third faster (1400).  Few queries are bound by HBM: each key and value is read once for
 // each of its heads, 16 tokens over 4600 keys on average in 8 heads of 128 at 5.1 TB/s.
 //
-// Tried and not kept: 64 queries to a wave (its sums leave the registers, 520 TFLOP/s); sums of rounded probabilities by dot products (3% faster, but o off by 2^-6 where one key has it all); workgroups that
-// take one tile after the other, which was to hide a tile's begin (32760 tokens over 512 keys 435 us for 420; with the next tile's
-// first keys on their way during the last ones 439); waves of different priorities (no difference).
+// Tried and not kept: 64 queries to a wave (its sums leave the registers, 520 TFLOP/s); sums of rounded probabilities by dot products
+// (3% faster, but o off by 2^-6 where one key has it all); workgroups that take one tile after the other, which was to hide a tile's
+// begin (32760 tokens over 512 keys 435 us for 420; with the next tile's first keys on their way during the last ones 439, with
+// queries loaded by the compiler, which waits for all loads then); waves of different priorities (no difference).
 //
 // Rows: the queries of a group's heads lie together, row = token * group + head of the group, so that one tile of keys serves
 // all heads that share it, and a single token of grouped heads fills as much of a tile as there is.
@@ -150,7 +151,8 @@ __device__ __forceinline__ void finish(const AttnParams& p, const AttnTile& t, i
 
 // 32 rows to each wave; 64 keys at a time, shared, in two buffers.  Heads of up to 64 values have three waves to a SIMD, for which
 // fewer of V's operands are read ahead: 2048 tokens in 16 heads over 4 of 64, 16 sequences, causal, 217 -> 195 us, whole 326 ->
-// 302; 8 of 4096 in 16 heads 630 -> 593.
+// 302; 8 of 4096 in 16 heads 630 -> 593.  (These are workgroups of four waves; of those of eight a compute unit has one, two waves
+// to a SIMD, in the same registers.)
 template <int DP, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void attention_kernel(AttnParams p) {
     __shared__ __attribute__((aligned(1024))) char lds[2][2][64 * kRowBytes<DP>];
@@ -192,7 +194,9 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void attention_kernel
 }
 
 // Up to 32 rows: the workgroup's four waves have the same ones and 32 keys each at a time, in buffers of their own, so they wait
-// for their own loads alone.  64 KB of keys and values are on their way to a compute unit while as much is read.
+// for their own loads alone.  A wave's next 16 KB are on their way while it finishes a tile, but not through its products: the
+// compiler does not know that the queries have arrived and waits for all loads in front of the first product of each turn.  What
+// overlaps loads and products is the four waves, each at another place of its turn: 5.1 TB/s.
 template <int DP>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     extern __shared__ __attribute__((aligned(1024))) char few_lds[];

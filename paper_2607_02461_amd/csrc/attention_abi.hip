@@ -105,7 +105,7 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
     std::vector<Work> whole, wide, few, every, keys;
     // Wide tiles load keys and values half as often, but a compute unit has one workgroup of them, whose begin and end nothing
     // else covers: 32760 tokens in 40 heads of 128 19.0 ms instead of 20.0, 4608 tokens 512 us instead of 502, over 512 keys
-    // 442 us instead of 418.
+    // 442 us instead of 418.  (Measured at D = 128; the plan does not know D, and heads of up to 64 values go by the same rule.)
     int64_t wide_tiles = 0, wide_cost = 0;
     for (const Sequence& s : sequences) {
         const int64_t tiles = s.q_len * group > kAttnFewRows ? ceil_div(s.q_len * group, kAttnWideRows) : 0;
@@ -142,7 +142,8 @@ void fill(orbit_attention p, const std::vector<Sequence>& sequences) {
     std::vector<AttnJoin> joins, row_joins, key_joins;
     // Resident on 256 compute units: two workgroups of four waves, one of eight, or one whose buffers take the LDS.  A unit takes 0.9
     // us forward (1.2 of few rows), 1.2 for the rows' gradients and 1.6 for the keys', a join 5 to 8 us, a part's 64 KB (16 of few
-    // rows, 128 of keys) twice their time at 4.7 TB/s.
+    // rows, 128 of keys) twice their time at 4.7 TB/s.  All of that is for D = 128: the plan does not know D.  Heads of up to 64 values
+    // have three workgroups of four waves to a compute unit forward and for the keys' gradients, and units of about half the time.
     divide(whole, p->kv_heads, {512, kAttnRows, 64, 1.5, 6.0, 0.030}, &p->slots, &joins, &list[kAttnForward]);
     divide(wide, p->kv_heads, {256, kAttnWideRows, 64, 2.0, 6.0, 0.060}, &p->slots, &joins, &list[kAttnForwardWide]);
     divide(few, p->kv_heads, {256, kAttnFewRows, 128, 2.5, 3.0, 0.004}, &p->slots, &joins, &list[kAttnFew]);

@@ -7,8 +7,10 @@
 // result is added up in memory; that costs 7 products of 2 D operations for each pair instead of the 5 that there are.
 //
 // Both are bound by the matrix cores and the power that they take: 3 and 4 products for each pair beside one exponential.  At 2 x
-// 4429 tokens in 24 heads of 128 they run at 1050 and 1000 TFLOP/s of these products, busy 56% and 51% of the time.  p and ds enter
-// their products in bf16, half a step of 2^-8 relative, as q, k, v and do have it; sums are fp32.
+// 4429 tokens in 24 heads of 128 they run at 1050 and 1000 TFLOP/s of these products, busy 56% and 50% of the time at 1.8 GHz.
+// Short sequences of 64 values keep neither unit busy (7 of up to 2048 tokens in 16 heads over 4, causal: matrix cores 34% and 27%,
+// vector units 42% and 33% of the time): workgroups' begins and one round of them of unequal length.  A tile of rows begins with its
+// rows of `out`, whose loads wait for each other.  p and ds enter their products in bf16, half a step of 2^-8 relative, as q, k, v and do have it; sums are fp32.
 //
 // Tried and not kept: 64 keys to a wave of the second kernel (spills); the first kernel's scores of 64 keys before their
 // gradients, so that operands of neighbouring products are shared (spills 38 registers at D = 128, 2320 us for 1655); three

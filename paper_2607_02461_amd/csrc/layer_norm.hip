@@ -94,8 +94,8 @@ struct Columns {
     }
     // whether value i of piece c is this thread's own
     __device__ __forceinline__ bool own(int c, int i) const { return have(c) && (!CUT || (C == 1 && small ? i < small : i >= skip(c))); }
-    // Only the last piece can lie behind the row (`shape` gives the fewest).  Said with CUT: 32760 x 5118 930 -> 297 us backward and
-    // 234 -> 197 forward in fp32.  Not without it, where a branch for each piece is faster: 32760 x 5120 294 us for 335 backward in
+    // Only the last piece can lie behind the row (`shape` gives the fewest).  Said with CUT: 32760 x 5118 930 -> 312 us backward and
+    // 234 -> 199 forward in fp32.  Not without it, where a branch for each piece is faster: 32760 x 5120 294 us for 335 backward in
     // fp32, with as many rows on their way as there are else with 8 waves, though 8858 x 3072 in bf16 20.4 for 19.0 forward.
     __device__ __forceinline__ bool have(int c) const { return !CUT ? within[c] : c < C - 1 || last; }
     __device__ __forceinline__ int skip(int c) const { return c < C - 1 ? 0 : cut; }
