@@ -194,9 +194,9 @@ __global__ __launch_bounds__(64 * WAVES, DP <= 64 ? 3 : 2) void attention_kernel
 }
 
 // Up to 32 rows: the workgroup's four waves have the same ones and 32 keys each at a time, in buffers of their own, so they wait
-// for their own loads alone.  A wave's next 16 KB are on their way while it finishes a tile, but not through its products: the
-// compiler does not know that the queries have arrived and waits for all loads in front of the first product of each turn.  What
-// overlaps loads and products is the four waves, each at another place of its turn: 5.1 TB/s.
+// for their own loads alone.  A wave asks for its next tile before a tile's products, but does not multiply beside those loads:
+// the compiler does not know that the queries have arrived and waits for all loads in front of the first product of each turn.
+// What overlaps loads and products is the four waves, each at another place of its turn: 5.1 TB/s.
 template <int DP>
 __global__ __launch_bounds__(256) void attention_few_kernel(AttnParams p) {
     extern __shared__ __attribute__((aligned(1024))) char few_lds[];
